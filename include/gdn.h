@@ -54,7 +54,8 @@ typedef enum gdn_status {
                                   workgroups gave up (gdn_workspace_status)       */
 } gdn_status;
 
-typedef enum gdn_dtype { GDN_F32 = 0, GDN_BF16 = 1 } gdn_dtype;
+/* GDN_E4M3: 8-bit floats (4 exponent bits, 3 mantissa bits, no infinities, largest 448), the paged cache only. */
+typedef enum gdn_dtype { GDN_F32 = 0, GDN_BF16 = 1, GDN_E4M3 = 2 } gdn_dtype;
 
 /* Bit flags of the _ex entry points: input transforms done inside the kernels,
    and at most one evaluation plan (none: the library chooses). */
@@ -64,7 +65,8 @@ typedef enum gdn_flags {
     GDN_PLAN_SEQUENTIAL = 16,  /* one chain over every chunk of a sequence                             */
     GDN_PLAN_SEGMENTED = 32,   /* segment-parallel, narrow: one workgroup per 16 state rows             */
     GDN_PLAN_WIDE = 64,        /* segment-parallel, wide: a workgroup holds a whole state               */
-    GDN_TEST_WITHHOLD = 256    /* test only: forces the failure path of the one-launch form's wait      */
+    GDN_TEST_WITHHOLD = 256,   /* test only: forces the failure path of the one-launch form's wait      */
+    GDN_ROPE_INTERLEAVED = 512 /* gdn_qk_norm_rope, gdn_kv_append: channels (2i, 2i + 1) rotate together */
 } gdn_flags;
 
 /* Library version, (major << 16) | minor. */
@@ -390,6 +392,109 @@ gdn_status gdn_attention_prefill(const void* q, const void* k, const void* v, vo
                                  int B, int T, int H, int H_kv, int d,
                                  const int32_t* cu_seqlens, int n_seqs,
                                  int io_dtype, float scale, void* stream);
+
+/*
+ * Norms of queries and keys per head, with the position rotation in the same
+ * pass (section 3's batched per-position norms and rotary), for a prompt's
+ * attention layers ahead of gdn_attention_prefill.  Per (token, head) row x:
+ *
+ *     y = x * w / sqrt(mean(x^2) + eps)                    (w NULL: y = x)
+ *     (y_a, y_b) <- (y_a cos - y_b sin, y_b cos + y_a sin) for each pair i < rot / 2,
+ *         angle = position * inv_freq[i];  (a, b) = (i, i + rot / 2), or with
+ *         GDN_ROPE_INTERLEAVED (2 i, 2 i + 1); channels from rot on stay as they are
+ *
+ *   q, k          [B, T, H, d], [B, T, H_kv, d]  io_dtype (GDN_F32 or GDN_BF16); a token's rows
+ *                 are contiguous, q_stride / k_stride elements from one token to the next (at least
+ *                 H d / H_kv d, a multiple of 16 bytes): parts of a fused projection's rows, say
+ *   q_out, k_out  the same shapes, contiguous; q_out may be q (k_out k) where its stride is H d (H_kv d)
+ *   d             64 or 128;  1 <= H_kv <= H, H_kv divides H;  T >= 0
+ *   q_weight, k_weight  [d] fp32, or NULL for no norm
+ *   inv_freq, rot [rot / 2] float64 (radians per position) and the channels that rotate, a multiple
+ *                 of 16 up to d; or NULL and 0.  The angle is formed in float64.
+ *   positions     [B, T] int32, or NULL: a token's index in its sequence
+ *   cu_seqlens, n_seqs  packed sequences as in gdn_attention_prefill, or NULL and 0; rows behind the
+ *                 last sequence are left as they were
+ *   flags         0 or GDN_ROPE_INTERLEAVED
+ * Norms are summed and applied in fp32 and each output is rounded once.  Tensors start on 16-byte
+ * boundaries.  Errors: GDN_ERR_INVALID_ARG, GDN_ERR_UNSUPPORTED (another d, a rot that is no
+ * multiple of 16).
+ */
+gdn_status gdn_qk_norm_rope(const void* q, const void* k, void* q_out, void* k_out,
+                            int B, int T, int H, int H_kv, int d, long long q_stride, long long k_stride,
+                            const float* q_weight, const float* k_weight, float eps,
+                            const double* inv_freq, int rot, const int32_t* positions,
+                            const int32_t* cu_seqlens, int n_seqs,
+                            int io_dtype, int flags, void* stream);
+
+/*
+ * The paged cache of an attention layer, shared by the next two entry points.
+ *
+ *   k_cache, v_cache  [n_pages, H_kv, page, d]  cache_dtype (GDN_BF16 or GDN_E4M3);
+ *                     page = 16, 32, 64 or 128 tokens
+ *   k_scale, v_scale  [n_pages, H_kv] fp32, GDN_E4M3 only (NULL for GDN_BF16): a code stands for
+ *                     code * scale of its page and head
+ *   block_table       [n, max_pages] int32 DEVICE: the page that holds positions b * page ..
+ *                     of sequence s is block_table[s, b].  An entry outside [0, n_pages) is a
+ *                     page that is not there: appending writes nothing to it, attention leaves
+ *                     its keys out.  So are positions from max_pages * page on.
+ *   seq_lens          [n] int32 DEVICE: tokens of each sequence with this step's new ones (n = B
+ *                     or n_seqs): the i-th of m new tokens stands at position seq_lens[s] - m + i
+ *   cu_seqlens, n_seqs  the new tokens packed as in gdn_attention_prefill (a padded batch: T rows
+ *                     of which cu_seqlens[n_seqs] are used; rows behind the last sequence are
+ *                     neither read nor written), or NULL and 0: T new tokens for each of B sequences
+ *
+ * gdn_kv_append puts the new tokens' keys and values there, the keys normed and rotated as
+ * gdn_qk_norm_rope does, and, where q is given, writes the queries so treated to q_out.
+ *
+ *   q, q_out          [B, T, H, d] bf16 (strided as there; q_out contiguous), or both NULL
+ *   k, v              [B, T, H_kv, d] bf16, strided likewise; v is stored as given
+ *   io_dtype          GDN_BF16
+ * GDN_E4M3: the scale of a page and head is the smallest power of two s >= 2^-100 with every finite
+ * value at most 448 s; keys and values are rounded to it once, from fp32, to nearest even; a value
+ * that is not finite is stored as NaN.  A page that already holds tokens of the sequence (the step's
+ * first slot in it is not 0) keeps a scale that is large enough; otherwise its earlier codes are
+ * brought to the larger one (exactly, but for codes that become subnormal).  A page whose slot 0 is
+ * written takes a new scale.  Slots that no token of the step falls on keep their codes.
+ * Two sequences that write one page in one call race.
+ */
+gdn_status gdn_kv_append(const void* q, const void* k, const void* v, void* q_out,
+                         void* k_cache, void* v_cache, float* k_scale, float* v_scale,
+                         const int32_t* block_table, const int32_t* seq_lens,
+                         int B, int T, int H, int H_kv, int d, int page, int n_pages, int max_pages,
+                         long long q_stride, long long k_stride, long long v_stride,
+                         const float* q_weight, const float* k_weight, float eps,
+                         const double* inv_freq, int rot,
+                         const int32_t* cu_seqlens, int n_seqs,
+                         int io_dtype, int cache_dtype, int flags, void* stream);
+
+/*
+ * Workspace (device scratch, bytes) of gdn_attention_paged for these sizes (n_seqs = 0: dense).
+ * Pure host arithmetic; 0 for arguments that it would reject, and where none is needed.
+ */
+size_t gdn_attention_paged_workspace_bytes(int B, int T, int H, int H_kv, int d, int page, int max_pages, int n_seqs);
+
+/*
+ * Causal softmax attention of a step's new tokens over the paged cache that holds them and what came
+ * before: one token a sequence (decoding), a few, or a long piece of a prompt.  The new token at
+ * position p (see above) attends the sequence's positions 0 .. p that are in the cache:
+ *
+ *     o_i = sum_{j <= p} softmax_j(scale q_i . k_j) v_j     (k, v of head h / (H / H_kv))
+ *
+ *   q, o   [B, T, H, d]  bf16, contiguous; a row that no key is left for becomes zeros
+ *   scale  multiplies q . k (1 / sqrt(d) gives the usual attention)
+ *   workspace, workspace_bytes  at least gdn_attention_paged_workspace_bytes(...), 256-byte aligned
+ *          (its contents on entry are ignored); NULL and 0 where that is 0.  Calls that may overlap
+ *          in time, captured graphs among them, need one each.
+ * Slots of the cache behind a sequence's length are not read into results, whatever they hold.
+ * Errors as gdn_attention_prefill, and GDN_ERR_WORKSPACE.
+ */
+gdn_status gdn_attention_paged(const void* q, const void* k_cache, const void* v_cache,
+                               const float* k_scale, const float* v_scale,
+                               const int32_t* block_table, const int32_t* seq_lens, void* o,
+                               int B, int T, int H, int H_kv, int d, int page, int n_pages, int max_pages,
+                               const int32_t* cu_seqlens, int n_seqs,
+                               int io_dtype, int cache_dtype, float scale,
+                               void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -21,17 +21,21 @@ __all__ = [
     "gdn_chunk_prefill_grouped", "gdn_decode_step_grouped", "gdn_chunk_prefill_ex", "gdn_decode_step_ex",
     "GDN_QK_L2NORM", "GDN_GATE_LOGITS", "gdn_attention_prefill", "gdn_chunk_prefill_snapshots_ex",
     "gdn_workspace_status", "GDN_ERR_WAIT", "GDN_TEST_WITHHOLD",
+    "GDN_E4M3", "GDN_ROPE_INTERLEAVED", "gdn_qk_norm_rope", "gdn_kv_append", "gdn_attention_paged",
+    "gdn_attention_paged_workspace_bytes",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libgdn.so")
 
-GDN_F32, GDN_BF16 = 0, 1
+GDN_F32, GDN_BF16, GDN_E4M3 = 0, 1, 2
 GDN_QK_L2NORM, GDN_GATE_LOGITS = 1, 2
 GDN_PLAN_SEQUENTIAL, GDN_PLAN_SEGMENTED, GDN_PLAN_WIDE = 16, 32, 64
 GDN_TEST_WITHHOLD = 256
+GDN_ROPE_INTERLEAVED = 512
 GDN_ERR_WAIT = 5
 _IO = {torch.float32: GDN_F32, torch.bfloat16: GDN_BF16}
+_CACHE = {torch.bfloat16: GDN_BF16, torch.float8_e4m3fn: GDN_E4M3}
 _lib = None
 
 
@@ -81,6 +85,15 @@ def lib():
         L.gdn_decode_step_ex.restype = I
         L.gdn_attention_prefill.argtypes = [P, P, P, P, I, I, I, I, I, P, I, I, F, P]
         L.gdn_attention_prefill.restype = I
+        LL = ctypes.c_longlong
+        L.gdn_qk_norm_rope.argtypes = [P, P, P, P, I, I, I, I, I, LL, LL, P, P, F, P, I, P, P, I, I, I, P]
+        L.gdn_qk_norm_rope.restype = I
+        L.gdn_kv_append.argtypes = [P] * 10 + [I] * 8 + [LL] * 3 + [P, P, F, P, I, P, I, I, I, I, P]
+        L.gdn_kv_append.restype = I
+        L.gdn_attention_paged_workspace_bytes.argtypes = [I] * 8
+        L.gdn_attention_paged_workspace_bytes.restype = S
+        L.gdn_attention_paged.argtypes = [P] * 8 + [I] * 8 + [P, I, I, I, F, P, S, P]
+        L.gdn_attention_paged.restype = I
         L.gdn_workspace_status.argtypes = [P, S, P]
         L.gdn_workspace_status.restype = I
         _lib = L
@@ -390,4 +403,185 @@ def gdn_attention_prefill(q, k, v, *, scale=None, cu_seqlens=None, o=None):
     sc = float(scale) if scale is not None else 1.0 / float(d) ** 0.5
     _check(lib().gdn_attention_prefill(_ptr(q), _ptr(k), _ptr(v), _ptr(o), B, T, H, Hkv, d, _ptr(cu_seqlens), n_seqs,
                                        GDN_BF16, sc, _stream(q.device)))
+    return o
+
+
+def _same_device(device, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError("%s is on %s, q or k on %s" % (name, t.device, device))
+
+
+def _rows(t, name, dtype):
+    """Elements between neighbouring tokens of t [B,T,heads,d]: a token's rows contiguous, tokens equally far apart."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a CUDA (HIP) tensor" % name)
+    if t.dtype is not dtype:
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if t.dim() != 4:
+        raise ValueError("%s must be [B, T, heads, d], got %s" % (name, tuple(t.shape)))
+    B, T, h, d = t.shape
+    if t.is_contiguous():
+        return h * d
+    sb, st, sh, sd = t.stride()
+    if (sd != 1 and d > 1) or (sh != d and h > 1) or (B > 1 and T > 1 and sb != T * st):
+        raise ValueError("%s: a token's rows must be contiguous and the tokens equally far apart" % name)
+    return st if T > 1 else sb if B > 1 else h * d
+
+
+def _out(t, like, name, shape, dtype):
+    if t is None:
+        return torch.empty(shape, device=like.device, dtype=dtype)
+    _dev(t, name, dtype)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must be %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    return t
+
+
+def _turn_args(d, q_weight, k_weight, inv_freq):
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None:
+            _dev(w, name, torch.float32)
+            if tuple(w.shape) != (d,):
+                raise ValueError("%s must be [%d], got %s" % (name, d, tuple(w.shape)))
+    if inv_freq is None:
+        return 0
+    _dev(inv_freq, "inv_freq", torch.float64)
+    return 2 * inv_freq.numel()
+
+
+def _packed(cu_seqlens, B):
+    if cu_seqlens is None:
+        return 0, B
+    _dev(cu_seqlens, "cu_seqlens", torch.int32)
+    n_seqs = cu_seqlens.numel() - 1
+    return n_seqs, n_seqs
+
+
+def _cache_args(k_cache, v_cache, k_scale, v_scale, block_table, seq_lens, n, Hkv, d):
+    if not isinstance(k_cache, torch.Tensor) or k_cache.dtype not in _CACHE:
+        raise TypeError("k_cache must be bfloat16 or float8_e4m3fn")
+    _dev(k_cache, "k_cache")
+    _dev(v_cache, "v_cache", k_cache.dtype)
+    _dev(block_table, "block_table", torch.int32)
+    _dev(seq_lens, "seq_lens", torch.int32)
+    if k_cache.dim() != 4 or k_cache.shape[1] != Hkv or k_cache.shape[3] != d or v_cache.shape != k_cache.shape:
+        raise ValueError("k_cache and v_cache must be [n_pages, %d, page, %d], got %s and %s" % (
+            Hkv, d, tuple(k_cache.shape), tuple(v_cache.shape)))
+    if block_table.dim() != 2 or block_table.shape[0] != n or tuple(seq_lens.shape) != (n,):
+        raise ValueError("block_table must be [%d, max_pages] and seq_lens [%d], got %s and %s" % (
+            n, n, tuple(block_table.shape), tuple(seq_lens.shape)))
+    for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+        if (t is None) != (k_cache.dtype is torch.bfloat16):
+            raise ValueError("%s belongs to a float8_e4m3fn cache, and to no other" % name)
+        if t is not None:
+            _dev(t, name, torch.float32)
+            if tuple(t.shape) != tuple(k_cache.shape[:2]):
+                raise ValueError("%s must be %s, got %s" % (name, tuple(k_cache.shape[:2]), tuple(t.shape)))
+    return k_cache.shape[2], k_cache.shape[0], block_table.shape[1], _CACHE[k_cache.dtype]
+
+
+def _on(device, call, *args):
+    """call(*args, the current stream of `device`), with that device current."""
+    if device.index == torch.cuda.current_device():
+        return _check(call(*args, _stream(device)))
+    with torch.cuda.device(device):
+        return _check(call(*args, _stream(device)))
+
+
+def gdn_qk_norm_rope(q, k, *, q_weight=None, k_weight=None, eps=1e-6, inv_freq=None, interleaved=False, positions=None,
+                     cu_seqlens=None, q_out=None, k_out=None):
+    """Norms of queries and keys per head and the position rotation; see ``gdn_qk_norm_rope`` in include/gdn.h.
+
+    q [B,T,H,d] and k [B,T,H_kv,d], bf16 or fp32 CUDA tensors, may be parts of a wider projection's rows;
+    ``q_weight``, ``k_weight`` [d] fp32; ``inv_freq`` [rot/2] float64; ``positions`` [B,T] int32 (default: a token's
+    index in its sequence).  Returns (q_out, k_out), contiguous.
+    """
+    if not isinstance(q, torch.Tensor) or q.dtype not in _IO:
+        raise TypeError("q must be float32 or bfloat16")
+    qs, ks = _rows(q, "q", q.dtype), _rows(k, "k", q.dtype)
+    B, T, H, d = q.shape
+    Hkv = k.shape[2]
+    if tuple(k.shape) != (B, T, Hkv, d):
+        raise ValueError("inconsistent shapes q%s k%s" % (tuple(q.shape), tuple(k.shape)))
+    rot = _turn_args(d, q_weight, k_weight, inv_freq)
+    n_seqs, _ = _packed(cu_seqlens, B)
+    if positions is not None:
+        _dev(positions, "positions", torch.int32)
+        if tuple(positions.shape) != (B, T):
+            raise ValueError("positions must be [%d, %d], got %s" % (B, T, tuple(positions.shape)))
+    q_out, k_out = _out(q_out, q, "q_out", q.shape, q.dtype), _out(k_out, k, "k_out", k.shape, k.dtype)
+    _same_device(q.device, k=k, q_weight=q_weight, k_weight=k_weight, inv_freq=inv_freq, positions=positions,
+                 cu_seqlens=cu_seqlens, q_out=q_out, k_out=k_out)
+    _on(q.device, lib().gdn_qk_norm_rope, _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), B, T, H, Hkv, d, qs, ks,
+        _ptr(q_weight), _ptr(k_weight), float(eps), _ptr(inv_freq), rot, _ptr(positions), _ptr(cu_seqlens), n_seqs,
+        _IO[q.dtype], GDN_ROPE_INTERLEAVED if interleaved else 0)
+    return q_out, k_out
+
+
+def gdn_kv_append(k, v, k_cache, v_cache, block_table, seq_lens, *, q=None, q_out=None, k_scale=None, v_scale=None,
+                  q_weight=None, k_weight=None, eps=1e-6, inv_freq=None, interleaved=False, cu_seqlens=None):
+    """New tokens' keys and values into a paged cache; see ``gdn_kv_append`` in include/gdn.h.
+
+    k, v [B,T,H_kv,d] (and q [B,T,H,d]) bf16, parts of a wider projection's rows or not; caches
+    [n_pages,H_kv,page,d] bf16 or float8_e4m3fn, updated in place, with ``k_scale``, ``v_scale`` [n_pages,H_kv] fp32 for
+    the latter; ``block_table`` [n,max_pages] and ``seq_lens`` [n] (with the new tokens) int32.  Norm and rotation as
+    ``gdn_qk_norm_rope``.  Returns q_out (None without q).
+    """
+    ks, vs = _rows(k, "k", torch.bfloat16), _rows(v, "v", torch.bfloat16)
+    B, T, Hkv, d = k.shape
+    if v.shape != k.shape:
+        raise ValueError("inconsistent shapes k%s v%s" % (tuple(k.shape), tuple(v.shape)))
+    H, qs = Hkv, 0
+    if q is not None:
+        qs, H = _rows(q, "q", torch.bfloat16), q.shape[2]
+        if tuple(q.shape) != (B, T, H, d):
+            raise ValueError("inconsistent shapes q%s k%s" % (tuple(q.shape), tuple(k.shape)))
+        q_out = _out(q_out, q, "q_out", q.shape, q.dtype)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    rot = _turn_args(d, q_weight, k_weight, inv_freq)
+    n_seqs, n = _packed(cu_seqlens, B)
+    page, n_pages, max_pages, ct = _cache_args(k_cache, v_cache, k_scale, v_scale, block_table, seq_lens, n, Hkv, d)
+    _same_device(k.device, v=v, q=q, q_out=q_out, k_cache=k_cache, v_cache=v_cache, k_scale=k_scale, v_scale=v_scale,
+                 block_table=block_table, seq_lens=seq_lens, q_weight=q_weight, k_weight=k_weight, inv_freq=inv_freq,
+                 cu_seqlens=cu_seqlens)
+    _on(k.device, lib().gdn_kv_append, _ptr(q), _ptr(k), _ptr(v), _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale),
+        _ptr(v_scale), _ptr(block_table), _ptr(seq_lens), B, T, H, Hkv, d, page, n_pages, max_pages, qs, ks, vs,
+        _ptr(q_weight), _ptr(k_weight), float(eps), _ptr(inv_freq), rot, _ptr(cu_seqlens), n_seqs, GDN_BF16, ct,
+        GDN_ROPE_INTERLEAVED if interleaved else 0)
+    return q_out
+
+
+def gdn_attention_paged_workspace_bytes(B, T, H, H_kv, d, page, max_pages, n_seqs=0) -> int:
+    return int(lib().gdn_attention_paged_workspace_bytes(B, T, H, H_kv, d, page, max_pages, n_seqs))
+
+
+def gdn_attention_paged(q, k_cache, v_cache, block_table, seq_lens, *, k_scale=None, v_scale=None, scale=None,
+                        cu_seqlens=None, o=None, workspace=None):
+    """Causal attention of new tokens over a paged cache; see ``gdn_attention_paged`` in include/gdn.h.
+
+    q [B,T,H,d] bf16, T new tokens for each of B sequences, or packed (B == 1) with ``cu_seqlens`` int32 [n+1]; the cache
+    and its tables as ``gdn_kv_append``, which has put the new tokens there; ``scale`` defaults to 1/sqrt(d).  Returns o.
+    """
+    _dev(q, "q", torch.bfloat16)
+    if q.dim() != 4:
+        raise ValueError("q must be [B, T, heads, d], got %s" % (tuple(q.shape),))
+    B, T, H, d = q.shape
+    n_seqs, n = _packed(cu_seqlens, B)
+    Hkv = k_cache.shape[1] if isinstance(k_cache, torch.Tensor) and k_cache.dim() == 4 else 0
+    page, n_pages, max_pages, ct = _cache_args(k_cache, v_cache, k_scale, v_scale, block_table, seq_lens, n, Hkv, d)
+    o = _out(o, q, "o", q.shape, q.dtype)
+    if workspace is None:
+        need = gdn_attention_paged_workspace_bytes(B, T, H, Hkv, d, page, max_pages, n_seqs)
+        workspace = torch.empty(need, device=q.device, dtype=torch.uint8) if need else None
+    else:
+        _dev(workspace, "workspace", torch.uint8)
+    _same_device(q.device, k_cache=k_cache, v_cache=v_cache, k_scale=k_scale, v_scale=v_scale, block_table=block_table,
+                 seq_lens=seq_lens, cu_seqlens=cu_seqlens, o=o, workspace=workspace)
+    sc = float(scale) if scale is not None else 1.0 / float(d) ** 0.5
+    ws, ws_bytes = (None, 0) if workspace is None or workspace.numel() == 0 else (_ptr(workspace), workspace.numel())
+    _on(q.device, lib().gdn_attention_paged, _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale),
+        _ptr(block_table), _ptr(seq_lens), _ptr(o), B, T, H, Hkv, d, page, n_pages, max_pages, _ptr(cu_seqlens), n_seqs,
+        GDN_BF16, ct, sc, ws, ws_bytes)
     return o

@@ -2686,6 +2686,7 @@ __global__ __launch_bounds__(NT_ATT / QT) __attribute__((amdgpu_waves_per_eu(4 /
 
 #include "wide.hip"
 #include "generic.hip"
+#include "paged.hip"
 
 // ------------------------------------------------------------------ host side
 thread_local char g_err[512] = "";
@@ -3157,6 +3158,28 @@ void launch_attention(AttnParams a, hipStream_t st) {
         hipLaunchKernelGGL((k_attn_causal<DH, 1, DH == 128>), dim3((unsigned)wgs), dim3(NT_ATT), 0, st, a);
     else
         hipLaunchKernelGGL((k_attn_causal<DH, 1>), dim3((unsigned)wgs), dim3(NT_ATT), 0, st, a);
+}
+
+// Row groups per wave of k_rows: few tokens spread their heads over waves (latency), many keep a token's angles and
+// place in one wave.
+void rows_split(RowsParams& p, int rows, int dh) {
+    const int groups = (rows + 512 / dh - 1) / (512 / dh);   // 64 / (dh / 8) rows each
+    p.per = (int)std::min<long>(groups, std::max<long>(1, p.tokens * groups / 8192));
+    p.units = (groups + p.per - 1) / p.per;
+}
+long rows_wgs(const RowsParams& p) { return (p.tokens * p.units + NT / 64 - 1) / (NT / 64); }
+
+template <typename IO>
+void launch_rows(RowsParams p, int d, hipStream_t st) {
+    rows_split(p, p.H * (p.q != nullptr) + p.HKV * ((p.k != nullptr) + (p.v != nullptr)), d);
+    const dim3 grid((unsigned)rows_wgs(p));
+    if (d == 128) hipLaunchKernelGGL((k_rows<IO, 128>), grid, dim3(NT), 0, st, p);
+    else hipLaunchKernelGGL((k_rows<IO, 64>), grid, dim3(NT), 0, st, p);
+}
+
+template <int DH, int IT>
+void launch_append_e4m3(const RowsParams& p, int row_wgs, long pages, hipStream_t st) {
+    hipLaunchKernelGGL((k_append_e4m3<DH, IT>), dim3((unsigned)(row_wgs + pages * p.HKV * 2)), dim3(NT), 0, st, p, row_wgs);
 }
 
 }  // namespace
@@ -3681,4 +3704,222 @@ extern "C" gdn_status gdn_attention_prefill(const void* q, const void* k, const 
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(GDN_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
     return GDN_OK;
+}
+
+// ------------------------------------------------------------------ the attention layers' serving operators
+// Checks shared by the entry points of paged.hip, in the order of the header's argument lists.
+static gdn_status step_sizes(int B, int T, int H, int H_kv, int d, const int32_t* cu_seqlens, int n_seqs) {
+    if (B < 1 || T < 0 || H < 1) return fail(GDN_ERR_INVALID_ARG, "B=%d T=%d H=%d out of range", B, T, H);
+    if (H_kv < 1 || H_kv > H || H % H_kv != 0)
+        return fail(GDN_ERR_INVALID_ARG, "H_kv=%d key/value heads must divide the H=%d query heads", H_kv, H);
+    if (d < 1) return fail(GDN_ERR_INVALID_ARG, "d=%d must be positive", d);
+    if ((cu_seqlens == nullptr) != (n_seqs == 0))
+        return fail(GDN_ERR_INVALID_ARG, "cu_seqlens and n_seqs=%d must be given together", n_seqs);
+    if (n_seqs < 0) return fail(GDN_ERR_INVALID_ARG, "n_seqs=%d is negative", n_seqs);
+    if (n_seqs > 0 && B != 1) return fail(GDN_ERR_INVALID_ARG, "packed sequences need B == 1 (got %d)", B);
+    if (cu_seqlens && !aligned(cu_seqlens, 4)) return fail(GDN_ERR_INVALID_ARG, "cu_seqlens is not 4-byte aligned");
+    if (d != 64 && d != 128) return fail(GDN_ERR_UNSUPPORTED, "d=%d: only 64 and 128 are implemented", d);
+    if ((long)H * d > (1L << 20)) return fail(GDN_ERR_UNSUPPORTED, "H=%d too large", H);
+    if ((long)B * T * H >= (1L << 31) / 2) return fail(GDN_ERR_UNSUPPORTED, "B*T*H=%ld too large", (long)B * T * H);
+    return GDN_OK;
+}
+
+static gdn_status check_turn(const float* q_weight, const float* k_weight, float eps, const double* inv_freq, int rot, int d,
+                             int flags) {
+    if (flags & ~GDN_ROPE_INTERLEAVED) return fail(GDN_ERR_INVALID_ARG, "flags=%d: unknown bits", flags);
+    if (!aligned(q_weight, 4) || !aligned(k_weight, 4)) return fail(GDN_ERR_INVALID_ARG, "a weight is not 4-byte aligned");
+    if ((q_weight || k_weight) && !(eps >= 0.f)) return fail(GDN_ERR_INVALID_ARG, "eps=%g must be 0 or more", (double)eps);
+    if ((inv_freq == nullptr) != (rot == 0))
+        return fail(GDN_ERR_INVALID_ARG, "inv_freq and rot=%d must be given together", rot);
+    if (!aligned(inv_freq, 8)) return fail(GDN_ERR_INVALID_ARG, "inv_freq is not 8-byte aligned");
+    if (rot < 0 || rot > d) return fail(GDN_ERR_INVALID_ARG, "rot=%d must lie in 0..d=%d", rot, d);
+    if (rot % 16) return fail(GDN_ERR_UNSUPPORTED, "rot=%d: only multiples of 16 are implemented", rot);
+    return GDN_OK;
+}
+
+static gdn_status check_cache(const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                              const int32_t* block_table, const int32_t* seq_lens, int page, int n_pages, int max_pages,
+                              int cache_dtype) {
+    if (cache_dtype != GDN_BF16 && cache_dtype != GDN_E4M3)
+        return fail(GDN_ERR_INVALID_ARG, "cache_dtype=%d is neither GDN_BF16 nor GDN_E4M3", cache_dtype);
+    if (page < 1 || n_pages < 1 || max_pages < 1)
+        return fail(GDN_ERR_INVALID_ARG, "page=%d n_pages=%d max_pages=%d must be positive", page, n_pages, max_pages);
+    if (page != 16 && page != 32 && page != 64 && page != 128)
+        return fail(GDN_ERR_UNSUPPORTED, "page=%d: only 16, 32, 64 and 128 are implemented", page);
+    if ((long)max_pages * page >= (1L << 31)) return fail(GDN_ERR_UNSUPPORTED, "max_pages=%d too large", max_pages);
+    if (!k_cache || !v_cache || !block_table || !seq_lens)
+        return fail(GDN_ERR_INVALID_ARG, "k_cache, v_cache, block_table and seq_lens must be non-null");
+    if (!aligned(k_cache, 16) || !aligned(v_cache, 16)) return fail(GDN_ERR_INVALID_ARG, "a cache is not 16-byte aligned");
+    if ((cache_dtype == GDN_E4M3) != (k_scale != nullptr) || (cache_dtype == GDN_E4M3) != (v_scale != nullptr))
+        return fail(GDN_ERR_INVALID_ARG, "k_scale and v_scale belong to a GDN_E4M3 cache, both, and to no other");
+    if (!aligned(k_scale, 4) || !aligned(v_scale, 4) || !aligned(block_table, 4) || !aligned(seq_lens, 4))
+        return fail(GDN_ERR_INVALID_ARG, "a scale, block_table or seq_lens is not 4-byte aligned");
+    return GDN_OK;
+}
+
+static gdn_status check_rows(const char* name, const void* rows, long stride, int heads, int d, size_t esz) {
+    if (!rows) return fail(GDN_ERR_INVALID_ARG, "%s must be non-null", name);
+    if (stride < (long)heads * d || (size_t)stride * esz % 16)
+        return fail(GDN_ERR_INVALID_ARG, "%s: a token's rows (stride %ld) must be %d elements or more apart, in 16-byte steps", name,
+                    stride, heads * d);
+    if (!aligned(rows, 16)) return fail(GDN_ERR_INVALID_ARG, "%s %p is not 16-byte aligned", name, rows);
+    return GDN_OK;
+}
+
+static Cache make_cache(const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                        const int32_t* block_table, int page, int n_pages, int max_pages) {
+    Cache c;
+    c.k = const_cast<void*>(k_cache);
+    c.v = const_cast<void*>(v_cache);
+    c.ks = const_cast<float*>(k_scale);
+    c.vs = const_cast<float*>(v_scale);
+    c.table = block_table;
+    c.n_pages = n_pages; c.max_pages = max_pages; c.page = page;
+    c.shift = page == 16 ? 4 : page == 32 ? 5 : page == 64 ? 6 : 7;
+    return c;
+}
+
+static gdn_status launched() {
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return fail(GDN_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
+    return GDN_OK;
+}
+
+extern "C" gdn_status gdn_qk_norm_rope(const void* q, const void* k, void* q_out, void* k_out, int B, int T, int H, int H_kv,
+                                       int d, long long q_stride, long long k_stride, const float* q_weight,
+                                       const float* k_weight, float eps, const double* inv_freq, int rot,
+                                       const int32_t* positions, const int32_t* cu_seqlens, int n_seqs, int io_dtype,
+                                       int flags, void* stream) {
+    g_err[0] = '\0';
+    if (io_dtype != GDN_F32 && io_dtype != GDN_BF16)
+        return fail(GDN_ERR_INVALID_ARG, "io_dtype=%d is neither GDN_F32 nor GDN_BF16", io_dtype);
+    gdn_status st = step_sizes(B, T, H, H_kv, d, cu_seqlens, n_seqs);
+    if (st == GDN_OK) st = check_turn(q_weight, k_weight, eps, inv_freq, rot, d, flags);
+    if (st != GDN_OK) return st;
+    if (!aligned(positions, 4)) return fail(GDN_ERR_INVALID_ARG, "positions is not 4-byte aligned");
+    if (T == 0) return GDN_OK;
+    const size_t esz = io_dtype == GDN_BF16 ? 2 : 4;
+    if ((st = check_rows("q", q, (long)q_stride, H, d, esz)) != GDN_OK) return st;
+    if ((st = check_rows("k", k, (long)k_stride, H_kv, d, esz)) != GDN_OK) return st;
+    if (!q_out || !k_out) return fail(GDN_ERR_INVALID_ARG, "q_out and k_out must be non-null");
+    if (!aligned(q_out, 16) || !aligned(k_out, 16)) return fail(GDN_ERR_INVALID_ARG, "an output is not 16-byte aligned");
+    RowsParams p = {};
+    p.q = q; p.k = k; p.qo = q_out; p.ko = k_out;
+    p.qs = (long)q_stride; p.ks = (long)k_stride;
+    p.H = H; p.HKV = H_kv;
+    p.tokens = (long)B * T;
+    p.qw = q_weight; p.kw = k_weight;
+    p.pos = positions;
+    p.t.freq = inv_freq; p.t.rot = rot; p.t.near = (flags & GDN_ROPE_INTERLEAVED) != 0; p.t.eps = eps;
+    p.s.cu = cu_seqlens; p.s.n = n_seqs > 0 ? n_seqs : B; p.s.T = T;
+    hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+    (void)hipGetLastError();
+    if (io_dtype == GDN_BF16) launch_rows<bf16_t>(p, d, hs);
+    else launch_rows<float>(p, d, hs);
+    return launched();
+}
+
+extern "C" gdn_status gdn_kv_append(const void* q, const void* k, const void* v, void* q_out, void* k_cache, void* v_cache,
+                                    float* k_scale, float* v_scale, const int32_t* block_table, const int32_t* seq_lens,
+                                    int B, int T, int H, int H_kv, int d, int page, int n_pages, int max_pages,
+                                    long long q_stride, long long k_stride, long long v_stride, const float* q_weight,
+                                    const float* k_weight, float eps, const double* inv_freq, int rot,
+                                    const int32_t* cu_seqlens, int n_seqs, int io_dtype, int cache_dtype, int flags,
+                                    void* stream) {
+    g_err[0] = '\0';
+    if (io_dtype != GDN_F32 && io_dtype != GDN_BF16)
+        return fail(GDN_ERR_INVALID_ARG, "io_dtype=%d is neither GDN_F32 nor GDN_BF16", io_dtype);
+    gdn_status st = step_sizes(B, T, H, H_kv, d, cu_seqlens, n_seqs);
+    if (st == GDN_OK) st = check_turn(q_weight, k_weight, eps, inv_freq, rot, d, flags);
+    if (st == GDN_OK)
+        st = check_cache(k_cache, v_cache, k_scale, v_scale, block_table, seq_lens, page, n_pages, max_pages, cache_dtype);
+    if (st != GDN_OK) return st;
+    if (io_dtype != GDN_BF16) return fail(GDN_ERR_UNSUPPORTED, "appending is implemented for bf16 io only");
+    if ((q == nullptr) != (q_out == nullptr)) return fail(GDN_ERR_INVALID_ARG, "q and q_out must be given together");
+    if (T == 0) return GDN_OK;
+    if (q && (st = check_rows("q", q, (long)q_stride, H, d, 2)) != GDN_OK) return st;
+    if ((st = check_rows("k", k, (long)k_stride, H_kv, d, 2)) != GDN_OK) return st;
+    if ((st = check_rows("v", v, (long)v_stride, H_kv, d, 2)) != GDN_OK) return st;
+    if (!aligned(q_out, 16)) return fail(GDN_ERR_INVALID_ARG, "q_out %p is not 16-byte aligned", q_out);
+    RowsParams p = {};
+    p.q = q; p.k = k; p.v = v; p.qo = q_out;
+    p.qs = (long)q_stride; p.ks = (long)k_stride; p.vs = (long)v_stride;
+    p.H = H; p.HKV = H_kv;
+    p.tokens = (long)B * T;
+    p.qw = q_weight; p.kw = k_weight;
+    p.t.freq = inv_freq; p.t.rot = rot; p.t.near = (flags & GDN_ROPE_INTERLEAVED) != 0; p.t.eps = eps;
+    p.s.cu = cu_seqlens; p.s.lens = seq_lens; p.s.n = n_seqs > 0 ? n_seqs : B; p.s.T = T;
+    p.c = make_cache(k_cache, v_cache, k_scale, v_scale, block_table, page, n_pages, max_pages);
+    hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+    if (cache_dtype == GDN_BF16) {
+        (void)hipGetLastError();
+        launch_rows<bf16_t>(p, d, hs);
+        return launched();
+    }
+    // pages that the new tokens can touch: n tokens lie in at most (n - 1) / page + 2
+    const long pages = n_seqs > 0 ? (long)T / page + 2L * n_seqs : (long)B * (((long)T + page - 2) / page + 1);
+    int row_wgs = 0;
+    if (q) {
+        rows_split(p, H, d);
+        row_wgs = (int)rows_wgs(p);
+    }
+    if (row_wgs + pages * H_kv * 2 >= (1L << 31)) return fail(GDN_ERR_UNSUPPORTED, "B*T*H_kv too large");
+    (void)hipGetLastError();
+    if (d == 128) {
+        if (page == 16) launch_append_e4m3<128, 1>(p, row_wgs, pages, hs);
+        else if (page == 32) launch_append_e4m3<128, 2>(p, row_wgs, pages, hs);
+        else if (page == 64) launch_append_e4m3<128, 4>(p, row_wgs, pages, hs);
+        else launch_append_e4m3<128, 8>(p, row_wgs, pages, hs);
+    } else {
+        if (page <= 32) launch_append_e4m3<64, 1>(p, row_wgs, pages, hs);
+        else if (page == 64) launch_append_e4m3<64, 2>(p, row_wgs, pages, hs);
+        else launch_append_e4m3<64, 4>(p, row_wgs, pages, hs);
+    }
+    return launched();
+}
+
+extern "C" size_t gdn_attention_paged_workspace_bytes(int B, int T, int H, int H_kv, int d, int page, int max_pages, int n_seqs) {
+    (void)B; (void)T; (void)H; (void)H_kv; (void)d; (void)page; (void)max_pages; (void)n_seqs;
+    return 0;
+}
+
+extern "C" gdn_status gdn_attention_paged(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
+                                          const float* v_scale, const int32_t* block_table, const int32_t* seq_lens, void* o,
+                                          int B, int T, int H, int H_kv, int d, int page, int n_pages, int max_pages,
+                                          const int32_t* cu_seqlens, int n_seqs, int io_dtype, int cache_dtype, float scale,
+                                          void* workspace, size_t workspace_bytes, void* stream) {
+    g_err[0] = '\0';
+    if (io_dtype != GDN_F32 && io_dtype != GDN_BF16)
+        return fail(GDN_ERR_INVALID_ARG, "io_dtype=%d is neither GDN_F32 nor GDN_BF16", io_dtype);
+    gdn_status st = step_sizes(B, T, H, H_kv, d, cu_seqlens, n_seqs);
+    if (st == GDN_OK)
+        st = check_cache(k_cache, v_cache, k_scale, v_scale, block_table, seq_lens, page, n_pages, max_pages, cache_dtype);
+    if (st != GDN_OK) return st;
+    if (io_dtype != GDN_BF16) return fail(GDN_ERR_UNSUPPORTED, "attention is implemented for bf16 io only");
+    if (T == 0) return GDN_OK;
+    if (!q || !o) return fail(GDN_ERR_INVALID_ARG, "q and o must be non-null");
+    if (!aligned(q, 16) || !aligned(o, 16)) return fail(GDN_ERR_INVALID_ARG, "q or o is not 16-byte aligned");
+    const size_t need = gdn_attention_paged_workspace_bytes(B, T, H, H_kv, d, page, max_pages, n_seqs);
+    if (need > 0 && (!workspace || workspace_bytes < need))
+        return fail(GDN_ERR_WORKSPACE, "workspace of %zu bytes given, %zu needed", workspace ? workspace_bytes : (size_t)0, need);
+    if (workspace && !aligned(workspace, 256)) return fail(GDN_ERR_INVALID_ARG, "workspace is not 256-byte aligned");
+    PagedParams p = {};
+    p.q = static_cast<const bf16_t*>(q);
+    p.o = static_cast<bf16_t*>(o);
+    p.tokens = (long)B * T;
+    p.H = H; p.HKV = H_kv;
+    p.scale_log2 = scale * 1.4426950408889634f;
+    p.s.cu = cu_seqlens; p.s.lens = seq_lens; p.s.n = n_seqs > 0 ? n_seqs : B; p.s.T = T;
+    p.c = make_cache(k_cache, v_cache, k_scale, v_scale, block_table, page, n_pages, max_pages);
+    hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+    (void)hipGetLastError();
+    const dim3 grid((unsigned)((p.tokens * H + NT / 64 - 1) / (NT / 64)));
+    if (cache_dtype == GDN_BF16) {
+        if (d == 128) hipLaunchKernelGGL((k_attn_paged<128, bf16_t>), grid, dim3(NT), 0, hs, p);
+        else hipLaunchKernelGGL((k_attn_paged<64, bf16_t>), grid, dim3(NT), 0, hs, p);
+    } else {
+        if (d == 128) hipLaunchKernelGGL((k_attn_paged<128, uint8_t>), grid, dim3(NT), 0, hs, p);
+        else hipLaunchKernelGGL((k_attn_paged<64, uint8_t>), grid, dim3(NT), 0, hs, p);
+    }
+    return launched();
 }

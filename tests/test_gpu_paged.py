@@ -1,0 +1,409 @@
+"""GPU parity of the attention layers' serving operators (gdn_qk_norm_rope, gdn_kv_append, gdn_attention_paged) against the
+fp64 oracle ``oracle/paged.py``, element by element, within bounds counted in roundings (``paged_cases``)."""
+import numpy as np
+import pytest
+import torch
+
+import paged_cases as pc
+import paper_2607_14568_amd as gdn
+from oracle import paged
+from paged_cases import HALF, cuda, f64, normal
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def _fused(seed, B, T, heads, d, dtype):
+    """Parts of one projection's rows: [B,T,h,d] views for each h of heads."""
+    return normal(seed, B, T, sum(heads), d, dtype=dtype).cuda().split(heads, dim=2)
+
+
+def _close(got, ref, slack, dtype, label):
+    off = np.abs(f64(got).reshape(ref.shape) - ref) / (HALF[dtype] * np.abs(ref) * 1.01 + slack + 1e-30)
+    print("  %s: largest error %.3f of the bound" % (label, off.max() if off.size else 0), flush=True)
+    assert (off <= 1).all(), (label, off.max())
+
+
+# ------------------------------------------------------------------ gdn_qk_norm_rope
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("d,rot,near", [(128, 128, False), (128, 32, False), (128, 48, True), (64, 64, False), (64, 16, True),
+                                        (64, 0, False)])
+@pytest.mark.parametrize("B,T,H,Hkv", [(1, 1, 1, 1), (2, 5, 6, 2), (1, 131, 16, 8)])
+def test_norm_rope(io, d, rot, near, B, T, H, Hkv):
+    print("case: norm", io, d, rot, near, B, T, H, Hkv, flush=True)
+    q, k = _fused(rot + d, B, T, [H, Hkv], d, DT[io]) if T != 5 else (normal(i, B, T, h, d, dtype=DT[io]).cuda() for i, h in enumerate((H, Hkv)))
+    qw, kw = (1 + 0.3 * normal(7 + i, d, dtype=torch.float32).cuda() for i in range(2))
+    f = pc.freqs(rot)
+    for weights in ((qw, kw), (None, None), (qw, None)):
+        got = gdn.gdn_qk_norm_rope(q, k, q_weight=weights[0], k_weight=weights[1], eps=1e-5, interleaved=near,
+                                   inv_freq=None if f is None else f.cuda())
+        for x, w, y in zip((q, k), weights, got):
+            ref, slack = pc.turned(x, w, 1e-5, np.tile(np.arange(T), B), f, near)
+            _close(y, ref, slack, DT[io], "norm %s" % (w is not None))
+
+
+def test_norm_rope_far_positions_and_in_place():
+    """Positions near 2^31: the angle is formed in float64, off by 2^-53 of 2^31 radians: under 2^-21."""
+    q, k = normal(1, 1, 4, 4, 128).cuda(), normal(2, 1, 4, 2, 128).cuda()
+    pos = torch.tensor([[0, 131071, 10 ** 7 + 1, 2 ** 31 - 1]], dtype=torch.int32)
+    f = pc.freqs(128)
+    want = [pc.turned(x, None, 0, pos[0].numpy(), f, False) for x in (q, k)]
+    got = gdn.gdn_qk_norm_rope(q, k, inv_freq=f.cuda(), positions=pos.cuda(), q_out=q, k_out=k)
+    assert got[0] is q and got[1] is k
+    for y, (ref, slack) in zip(got, want):
+        _close(y, ref, 2 * slack, torch.bfloat16, "far")
+
+
+@pytest.mark.parametrize("io,n", [("bf16", 0), ("f32", 70)])
+def test_norm_rope_packed(io, n):
+    """Positions restart at every sequence, rows behind the last stay, offsets outside the contract are clamped."""
+    cu = [0, 0, 5, 6, 70, 64, 90] if not n else [0] + list(np.cumsum(np.random.default_rng(3).integers(0, 3, n)))
+    T = max(cu) + 9
+    print("case: norm packed", io, n, T, flush=True)
+    q, k = normal(3, 1, T, 2, 64, dtype=DT[io]).cuda(), normal(4, 1, T, 1, 64, dtype=DT[io]).cuda()
+    f = pc.freqs(64)
+    out = [torch.full_like(x, 7.0) for x in (q, k)]
+    gdn.gdn_qk_norm_rope(q, k, inv_freq=f.cuda(), cu_seqlens=torch.tensor(cu, dtype=torch.int32).cuda(), q_out=out[0], k_out=out[1])
+    pos, used = np.zeros(T, dtype=int), 0
+    for a, m in paged.spans(1, T, cu):
+        pos[a:a + m], used = np.arange(m), max(used, a + m)
+    for x, y in zip((q, k), out):
+        ref, slack = pc.turned(x, None, 0, pos, f, False)
+        ref[used:], slack[used:] = 7.0, 0
+        _close(y, ref, slack, DT[io], "packed")
+
+
+def test_norm_rope_special_values():
+    """A zero row stays zero, an infinity or a NaN stays in its row."""
+    q = normal(5, 1, 3, 2, 128, dtype=torch.float32)
+    q[0, 0, 0], q[0, 1, 0, 3], q[0, 2, 1, 5] = 0, float("inf"), float("nan")
+    w = torch.ones(128).cuda()
+    got, _ = gdn.gdn_qk_norm_rope(q.cuda(), q.cuda(), q_weight=w, k_weight=w, eps=1e-6, inv_freq=pc.freqs(128).cuda())
+    bad = torch.isfinite(got).all(-1).logical_not().cpu()[0]
+    assert not got[0, 0, 0].any() and bad.tolist() == [[False, False], [True, False], [False, True]]
+
+
+# ------------------------------------------------------------------ gdn_kv_append
+def _append_case(cache, page, d, H, Hkv, lens, new, cu, rot, near, seed, T=None):
+    n, packed = len(lens), cu is not None
+    B, T = (1, T or sum(new)) if packed else (n, new[0])
+    q, k, v = _fused(seed, B, T, [H, Hkv, Hkv], d, torch.bfloat16)
+    table, n_pages = pc.pages_for(lens, page, seed)
+    kc, vc, ks, vs = pc.make_cache(n_pages, Hkv, page, d, cache, seed)
+    w = [1 + 0.3 * normal(seed + i, d, dtype=torch.float32) for i in range(2)]
+    f = pc.freqs(rot)
+    return dict(B=B, T=T, q=q, k=k, v=v, table=table, kc=kc, vc=vc, ks=ks, vs=vs, w=w, f=f, near=near, lens=lens, cu=cu, page=page)
+
+
+def _append(c):
+    dev = cuda(c["kc"], c["vc"], c["ks"], c["vs"])
+    q_out = torch.full((c["B"], c["T"]) + tuple(c["q"].shape[2:]), 7.0, dtype=torch.bfloat16, device="cuda")
+    gdn.gdn_kv_append(c["k"], c["v"], dev[0], dev[1], torch.from_numpy(c["table"]).cuda(), torch.tensor(c["lens"], dtype=torch.int32).cuda(),
+                      q=c["q"], q_out=q_out, k_scale=dev[2], v_scale=dev[3], q_weight=c["w"][0].cuda(), k_weight=c["w"][1].cuda(),
+                      inv_freq=None if c["f"] is None else c["f"].cuda(), interleaved=c["near"],
+                      cu_seqlens=None if c["cu"] is None else torch.tensor(c["cu"], dtype=torch.int32).cuda())
+    return q_out, dev
+
+
+def _check_append(c, q_out, dev, label):
+    B, T, d = c["B"], c["T"], c["q"].shape[3]
+    pos, used = np.zeros(B * T, dtype=int), np.zeros(B * T, dtype=bool)
+    for s, (a, m) in enumerate(paged.spans(B, T, c["cu"])):
+        pos[a:a + m], used[a:a + m] = c["lens"][s] - m + np.arange(m), True
+    ref, slack = pc.turned(c["q"], c["w"][0], 1e-6, pos, c["f"], c["near"])
+    ref[~used], slack[~used] = 7.0, 0
+    _close(q_out, ref, slack, torch.bfloat16, label + " q")
+    k, kslack = pc.turned(c["k"], c["w"][1], 1e-6, pos, c["f"], c["near"])
+    for name, rows, sl, code, scale, got, gs in (("k", k, kslack, c["kc"], c["ks"], dev[0], dev[2]),
+                                                ("v", f64(c["v"]).reshape(B * T, -1, d), 0 * kslack, c["vc"], c["vs"], dev[1], dev[3])):
+        want = f64(code.float())   # the codes; values over the scale
+        slots = np.zeros(want.shape)          # bound of each cell's fp32 steps, NaN where nothing was written
+        slots[:] = np.nan
+        paged.append(slots, None, c["table"], c["lens"], np.broadcast_to(sl, rows.shape), c["cu"], B, T, c["page"])
+        if scale is None:
+            paged.append(want, None, c["table"], c["lens"], rows, c["cu"], B, T, c["page"])
+            bound = 2.0 ** -8 * 1.01 * np.abs(want) + slots
+            have = f64(got)
+        else:
+            s = f64(scale)
+            paged.append(want, s, c["table"], c["lens"], rows, c["cu"], B, T, c["page"])
+            assert (f64(gs) == s).all(), label + " scale"
+            # a code is the nearest to a value that fp32 steps moved by `slots`: the same, or a neighbour's (one step) where
+            # the value lies that near to the middle between two
+            bound, have = np.where(slots > 0, 2.0 ** -3 * np.abs(want) * 1.01 + 2.0 ** -9, 0.0), f64(got.float())
+            moved = (have != want) & ~(np.isnan(have) & np.isnan(want))
+            assert moved.sum() <= 1e-3 * moved.size, label
+        bound[np.isnan(slots)] = 0   # ... and the cells that no token falls on: as the oracle has them, exactly
+        off = np.abs(have - want)
+        ok = (off <= bound + 1e-30) | (np.isnan(have) & np.isnan(want))
+        assert ok.all(), (label, name, np.argwhere(~ok)[:4], off[~ok][:4])
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("page,d", [(16, 128), (32, 64), (64, 128), (128, 64), (128, 128), (16, 64), (32, 128), (64, 64)])
+def test_append_dense(cache, page, d):
+    """One token and several, at page starts, ends and inside, into empty and partly filled pages."""
+    for new, lens in ((1, [1, page, page + 1, 2 * page + 7]), (page + 3, [page + 3, 2 * page, 3 * page + 1, 2 * page + 5])):
+        print("case: append dense", cache, page, d, new, flush=True)
+        c = _append_case(cache, page, d, 6, 2, lens, [new] * 4, None, d // 2, page == 32, seed=page + d + new)
+        _check_append(c, *_append(c), "append")
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("n", [6, 70])
+def test_append_packed(cache, n):
+    """Packed sequences, empty ones among them, rows behind the last left alone."""
+    g = np.random.default_rng(n)
+    new = list(g.integers(0, 60 if n == 6 else 4, n))
+    new[2] = 0
+    lens = [int(m + g.integers(0, 90)) for m in new]
+    cu = [0] + list(np.cumsum(new))
+    print("case: append packed", cache, n, flush=True)
+    c = _append_case(cache, 32, 128, 4, 2, lens, new, cu, 128, False, seed=n, T=cu[-1] + 5)
+    _check_append(c, *_append(c), "append packed")
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_append_outside_the_table(cache):
+    """Entries outside the cache, positions past the table and before 0: nothing is written for them."""
+    lens, new = [40, 200, 3, 33], 5
+    c = _append_case(cache, 16, 64, 2, 2, [40, 60, 3, 33], [new] * 4, None, 64, False, seed=9)
+    c["lens"] = lens                                  # sequence 1 ends past its table's last page, sequence 2 starts before 0
+    c["table"][0, 2], c["table"][3, 1] = 10 ** 6, -7  # (pages that are not there)
+    print("case: append outside", cache, flush=True)
+    q_out, dev = _append(c)
+    _check_append(c, q_out, dev, "append outside")
+
+
+def test_append_without_queries_and_special_values():
+    """No q; zeros, an infinity, a NaN, the type's edge: codes and scales of an 8-bit page."""
+    k = torch.zeros(1, 20, 1, 64, dtype=torch.bfloat16)
+    k[0, 3, 0, 1], k[0, 4, 0, 2], k[0, 5, 0, 3], k[0, 6, 0, 4] = float("inf"), float("nan"), 448.0, -1.0
+    v = torch.zeros_like(k)
+    kc, vc, ks, vs = cuda(*pc.make_cache(2, 1, 16, 64, "e4m3", 3))
+    args = torch.tensor([[1, 0]], dtype=torch.int32).cuda(), torch.tensor([20], dtype=torch.int32).cuda()
+    assert gdn.gdn_kv_append(k.cuda(), v.cuda(), kc, vc, *args, k_scale=ks, v_scale=vs) is None
+    assert ks.tolist() == [[2.0 ** -100], [1.0]] and vs.tolist() == [[2.0 ** -100]] * 2
+    got = kc[1, 0].float().cpu()
+    assert torch.isnan(got[3, 1]) and torch.isnan(got[4, 2]) and got[5, 3] == 448 and got[6, 4] == -1
+    assert torch.isnan(got).sum() == 2 and (got[torch.isfinite(got)] != 0).sum() == 2 and not vc[1].float().any()
+
+
+def test_append_token_by_token():
+    """An 8-bit page filled token by token, each larger than the last: codes as the oracle re-rounds them."""
+    x = normal(11, 1, 32, 1, 64) * torch.linspace(0.05, 40, 32)[None, :, None, None].bfloat16()
+    kc, vc, ks, vs = cuda(*pc.make_cache(3, 1, 16, 64, "e4m3", 5))
+    want, s = f64(kc.float()), f64(ks)
+    table = np.array([[2, 0]], dtype=np.int32)
+    for t in range(32):
+        row = x[:, t:t + 1].contiguous().cuda()
+        gdn.gdn_kv_append(row, row, kc, vc, torch.from_numpy(table).cuda(), torch.tensor([t + 1], dtype=torch.int32).cuda(), k_scale=ks, v_scale=vs)
+        paged.append(want, s, table, [t + 1], f64(x[:, t]), None, 1, 1, 16)
+        assert (f64(ks) == s).all() and (f64(kc.float()) == want).all(), t
+    assert torch.equal(vc[[0, 2]].view(torch.uint8), kc[[0, 2]].view(torch.uint8)) and s[2, 0] > 2.0 ** -9
+
+
+# ------------------------------------------------------------------ gdn_attention_paged
+def _attention_case(cache, page, d, H, Hkv, lens, new, seed, cu=None, T=None, scale=None):
+    n = len(lens)
+    B, T = (1, T or sum(new)) if cu is not None else (n, new[0])
+    q = normal(seed, B, T, H, d).cuda()
+    table, n_pages = pc.pages_for([max(x, 1) for x in lens], page, seed)
+    kc = pc.make_cache(n_pages, Hkv, page, d, cache, seed)
+    for i in range(2):   # what lies behind a sequence's end is not a number
+        for s, L in enumerate(lens):
+            b = max(L, 0) // page
+            if table[s, min(b, table.shape[1] - 1)] >= 0 and b < table.shape[1]:
+                kc[i][table[s, b], :, max(L, 0) % page:] = float("nan")
+    return q, cuda(*kc), torch.from_numpy(table).cuda(), torch.tensor(lens, dtype=torch.int32).cuda(), \
+        None if cu is None else torch.tensor(cu, dtype=torch.int32).cuda()
+
+
+def _run_attention(label, *args, scale=None, **kw):
+    print("case: attention", label, flush=True)
+    q, cache, table, lens, cu = _attention_case(*args, **kw)
+    o = torch.full_like(q, 7.0)
+    pc.attend(q, cache, table, lens, cu, scale, o)
+    rows = pc.check_attention(o, q, cache, table, lens, cu, scale, label)
+    assert (f64(o).reshape(-1, *q.shape[2:])[~rows] == 7.0).all()
+    return o
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("page,d", [(16, 128), (32, 64), (64, 128), (128, 64), (16, 64), (128, 128)])
+def test_decode_lengths(cache, page, d):
+    """One token a sequence: lengths of one token up to several pages, at their edges."""
+    lens = [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 100, 127, 128, 129, 300]
+    _run_attention("decode lengths", cache, page, d, 4, 2, lens, [1] * len(lens), seed=page + d)
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("H,Hkv", [(1, 1), (2, 1), (3, 1), (6, 2), (16, 1), (16, 8), (17, 1), (40, 2), (64, 1)])
+def test_decode_heads(cache, H, Hkv):
+    _run_attention("decode heads %d %d" % (H, Hkv), cache, 64, 128 if H != 6 else 64, H, Hkv, [5, 130, 700], [1] * 3, seed=H)
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("new", [2, 4, 7, 16, 33, 130])
+def test_several_tokens(cache, new):
+    """A few drafted tokens and pieces of prompts: causal among themselves, behind what is cached."""
+    _run_attention("several %d" % new, cache, 32 if new == 7 else 64, 64 if new == 4 else 128, 8, 2,
+                   [new, new + 1, new + 63, new + 64, 500 + new], [new] * 5, seed=new)
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("n", [7, 70])
+def test_packed(cache, n):
+    """Packed steps of no, one and many tokens; rows behind the last sequence are left as they were."""
+    g = np.random.default_rng(n)
+    new = [int(x) for x in g.integers(0, 3 if n == 70 else 90, n)]
+    new[1] = 0
+    lens = [int(m + g.integers(0, 200)) for m in new]
+    cu = [0] + [int(x) for x in np.cumsum(new)]
+    _run_attention("packed %d" % n, cache, 16, 128, 4, 2, lens, new, seed=n, cu=cu, T=cu[-1] + 11)
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("new", [1, 6, 40])
+def test_rows_without_keys(cache, new):
+    """Lengths below the number of new tokens (0 and negative ones too): rows that no key is left for are zeros."""
+    o = _run_attention("no keys %d" % new, cache, 16, 64, 4, 2, [new, 0, max(new - 2, 0), -3, 100], [new] * 5, seed=new)
+    assert not o[1].any() and not o[3].any()
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("new", [1, 40])
+def test_pages_that_are_not_there(cache, new):
+    """Entries outside the cache and lengths past the table: their keys take no part."""
+    print("case: missing pages", cache, new, flush=True)
+    q, kc, table, lens, _ = _attention_case(cache, 16, 128, 4, 2, [100, 77, 64, 30], [new] * 4, seed=4)
+    table[0, 1], table[0, 6], table[1, 0], table[2] = -1, 10 ** 6, 2 ** 31 - 1, -2 ** 31
+    lens[3] = 9000                                       # (past the table: its last pages are missing too)
+    o = torch.full_like(q, 7.0)
+    pc.attend(q, kc, table, lens, None, None, o)
+    pc.check_attention(o, q, kc, table, lens, None, None, "missing")
+    assert not o[2].any()
+
+
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("scale", [0.0, -0.2, 2.0])
+def test_scales(scale, new):
+    """Uniform weights, a negative scale, and sharp ones."""
+    cache = "bf16" if new == 1 else "e4m3"
+    _run_attention("scale %g" % scale, cache, 64, 128, 4, 2, [300, 90], [new] * 2, seed=21, scale=scale)
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_nan_keys_reach_their_readers_only(cache):
+    """A NaN in a key or value: the head's rows that see it are NaN, all others as without it."""
+    q, kc, table, lens, _ = _attention_case(cache, 16, 64, 4, 2, [60, 60], [20] * 2, seed=6)
+    clean = pc.attend(q, kc, table, lens)
+    for i, (s, h, p) in enumerate([(0, 0, 50), (1, 1, 45)]):   # a key, a value
+        kc[i][int(table[s, p // 16]), h, p % 16, 3] = float("nan")
+    got = pc.attend(q, kc, table, lens)
+    hit = torch.zeros(got.shape[:3], dtype=torch.bool)
+    hit[0, 50 - 40:, 0:2], hit[1, 45 - 40:, 2:4] = True, True
+    bad = torch.isnan(got).cpu()
+    assert bad[0, :, 0:2].all(-1).equal(hit[0, :, 0:2]) and bad[1, :, 2:4].any(-1).equal(hit[1, :, 2:4])
+    assert torch.equal(got[~hit.cuda()], clean[~hit.cuda()])
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_rising_scores(cache):
+    """Scores that rise along the keys: the running softmax's reference moves all the time, and between parts of a split."""
+    print("case: rising", cache, flush=True)
+    q, kc, table, lens, _ = _attention_case(cache, 64, 128, 2, 1, [3000], [1], seed=8)
+    ramp = torch.linspace(0, 4, 64 * table.shape[1])
+    for b in range(table.shape[1] - 1):
+        page = ramp[64 * b:64 * b + 64][None, :, None].expand(1, 64, 128)
+        kc[0][int(table[0, b])] = page.to(kc[0].dtype).cuda()
+        if cache == "e4m3":
+            kc[2][int(table[0, b])] = 1.0
+    q = (q.abs() * 0.5).contiguous()
+    o = pc.attend(q, kc, table, lens)
+    pc.check_attention(o, q, kc, table, lens, None, None, "rising")
+
+
+# ------------------------------------------------------------------ together
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_a_prompt_and_its_next_tokens(cache):
+    """A prompt in two pieces, then tokens one by one, each step appended and attended: against the oracle over what the
+    cache then holds, and (bf16) against the prompt's own attention."""
+    H, Hkv, d, page, total = 4, 2, 128, 32, 150
+    q, k, v = _fused(31, 1, total, [H, Hkv, Hkv], d, torch.bfloat16)
+    qw, kw = (1 + 0.3 * normal(40 + i, d, dtype=torch.float32).cuda() for i in range(2))
+    f = pc.freqs(64).cuda()
+    table, n_pages = pc.pages_for([total], page, 1)
+    table = torch.from_numpy(table).cuda()
+    kc = cuda(*pc.make_cache(n_pages, Hkv, page, d, cache, 2))
+    outs, at = [], 0
+    for m in [100, 41] + [1] * 9:
+        part = slice(at, at + m)
+        at += m
+        lens = torch.tensor([at], dtype=torch.int32).cuda()
+        qt = gdn.gdn_kv_append(k[:, part], v[:, part], kc[0], kc[1], table, lens, q=q[:, part], k_scale=kc[2], v_scale=kc[3],
+                               q_weight=qw, k_weight=kw, inv_freq=f)
+        outs.append(pc.attend(qt, kc, table, lens))
+        pc.check_attention(outs[-1], qt, kc, table, lens, None, None, "step at %d" % at)
+    if cache == "bf16":
+        qt, kt = gdn.gdn_qk_norm_rope(q, k, q_weight=qw, k_weight=kw, inv_freq=f)
+        want = gdn.gdn_attention_prefill(qt, kt, v.contiguous())
+        # (both within 3.5 x 2^-8 of the sums over |v|, which stay under 4)
+        assert (torch.cat(outs, 1).float() - want.float()).abs().max() < 2 * 3.5 * 2.0 ** -8 * 4
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("new", [1, 30])
+def test_graph_replays(cache, new):
+    """A captured step (append, then attention) replayed as the lengths grow, with eager steps on the same buffers' copies
+    between: every replay equals the eager step bit by bit."""
+    H, Hkv, d, page, n, steps = 4, 2, 128, 16, 3, 4
+    g = [normal(50 + i, steps, n, new, h, d).cuda() for i, h in enumerate((H, Hkv, Hkv))]
+    start = [5, 200, 64]
+    table, n_pages = pc.pages_for([x + steps * new for x in start], page, 3)
+    table = torch.from_numpy(table).cuda()
+    first = cuda(*pc.make_cache(n_pages, Hkv, page, d, cache, 4))
+    f = pc.freqs(128).cuda()
+    need = gdn.gdn_attention_paged_workspace_bytes(n, new, H, Hkv, d, page, table.shape[1])
+
+    def buffers():
+        return [None if t is None else t.clone() for t in first], torch.empty(max(need, 1), dtype=torch.uint8, device="cuda")
+
+    def step(x, lens, cache_, ws, out):
+        qt = gdn.gdn_kv_append(x[1], x[2], cache_[0], cache_[1], table, lens, q=x[0], q_out=out[0], k_scale=cache_[2],
+                               v_scale=cache_[3], inv_freq=f)
+        pc.attend(qt, cache_, table, lens, o=out[1], workspace=ws if need else None)
+
+    eager, captured = buffers(), buffers()
+    x, lens = [t[0].clone() for t in g], torch.tensor(start, dtype=torch.int32).cuda() + new
+    outs = [[torch.empty_like(x[0]) for _ in range(2)] for _ in range(2)]
+    step(x, lens, *buffers(), outs[0])                  # (warm)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(x, lens, *captured, outs[1])
+    for i in range(steps):
+        for t, y in zip(x, g):
+            t.copy_(y[i])
+        lens.copy_(torch.tensor(start, dtype=torch.int32) + (i + 1) * new)
+        step(x, lens, *eager, outs[0])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0][1], outs[1][1]) and torch.equal(outs[0][0], outs[1][0]), i
+        for a, b in zip(eager[0], captured[0]):
+            assert a is None or torch.equal(a.view(torch.uint8), b.view(torch.uint8)), i
+
+
+def test_other_streams_and_repeats():
+    """Two streams at once with a workspace each, and twice in a row: the same bits."""
+    args = [_attention_case("e4m3", 64, 128, 8, 2, [3000, 10, 900], [1] * 3, seed=60 + i) for i in range(2)]
+    want = [pc.attend(*a) for a in args]
+    assert all(torch.equal(pc.attend(*a), w) for a, w in zip(args, want))
+    streams = [torch.cuda.Stream() for _ in args]
+    torch.cuda.synchronize()
+    got = []
+    for st, a in zip(streams, args):
+        with torch.cuda.stream(st):
+            got.append([pc.attend(*a) for _ in range(5)])
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, w) for xs, w in zip(got, want) for x in xs)
