@@ -3182,6 +3182,41 @@ void launch_append_e4m3(const RowsParams& p, int row_wgs, long pages, hipStream_
     hipLaunchKernelGGL((k_append_e4m3<DH, IT>), dim3((unsigned)(row_wgs + pages * p.HKV * 2)), dim3(NT), 0, st, p, row_wgs);
 }
 
+// How gdn_attention_paged cuts a step (pure host arithmetic, so that the workspace needs no device): row blocks of RB rows
+// per key/value head at most, and items beyond one per block.
+struct PagedPlan {
+    int rb;                // rows per block
+    long blocks, spare;
+    int row_groups;        // groups of 4 rows that a block can hold
+};
+PagedPlan paged_plan(int B, int T, int H, int H_kv, int n_seqs) {
+    const long G = H / H_kv;
+    PagedPlan p;
+    p.rb = 16;
+    p.blocks = n_seqs > 0 ? (T * G) / p.rb + std::min<long>(n_seqs, T) : B * ((T * G + p.rb - 1) / p.rb);
+    p.row_groups = n_seqs > 0 ? p.rb / 4 : (int)((std::min<long>(T * G, p.rb) + 3) / 4);
+    const long want = 4 * PLAN_CUS / H_kv;   // items per key/value head
+    p.spare = std::max(0L, want - p.blocks);
+    return p;
+}
+struct PagedLayout { size_t po, total; };
+PagedLayout paged_layout(const PagedPlan& p, int H_kv, int d) {
+    PagedLayout l = {0, 0};
+    if (p.spare == 0) return l;
+    const size_t rows = (size_t)(p.blocks + p.spare) * H_kv * p.rb;
+    l.po = round_up(rows * sizeof(float2), 256);
+    l.total = l.po + rows * d * sizeof(float);
+    return l;
+}
+
+template <int DH, typename CT>
+void launch_paged(const PagedParams& p, const PagedPlan& plan, hipStream_t st) {
+    hipLaunchKernelGGL((k_attn_rows<DH, CT>), dim3((unsigned)(p.items * p.HKV)), dim3(NT), 0, st, p);
+    if (p.spare > 0)
+        hipLaunchKernelGGL((k_attn_join<DH, 16>), dim3((unsigned)(plan.blocks * p.HKV * plan.row_groups)), dim3(NT), 0, st, p,
+                           plan.row_groups);
+}
+
 }  // namespace
 
 extern "C" int gdn_version(void) { return (0 << 16) | 1; }
@@ -3746,7 +3781,7 @@ static gdn_status check_cache(const void* k_cache, const void* v_cache, const fl
         return fail(GDN_ERR_INVALID_ARG, "page=%d n_pages=%d max_pages=%d must be positive", page, n_pages, max_pages);
     if (page != 16 && page != 32 && page != 64 && page != 128)
         return fail(GDN_ERR_UNSUPPORTED, "page=%d: only 16, 32, 64 and 128 are implemented", page);
-    if ((long)max_pages * page >= (1L << 31)) return fail(GDN_ERR_UNSUPPORTED, "max_pages=%d too large", max_pages);
+    if ((long)max_pages * page > (1L << 30)) return fail(GDN_ERR_UNSUPPORTED, "max_pages=%d too large", max_pages);
     if (!k_cache || !v_cache || !block_table || !seq_lens)
         return fail(GDN_ERR_INVALID_ARG, "k_cache, v_cache, block_table and seq_lens must be non-null");
     if (!aligned(k_cache, 16) || !aligned(v_cache, 16)) return fail(GDN_ERR_INVALID_ARG, "a cache is not 16-byte aligned");
@@ -3879,8 +3914,10 @@ extern "C" gdn_status gdn_kv_append(const void* q, const void* k, const void* v,
 }
 
 extern "C" size_t gdn_attention_paged_workspace_bytes(int B, int T, int H, int H_kv, int d, int page, int max_pages, int n_seqs) {
-    (void)B; (void)T; (void)H; (void)H_kv; (void)d; (void)page; (void)max_pages; (void)n_seqs;
-    return 0;
+    if (B < 1 || T < 1 || H < 1 || H_kv < 1 || H % H_kv || (d != 64 && d != 128) || n_seqs < 0 || (n_seqs > 0 && B != 1) ||
+        page < 1 || max_pages < 1)
+        return 0;
+    return paged_layout(paged_plan(B, T, H, H_kv, n_seqs), H_kv, d).total;
 }
 
 extern "C" gdn_status gdn_attention_paged(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
@@ -3906,20 +3943,23 @@ extern "C" gdn_status gdn_attention_paged(const void* q, const void* k_cache, co
     PagedParams p = {};
     p.q = static_cast<const bf16_t*>(q);
     p.o = static_cast<bf16_t*>(o);
-    p.tokens = (long)B * T;
-    p.H = H; p.HKV = H_kv;
+    p.H = H; p.HKV = H_kv; p.G = H / H_kv;
     p.scale_log2 = scale * 1.4426950408889634f;
     p.s.cu = cu_seqlens; p.s.lens = seq_lens; p.s.n = n_seqs > 0 ? n_seqs : B; p.s.T = T;
     p.c = make_cache(k_cache, v_cache, k_scale, v_scale, block_table, page, n_pages, max_pages);
+    const PagedPlan plan = paged_plan(B, T, H, H_kv, n_seqs);
+    const PagedLayout lay = paged_layout(plan, H_kv, d);
+    p.items = (int)(plan.blocks + plan.spare); p.spare = (int)plan.spare;
+    p.pml = reinterpret_cast<float2*>(workspace);
+    p.po = reinterpret_cast<float*>(static_cast<char*>(workspace) + lay.po);
     hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
     (void)hipGetLastError();
-    const dim3 grid((unsigned)((p.tokens * H + NT / 64 - 1) / (NT / 64)));
     if (cache_dtype == GDN_BF16) {
-        if (d == 128) hipLaunchKernelGGL((k_attn_paged<128, bf16_t>), grid, dim3(NT), 0, hs, p);
-        else hipLaunchKernelGGL((k_attn_paged<64, bf16_t>), grid, dim3(NT), 0, hs, p);
+        if (d == 128) launch_paged<128, bf16_t>(p, plan, hs);
+        else launch_paged<64, bf16_t>(p, plan, hs);
     } else {
-        if (d == 128) hipLaunchKernelGGL((k_attn_paged<128, uint8_t>), grid, dim3(NT), 0, hs, p);
-        else hipLaunchKernelGGL((k_attn_paged<64, uint8_t>), grid, dim3(NT), 0, hs, p);
+        if (d == 128) launch_paged<128, uint8_t>(p, plan, hs);
+        else launch_paged<64, uint8_t>(p, plan, hs);
     }
     return launched();
 }
