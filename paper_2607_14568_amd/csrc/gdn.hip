@@ -3182,28 +3182,40 @@ void launch_append_e4m3(const RowsParams& p, int row_wgs, long pages, hipStream_
     hipLaunchKernelGGL((k_append_e4m3<DH, IT>), dim3((unsigned)(row_wgs + pages * p.HKV * 2)), dim3(NT), 0, st, p, row_wgs);
 }
 
-// How gdn_attention_paged cuts a step (pure host arithmetic, so that the workspace needs no device): row blocks of RB rows
-// per key/value head at most, and items beyond one per block.
+// How gdn_attention_paged cuts a step (pure host arithmetic, so that the workspace needs no device): see PagedParams.
 struct PagedPlan {
-    int rb;                // rows per block
-    long blocks, spare;
-    int row_groups;        // groups of 4 rows that a block can hold
+    int rb;                      // rows per block
+    long blocks, items;          // row blocks, and items, per key/value head at most
+    int round, fine, spare;
+    int joins;                   // workgroups of k_attn_join per row block
 };
-PagedPlan paged_plan(int B, int T, int H, int H_kv, int n_seqs) {
+PagedPlan paged_plan(int B, int T, int H, int H_kv, int page, int max_pages, int n_seqs) {
     const long G = H / H_kv;
-    PagedPlan p;
-    p.rb = 16;
+    PagedPlan p = {};
+    p.rb = T * G > 32L * std::max(n_seqs, 1) ? AQ : 16;
     p.blocks = n_seqs > 0 ? (T * G) / p.rb + std::min<long>(n_seqs, T) : B * ((T * G + p.rb - 1) / p.rb);
-    p.row_groups = n_seqs > 0 ? p.rb / 4 : (int)((std::min<long>(T * G, p.rb) + 3) / 4);
-    const long want = 4 * PLAN_CUS / H_kv;   // items per key/value head
-    p.spare = std::max(0L, want - p.blocks);
+    p.joins = p.rb == 16 ? (int)std::min<long>(T * G, 16) : (int)(std::min<long>(T * G, AQ) + 15) / 16;
+    const long units = ((long)page * max_pages + UNIT - 1) / UNIT;   // of a row block at most
+    p.round = (int)std::max(1L, 2 * PLAN_CUS / H_kv);   // two workgroups per CU
+    if (p.rb == 16) {
+        p.fine = 8;
+        const long most = 8 * PLAN_CUS / H_kv;
+        p.spare = (int)std::max(0L, std::min(most - p.blocks, p.blocks * units / p.fine));
+        p.items = std::max<long>(p.blocks + p.spare, std::min<long>(p.round, p.blocks * units));
+        if (units == 1) p.spare = 0;
+    } else {
+        p.fine = 1 << 23;
+        p.items = std::max<long>(p.blocks, std::min<long>(p.round, p.blocks * units));
+        p.spare = p.items > p.blocks + p.blocks / 4 ? (int)(p.items - p.blocks) : 0;
+    }
+    if (p.spare == 0) p.items = p.blocks;
     return p;
 }
 struct PagedLayout { size_t po, total; };
 PagedLayout paged_layout(const PagedPlan& p, int H_kv, int d) {
     PagedLayout l = {0, 0};
     if (p.spare == 0) return l;
-    const size_t rows = (size_t)(p.blocks + p.spare) * H_kv * p.rb;
+    const size_t rows = (size_t)p.items * H_kv * p.rb;
     l.po = round_up(rows * sizeof(float2), 256);
     l.total = l.po + rows * d * sizeof(float);
     return l;
@@ -3211,10 +3223,13 @@ PagedLayout paged_layout(const PagedPlan& p, int H_kv, int d) {
 
 template <int DH, typename CT>
 void launch_paged(const PagedParams& p, const PagedPlan& plan, hipStream_t st) {
-    hipLaunchKernelGGL((k_attn_rows<DH, CT>), dim3((unsigned)(p.items * p.HKV)), dim3(NT), 0, st, p);
-    if (p.spare > 0)
-        hipLaunchKernelGGL((k_attn_join<DH, 16>), dim3((unsigned)(plan.blocks * p.HKV * plan.row_groups)), dim3(NT), 0, st, p,
-                           plan.row_groups);
+    const dim3 grid((unsigned)(p.items * p.HKV)), joins((unsigned)(plan.blocks * p.HKV * plan.joins));
+    if (plan.rb == 16) hipLaunchKernelGGL((k_attn_rows<DH, CT>), grid, dim3(NT), 0, st, p);
+    else hipLaunchKernelGGL((k_attn_tile<DH, CT, 1>), grid, dim3(NT_ATT), 0, st, p);
+    if (p.spare > 0) {
+        if (plan.rb == 16) hipLaunchKernelGGL((k_attn_join<DH, 16>), joins, dim3(NT), 0, st, p, plan.joins);
+        else hipLaunchKernelGGL((k_attn_join<DH, AQ>), joins, dim3(NT), 0, st, p, plan.joins);
+    }
 }
 
 }  // namespace
@@ -3917,7 +3932,7 @@ extern "C" size_t gdn_attention_paged_workspace_bytes(int B, int T, int H, int H
     if (B < 1 || T < 1 || H < 1 || H_kv < 1 || H % H_kv || (d != 64 && d != 128) || n_seqs < 0 || (n_seqs > 0 && B != 1) ||
         page < 1 || max_pages < 1)
         return 0;
-    return paged_layout(paged_plan(B, T, H, H_kv, n_seqs), H_kv, d).total;
+    return paged_layout(paged_plan(B, T, H, H_kv, page, max_pages, n_seqs), H_kv, d).total;
 }
 
 extern "C" gdn_status gdn_attention_paged(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
@@ -3947,9 +3962,9 @@ extern "C" gdn_status gdn_attention_paged(const void* q, const void* k_cache, co
     p.scale_log2 = scale * 1.4426950408889634f;
     p.s.cu = cu_seqlens; p.s.lens = seq_lens; p.s.n = n_seqs > 0 ? n_seqs : B; p.s.T = T;
     p.c = make_cache(k_cache, v_cache, k_scale, v_scale, block_table, page, n_pages, max_pages);
-    const PagedPlan plan = paged_plan(B, T, H, H_kv, n_seqs);
+    const PagedPlan plan = paged_plan(B, T, H, H_kv, page, max_pages, n_seqs);
     const PagedLayout lay = paged_layout(plan, H_kv, d);
-    p.items = (int)(plan.blocks + plan.spare); p.spare = (int)plan.spare;
+    p.items = (int)plan.items; p.round = plan.round; p.fine = plan.fine; p.spare = plan.spare;
     p.pml = reinterpret_cast<float2*>(workspace);
     p.po = reinterpret_cast<float*>(static_cast<char*>(workspace) + lay.po);
     hipStream_t hs = reinterpret_cast<hipStream_t>(stream);

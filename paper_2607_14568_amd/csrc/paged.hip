@@ -374,11 +374,11 @@ __global__ __launch_bounds__(NT) void k_append_e4m3(RowsParams p, int row_wgs) {
 
 // ------------------------------------------------------------------ attention: items of a step
 // The query rows of a sequence and key/value head, r = i G + g for new token i and the g-th of the head's G query heads, go
-// in blocks of RB.  A block's keys are cut into chunks of c units of UNIT keys, c so that the step's items, (row block,
-// chunk) pairs, are at most `items`: with N the sum over the row blocks of their units and X = items - (row blocks),
-// c = ceil(N / X) gives at most N / c + (row blocks).  So the long sequences of a batch are cut and the short ones are not,
-// whatever their lengths, which the host does not know.  A block of one chunk writes its output, one of several
-// partial sums, which k_attn_join adds up in order.
+// in blocks of RB.  A block's keys are cut into chunks of c units of UNIT keys, c from the step's lengths, which the host
+// does not know: the least with which all items, (row block, chunk) pairs, are resident at once (`round` of them per
+// key/value head); where that is more than `fine` units, max(fine, N / spare) with N the units of all row blocks, which
+// gives at most N / c + (row blocks) items.  So the long sequences of a batch are cut and the short ones are not.  A block of
+// one chunk writes its output, one of several partial sums, which k_attn_join adds up in order.
 constexpr int UNIT = 128;
 
 struct PagedParams {
@@ -386,7 +386,8 @@ struct PagedParams {
     bf16_t* o;
     int H, HKV, G;
     float scale_log2;
-    int items, spare;      // items per key/value head (the grid), and those beyond one per row block (0: no cuts)
+    int items;             // per key/value head (the grid)
+    int round, fine, spare; // see above; spare 0: no cuts
     float* po;             // partial sums of item w, head hk: [w HKV + hk][RB][DH], and their largest score and weight sum
     float2* pml;           // ... [w HKV + hk][RB]
     StepSeqs s;
@@ -418,15 +419,24 @@ template <int RB, bool BLOCK = false> __device__ __forceinline__ bool find_item(
     };
     int at = 0, c = 1 << 23;   // (2^30 keys, the most a table holds)
     if (p.spare > 0) {
-        long total = 0;
-        for (int base = 0; base < p.s.n; base += 64) {
-            load(base, at);
-            total += (long)nrb * units;
-        }
+        // the sum over the row blocks of ceil(units / c), and (c = 1) of their units
+        auto count = [&](int c) {
+            long sum = 0;
+            int at = 0;
+            for (int base = 0; base < p.s.n; base += 64) {
+                if (base > 0 || p.s.n > 64) load(base, at);
+                sum += (long)nrb * ((units + c - 1) / c);
+            }
 #pragma unroll
-        for (int off = 1; off < 64; off <<= 1) total += __shfl_xor(total, off, 64);
-        c = (int)min((total + p.spare - 1) / p.spare, (long)c);
-        c = max(__builtin_amdgcn_readfirstlane(c), 1);
+            for (int off = 1; off < 64; off <<= 1) sum += __shfl_xor(sum, off, 64);
+            return __shfl(sum, 0, 64);
+        };
+        load(0, at);
+        const long total = count(1);
+        c = (int)min(max((total + p.round - 1) / p.round, 1L), (long)c);
+        while (c <= p.fine && count(c) > p.round) c += (c + 7) / 8;
+        if (c > p.fine) c = (int)min(max((total + p.spare - 1) / p.spare, (long)p.fine), 1L << 23);
+        c = __builtin_amdgcn_readfirstlane(c);
     }
     int items = 0, blocks = 0;   // before sequence base
     at = 0;
@@ -449,9 +459,9 @@ template <int RB, bool BLOCK = false> __device__ __forceinline__ bool find_item(
             it.nrb = __builtin_amdgcn_readlane(nrb, l);
             const int fi = items + __builtin_amdgcn_readlane(si - cnt, l), fb = blocks + __builtin_amdgcn_readlane(sb - nrb, l);
             const int r = BLOCK ? w - fb : w - fi;
-            it.rb = r % it.nrb;
+            it.rb = it.nrb - 1 - r % it.nrb;   // (blocks with the most keys first)
             it.chunk = r / it.nrb;
-            it.first = fi + it.rb;
+            it.first = fi + r % it.nrb;
             it.c = c * UNIT;
             it.end = block_end<RB>(p, it.n, it.len, it.rb);
             return true;
@@ -681,17 +691,20 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
             acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va), pf, acc[n], 0, 0, 0);
         }
     };
-    Step a, b;
-    int kb = k0 + 32 * wave;
-    if (kb < k1) load(a, kb);
-    while (kb < k1) {
-        if (kb + 32 * NW < k1) load(b, kb + 32 * NW);
-        compute(a, kb);
-        kb += 32 * NW;
-        if (kb >= k1) break;
-        if (kb + 32 * NW < k1) load(a, kb + 32 * NW);
-        compute(b, kb);
-        kb += 32 * NW;
+    // DEPTH steps' loads are in flight: 16 KB a wave
+    constexpr int DEPTH = 256 / (DH * ESZ) + 1, NEXT = 32 * NW;
+    Step ring[DEPTH];
+#pragma unroll
+    for (int z = 0; z < DEPTH - 1; ++z)
+        if (k0 + 32 * wave + NEXT * z < k1) load(ring[z], k0 + 32 * wave + NEXT * z);
+    for (int kb = k0 + 32 * wave; kb < k1; kb += NEXT * DEPTH) {
+#pragma unroll
+        for (int z = 0; z < DEPTH; ++z) {
+            const int at = kb + NEXT * z;
+            if (at >= k1) break;
+            if (at + NEXT * (DEPTH - 1) < k1) load(ring[(z + DEPTH - 1) % DEPTH], at + NEXT * (DEPTH - 1));
+            compute(ring[z], at);
+        }
     }
     // the four waves' sums: acc[n][e] is channel CW (4 lg + e) + n of query l16
     l += __shfl_xor(l, 16, 64);
@@ -730,41 +743,350 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
     }
 }
 
-// ------------------------------------------------------------------ k_attn_join
-// One wave per row: the sum of its chunks' partial sums, in order (so that the result does not depend on which ended first).
-template <int DH, int RB>
-__global__ __launch_bounds__(NT) void k_attn_join(PagedParams p, int groups) {   // groups of 4 rows per row block
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int u = blockIdx.x / groups, r = (int)(blockIdx.x % groups) * (NT / 64) + wave, hk = u % p.HKV;
+// ------------------------------------------------------------------ k_attn_tile: many rows
+// Attention of blocks of 128 rows; bound by the matrix units and the softmax beside them.  Blocks of 64 keys and values
+// lie in a double-buffered LDS ring (16-byte chunks XOR-swizzled as in k_attn_causal, whose products, running softmax and
+// operand orders these are): a bf16 cache is copied there without registers, e4m3 codes are loaded a block ahead, made
+// bf16 once (exactly) and stored; their scales multiply the scores and the weights.
+template <int DH, typename CT, int QT>
+__global__ __launch_bounds__(NT_ATT / QT) __attribute__((amdgpu_waves_per_eu(4 / QT))) void k_attn_tile(PagedParams p) {
+    constexpr bool E4M3 = sizeof(CT) == 1;
+    constexpr int RB = AQ, NTH = NT_ATT / QT, NW = NTH / 64, NCH = DH / 8, RPI = 64 / NCH, NKB = DH / 32, NDT = DH / 16, ESZ = sizeof(CT);
+    __shared__ AttnLds<DH> lds;
+    __shared__ int odd;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l16 = lane & 15, lg = lane >> 4;
+    const int hk = (int)(blockIdx.x % p.HKV);
     Item it;
-    if (!find_item<RB, true>(p, u / p.HKV, it)) return;
-    const int rr = it.rb * RB + r;
-    if (it.end <= it.c || rr >= it.n * p.G) return;
-    const int chunks = (it.end + it.c - 1) / it.c;
-    auto slot = [&](int j) { return ((long)(it.first + j * it.nrb) * p.HKV + hk) * RB + r; };
-    float M = LOWEST, sum = 0.f;
-    for (int j0 = 0; j0 < chunks; j0 += 64) M = fmaxf(M, j0 + lane < chunks ? p.pml[slot(j0 + lane)].x : LOWEST);
+    if (!find_item<RB>(p, (int)(blockIdx.x / p.HKV), it)) return;
+    const int k0 = it.chunk * it.c, k1 = min(it.end - k0, it.c) + k0;
+    if (it.chunk > 0 && k0 >= it.end) return;
+    const int rows = it.n * p.G, base = it.len - it.n;   // rows of the sequence; position of its first new token
+    const int r0 = it.rb * RB + 16 * QT * wave;          // this wave's first row
+    const int wlast = r0 < rows ? base + min(r0 + 16 * QT - 1, rows - 1) / p.G : -1;   // the last key that its rows see
+    auto swz = [](int r) {
+        return NCH == 16 ? (4 * (r & 3)) | (2 * ((r >> 2) & 1)) | ((r >> 3) & 1)
+                         : (4 * ((r >> 1) & 1)) | (2 * ((r >> 2) & 1)) | ((r >> 3) & 1);
+    };
+    auto kq = [swz](int r, int cc) { return r * DH + (((cc >> 3) ^ swz(r)) << 3) + (cc & 7); };
+
+    int last[QT];   // of this lane's rows
+    bf16x8 qf[QT][NKB];
 #pragma unroll
-    for (int off = 1; off < 64; off <<= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
-    constexpr int CPL = DH / 64;   // channels per lane
-    float o[CPL] = {};
-    for (int j0 = 0; j0 < chunks; j0 += 64) {
-        const float2 ml = j0 + lane < chunks ? p.pml[slot(j0 + lane)] : float2{LOWEST, 0.f};
-        const float w = __builtin_amdgcn_exp2f(ml.x - M);
-        sum += w * ml.y;
-        const int many = min(chunks - j0, 64);
-#pragma unroll 4
-        for (int j = 0; j < many; ++j) {
-            const float wj = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), j));
-            const float* src = p.po + slot(j0 + j) * DH + CPL * lane;
+    for (int u = 0; u < QT; ++u) {
+        const int r = r0 + 16 * u + l16, qi = r / p.G;
+        last[u] = base + qi;
+        const bf16_t* src = p.q + ((long)(it.tok + qi) * p.H + hk * p.G + r % p.G) * DH;
 #pragma unroll
-            for (int e = 0; e < CPL; ++e) o[e] += wj * src[e];
+        for (int kb = 0; kb < NKB; ++kb) {
+            qf[u][kb] = bf16x8{};
+            if (r < rows) qf[u][kb] = *reinterpret_cast<const bf16x8*>(src + 32 * kb + 8 * lg);
         }
     }
+    PageWalk<E4M3> walk;
+    walk.row = p.c.table + (long)it.s * p.c.max_pages;
+    if (k1 > k0) walk.load(p, hk, k0 >> p.c.shift);
+    // what a block's keys need when they are used, taken when their copies are sent off
+    struct Block { int there; float ks[E4M3 ? 4 : 1], vs[E4M3 ? 4 : 1]; } cur, nxt;   // there: bit t, the page of keys 16 t ..
+    auto look = [&](Block& x, int kb) {
+        x.there = 0;
 #pragma unroll
-    for (int off = 1; off < 64; off <<= 1) sum += __shfl_xor(sum, off, 64);
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    bf16_t* dst = p.o + ((long)(it.tok + rr / p.G) * p.H + hk * p.G + rr % p.G) * DH + CPL * lane;
+        for (int t = 0; t < 4; ++t) {
+            const int key = kb + 16 * t, b = key >> p.c.shift;
+            const int id = key < k1 ? walk.page(p, hk, b) : -1;
+            x.there |= (id >= 0) << t;
+            if constexpr (E4M3) {
+                x.ks[t] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, walk.ks), b - walk.first));
+                x.vs[t] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, walk.vs), b - walk.first));
+            }
+        }
+    };
+    // Rows of the block at key kb by descriptors whose offset 0 would be the block's first row: of the whole block where a page
+    // holds it, else of the 16 rows around row r.  Rows past the item's keys, and of pages that are not there, read as zeros.
+    auto describe = [&](int kb, int r, __amdgpu_buffer_rsrc_t& rk, __amdgpu_buffer_rsrc_t& rv) {
+        const int g = p.c.page >= AKB ? 0 : r & ~15, span = p.c.page >= AKB ? AKB : 16, key = kb + g;
+        const int id = key < k1 ? walk.page(p, hk, key >> p.c.shift) : -1;
+        const long at = (((((long)max(id, 0) * p.HKV + hk) << p.c.shift) + (key & (p.c.page - 1))) - g) * DH * ESZ;
+        const uint32_t bytes = id >= 0 ? (uint32_t)(g + min(k1 - key, span)) * DH * ESZ : 0;
+        rk = rsrc((const char*)p.c.k + at, bytes);
+        rv = rsrc((const char*)p.c.v + at, bytes);
+    };
+    constexpr int NCW = AKB / RPI / NW;                   // bf16: this wave's 1 KB copies of K, and of V
+    constexpr int PB = AKB * DH / NTH < 16 ? 8 : 16;      // e4m3: bytes of a piece, and this thread's pieces of K, and of V
+    constexpr int NCB = AKB * DH / PB / NTH;
+    static_assert(NCW >= 1 && NCB >= 1, "every thread copies the same share");
+    int4v kc[E4M3 ? NCB : 1], vc[E4M3 ? NCB : 1];
+    auto issue = [&](int kb, auto SLOT) {
+        constexpr int sl = decltype(SLOT)::value;
+        __amdgpu_buffer_rsrc_t rk, rv;
+        if constexpr (E4M3) {
 #pragma unroll
-    for (int e = 0; e < CPL; ++e) dst[e] = from_f<bf16_t>(o[e] * inv);
+            for (int c = 0; c < NCB; ++c) {
+                const int row = 64 * (wave + NW * c) * PB / DH;   // the first of the wave's rows
+                if (c == 0 || p.c.page < AKB) describe(kb, row, rk, rv);
+                const int off = (tid + NTH * c) * PB;
+                if constexpr (PB == 16) {
+                    kc[c] = __builtin_bit_cast(int4v, bload16(rk, off));
+                    vc[c] = __builtin_bit_cast(int4v, bload16(rv, off));
+                } else {
+                    const auto k2 = __builtin_amdgcn_raw_buffer_load_b64(rk, off, 0, 0), v2 = __builtin_amdgcn_raw_buffer_load_b64(rv, off, 0, 0);
+                    kc[c] = int4v{(int)k2[0], (int)k2[1], 0, 0};
+                    vc[c] = int4v{(int)v2[0], (int)v2[1], 0, 0};
+                }
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < NCW; ++c) {
+                const int first = RPI * (wave + NW * c), r = first + lane / NCH;
+                if (c == 0 || p.c.page < AKB) describe(kb, first, rk, rv);
+                const int off = r * DH * 2 + (((lane % NCH) ^ swz(r)) << 4);
+                bdma16(rk, &lds.k[sl][first * DH], off);
+                bdma16(rv, &lds.v[sl][first * DH], off);
+            }
+        }
+    };
+    auto stage = [&](auto SLOT) {   // e4m3: the loaded codes into the ring
+        constexpr int sl = decltype(SLOT)::value;
+        if constexpr (E4M3) {
+#pragma unroll
+            for (int c = 0; c < NCB; ++c) {
+                const int piece = tid + NTH * c, r = piece * PB / DH, cc = piece * PB % DH;
+#pragma unroll
+                for (int z = 0; z < PB / 8; ++z) {
+                    const int4v k4 = {fp8_pair(kc[c][2 * z], false), fp8_pair(kc[c][2 * z], true),
+                                      fp8_pair(kc[c][2 * z + 1], false), fp8_pair(kc[c][2 * z + 1], true)};
+                    const int4v v4 = {fp8_pair(vc[c][2 * z], false), fp8_pair(vc[c][2 * z], true),
+                                      fp8_pair(vc[c][2 * z + 1], false), fp8_pair(vc[c][2 * z + 1], true)};
+                    *reinterpret_cast<int4v*>(&lds.k[sl][kq(r, cc + 8 * z)]) = k4;
+                    *reinterpret_cast<int4v*>(&lds.v[sl][kq(r, cc + 8 * z)]) = v4;
+                }
+            }
+        }
+    };
+    const float sl2 = p.scale_log2;
+    float m[QT], l[QT];
+    floatx4 oacc[QT][NDT];
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+        m[u] = LOWEST;
+        l[u] = 0.f;
+#pragma unroll
+        for (int t = 0; t < NDT; ++t) oacc[u][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    // A weight of 0 does not hide a value that is not finite (0 x NaN).  In the blocks from `part` on, where some rows do not
+    // see a key that others see, such values are taken out, and the rows that see them are made NaN at the end.
+    const int all = base + it.rb * RB / p.G;   // the last key that every row sees
+    const int part = all < k0 ? k0 : k0 + (all + 1 - k0) / AKB * AKB;
+    if (tid == 0) odd = 0;
+    auto block = [&](const int kb, auto SLOT) {
+        constexpr int SL = decltype(SLOT)::value;
+        if constexpr (!E4M3) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's copies of the block
+        lds_barrier();   // everyone's; the other slot is no longer read
+        cur = nxt;
+        if (kb + AKB < k1) {
+            look(nxt, kb + AKB);
+            issue(kb + AKB, Ic<1 - SL>{});
+        }
+        if (kb >= part) {
+            bool found = false;
+#pragma unroll
+            for (int c = 0; c < AKB * DH / 8 / NTH; ++c) {
+                int4v* at = reinterpret_cast<int4v*>(&lds.v[SL][(tid + NTH * c) * 8]);
+                int4v x = *at;
+                bool any = false;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const bool hi = (x[i] & 0x7f800000) == 0x7f800000, lo = (x[i] & 0x7f80) == 0x7f80;
+                    any = any || hi || lo;
+                    x[i] = (hi ? 0 : x[i] & 0xffff0000) | (lo ? 0 : x[i] & 0xffff);
+                }
+                if (any) *at = x;
+                found = found || any;
+            }
+            if (found) odd = 1;
+            lds_barrier();
+        }
+        if (kb <= wlast) {
+            const bf16_t* sk = lds.k[SL];
+            const bf16_t* sv = lds.v[SL];
+            floatx4 st[QT][4];   // S^T of query tile u: keys 16 t + 4 lg + e, query l16
+#pragma unroll
+            for (int u = 0; u < QT; ++u)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) st[u][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int i = 0; i < NKB; ++i) {
+                    const bf16x8 ka = *reinterpret_cast<const bf16x8*>(&sk[kq(16 * t + l16, 32 * i + 8 * lg)]);
+#pragma unroll
+                    for (int u = 0; u < QT; ++u) st[u][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qf[u][i], st[u][t], 0, 0, 0);
+                }
+            const bool whole = kb + AKB <= k1 && cur.there == 15;
+            bf16x8 pf[QT][2];
+#pragma unroll
+            for (int u = 0; u < QT; ++u) {
+                const bool diag = !whole || kb + AKB - 1 > base + (r0 + 16 * u) / p.G;   // some key is masked for this tile
+                if constexpr (E4M3) {
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) st[u][t] *= cur.ks[t];
+                }
+                // bm: the block's largest scaled score of this lane's query; the weights are 2^(fs x - m)
+                float bm, fs = sl2;
+                if (!diag && sl2 >= 0.f) {
+                    bm = st[u][0][0];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) bm = fmaxf(bm, st[u][t][e]);
+                    bm *= sl2;
+                } else {
+                    bm = -INFINITY;
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int key = kb + 16 * t + 4 * lg + e;
+                            const float x = key > last[u] || key >= k1 || !((cur.there >> t) & 1) ? -INFINITY : st[u][t][e] * sl2;
+                            st[u][t][e] = x;
+                            bm = fmaxf(bm, x);
+                        }
+                    fs = 1.f;
+                }
+                // the reference m moves only when a score passes it by more than 8 (weights stay below 2^8)
+                if (__builtin_amdgcn_ballot_w64(bm > m[u] + 8.f)) {
+                    bm = fmaxf(bm, __shfl_xor(bm, 16, 64));
+                    bm = fmaxf(bm, __shfl_xor(bm, 32, 64));
+                    const float mn = bm > m[u] + 8.f ? bm : m[u], a = __builtin_amdgcn_exp2f(m[u] - mn);
+#pragma unroll
+                    for (int t = 0; t < NDT; ++t) oacc[u][t] *= a;
+                    l[u] *= a;
+                    m[u] = mn;
+                }
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        st[u][t][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[u][t][e], fs, -m[u]));
+                        l[u] += st[u][t][e];
+                    }
+                if constexpr (E4M3) {
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) st[u][t] *= cur.vs[t];
+                }
+                pf[u][0] = pack_bf16(st[u][0], st[u][1]);
+                pf[u][1] = pack_bf16(st[u][2], st[u][3]);
+            }
+#pragma unroll
+            for (int t = 0; t < NDT; ++t)
+#pragma unroll
+                for (int kk = 0; kk < 2; ++kk) {
+                    const int r = 32 * kk + 4 * lg + (l16 >> 2), c = 16 * t + 4 * (l16 & 3);
+                    const bf16x8 va = join4(lds_tr8(&sv[kq(r, c)]), lds_tr8(&sv[kq(r + 16, c)]));
+#pragma unroll
+                    for (int u = 0; u < QT; ++u) oacc[u][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pf[u][kk], oacc[u][t], 0, 0, 0);
+                }
+        }
+        if (kb + AKB < k1) stage(Ic<1 - SL>{});
+    };
+    if (k0 < k1) {
+        look(nxt, k0);
+        issue(k0, Ic<0>{});
+        stage(Ic<0>{});
+    }
+    for (int kb = k0; kb < k1; kb += 2 * AKB) {
+        block(kb, Ic<0>{});
+        if (kb + AKB < k1) block(kb + AKB, Ic<1>{});
+    }
+    // (the barrier behind the last search of the values, if there was one, is ahead of this read)
+#pragma unroll 1
+    for (int key = part < k1 && odd ? part : k1; key < k1; ++key) {   // (rare)
+        const int id = __builtin_amdgcn_readfirstlane(page_of(p.c, it.s, key >> p.c.shift));
+        if (id < 0) continue;
+        const long at = ((((long)id * p.HKV + hk) << p.c.shift) + (key & (p.c.page - 1))) * DH + 4 * lg;
+#pragma unroll
+        for (int t = 0; t < NDT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const CT x = ((const CT*)p.c.v)[at + 16 * t + e];
+                const bool bad = E4M3 ? (x & 0x7f) == 0x7f : (x & 0x7f80) == 0x7f80;
+#pragma unroll
+                for (int u = 0; u < QT; ++u)
+                    if (bad && key <= last[u]) oacc[u][t][e] = __uint_as_float(0x7fc00000u);
+            }
+    }
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+        l[u] += __shfl_xor(l[u], 16, 64);
+        l[u] += __shfl_xor(l[u], 32, 64);
+        const int r = r0 + 16 * u + l16;
+        if (r >= rows) continue;
+        if (it.end <= it.c) {   // the only chunk
+            const float inv = l[u] == 0.f ? 0.f : 1.f / l[u];   // no key: zeros
+            bf16_t* dst = p.o + ((long)(it.tok + r / p.G) * p.H + hk * p.G + r % p.G) * DH + 4 * lg;
+#pragma unroll
+            for (int t = 0; t < NDT; ++t) *reinterpret_cast<bf16x4*>(dst + 16 * t) = __builtin_convertvector(oacc[u][t] * inv, bf16x4);
+        } else {
+            const long slot = (long)blockIdx.x * RB + (r - it.rb * RB);
+            if (lg == 0) p.pml[slot] = float2{m[u], l[u]};
+#pragma unroll
+            for (int t = 0; t < NDT; ++t) *reinterpret_cast<floatx4*>(p.po + slot * DH + 16 * t + 4 * lg) = oacc[u][t];
+        }
+    }
+}
+
+// ------------------------------------------------------------------ k_attn_join
+// The sum of a row's chunks' partial sums, over loads of 4 channels a lane, lanes and waves in a fixed order (so that the
+// result does not depend on which chunk ended first).  Rows of 16-row blocks may have many chunks: a workgroup a row, its
+// waves sharing them.  Those of 128-row blocks have few: a wave a row, 16 rows a workgroup.
+template <int DH, int RB>
+__global__ __launch_bounds__(NT) void k_attn_join(PagedParams p, int groups) {   // workgroups per row block
+    constexpr int LPR = DH / 4, SUB = 64 / LPR, NW = NT / 64;   // lanes per row; chunks that a wave's load takes at once
+    constexpr int ROWS = RB == 16 ? 1 : 16, SHARE = RB == 16 ? NW : 1;   // rows per workgroup, waves per row
+    __shared__ float red[NW][DH];
+    __shared__ float reds[NW];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int u = blockIdx.x / groups, hk = u % p.HKV, c4 = 4 * (lane % LPR);
+    Item it;
+    if (!find_item<RB, true>(p, u / p.HKV, it) || it.end <= it.c) return;
+    const int chunks = (it.end + it.c - 1) / it.c;
+    for (int i = SHARE == 1 ? wave : 0; i < ROWS; i += NW) {
+        const int r = (int)(blockIdx.x % groups) * ROWS + i, rr = it.rb * RB + r;
+        if (rr >= it.n * p.G) return;
+        auto slot = [&](int j) { return ((long)(it.first + j * it.nrb) * p.HKV + hk) * RB + r; };
+        float M = LOWEST, sum = 0.f;
+        for (int j0 = 0; j0 < chunks; j0 += 64) M = fmaxf(M, j0 + lane < chunks ? p.pml[slot(j0 + lane)].x : LOWEST);
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
+        floatx4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int j = (SHARE == 1 ? 0 : wave * SUB) + lane / LPR; j < chunks; j += SHARE * SUB) {
+            const float2 ml = p.pml[slot(j)];
+            const float w = __builtin_amdgcn_exp2f(ml.x - M);
+            sum += w * ml.y;
+            o += w * f4(p.po + slot(j) * DH + c4);
+        }
+#pragma unroll
+        for (int off = LPR; off < 64; off <<= 1) {
+            sum += __shfl_xor(sum, off, 64);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], off, 64);
+        }
+        if constexpr (SHARE > 1) {
+            if (lane < LPR) *reinterpret_cast<floatx4*>(&red[wave][c4]) = o;
+            if (lane == 0) reds[wave] = sum;
+            __syncthreads();
+            if (wave != 0) return;
+            sum = reds[0];
+            o = f4(&red[0][c4]);
+#pragma unroll
+            for (int w = 1; w < NW; ++w) {
+                sum += reds[w];
+                o += f4(&red[w][c4]);
+            }
+        }
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        bf16_t* dst = p.o + ((long)(it.tok + rr / p.G) * p.H + hk * p.G + rr % p.G) * DH + c4;
+        if (lane < LPR) *reinterpret_cast<bf16x4*>(dst) = __builtin_convertvector(o * inv, bf16x4);
+    }
 }
