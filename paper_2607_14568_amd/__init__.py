@@ -406,10 +406,14 @@ def gdn_attention_prefill(q, k, v, *, scale=None, cu_seqlens=None, o=None):
     return o
 
 
-def _same_device(device, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.device != device:
-            raise ValueError("%s is on %s, q or k on %s" % (name, t.device, device))
+def _same(dev, *tensors):
+    """Each (tensor or None, name, dtype): contiguous, of that type, on device number ``dev``."""
+    for t, name, dtype in tensors:
+        if t is None:
+            continue
+        if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
+            _dev(t, name, dtype)
+            raise ValueError("%s is on %s, the call's first tensor on device %d" % (name, t.device, dev))
 
 
 def _rows(t, name, dtype):
@@ -429,64 +433,53 @@ def _rows(t, name, dtype):
     return st if T > 1 else sb if B > 1 else h * d
 
 
-def _out(t, like, name, shape, dtype):
-    if t is None:
-        return torch.empty(shape, device=like.device, dtype=dtype)
-    _dev(t, name, dtype)
-    if tuple(t.shape) != tuple(shape):
+def _shaped(t, name, shape):
+    if t is not None and t.shape != shape:
         raise ValueError("%s must be %s, got %s" % (name, tuple(shape), tuple(t.shape)))
-    return t
-
-
-def _turn_args(d, q_weight, k_weight, inv_freq):
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is not None:
-            _dev(w, name, torch.float32)
-            if tuple(w.shape) != (d,):
-                raise ValueError("%s must be [%d], got %s" % (name, d, tuple(w.shape)))
-    if inv_freq is None:
-        return 0
-    _dev(inv_freq, "inv_freq", torch.float64)
-    return 2 * inv_freq.numel()
 
 
 def _packed(cu_seqlens, B):
+    """(n_seqs of the C call, sequences)."""
     if cu_seqlens is None:
         return 0, B
-    _dev(cu_seqlens, "cu_seqlens", torch.int32)
     n_seqs = cu_seqlens.numel() - 1
     return n_seqs, n_seqs
 
 
-def _cache_args(k_cache, v_cache, k_scale, v_scale, block_table, seq_lens, n, Hkv, d):
-    if not isinstance(k_cache, torch.Tensor) or k_cache.dtype not in _CACHE:
+def _cache_args(dev, k_cache, v_cache, k_scale, v_scale, block_table, seq_lens, cu_seqlens, n, Hkv, d):
+    ct = _CACHE.get(k_cache.dtype) if isinstance(k_cache, torch.Tensor) else None
+    if ct is None:
         raise TypeError("k_cache must be bfloat16 or float8_e4m3fn")
-    _dev(k_cache, "k_cache")
-    _dev(v_cache, "v_cache", k_cache.dtype)
-    _dev(block_table, "block_table", torch.int32)
-    _dev(seq_lens, "seq_lens", torch.int32)
-    if k_cache.dim() != 4 or k_cache.shape[1] != Hkv or k_cache.shape[3] != d or v_cache.shape != k_cache.shape:
+    _same(dev, (k_cache, "k_cache", k_cache.dtype), (v_cache, "v_cache", k_cache.dtype), (block_table, "block_table", torch.int32),
+          (seq_lens, "seq_lens", torch.int32), (cu_seqlens, "cu_seqlens", torch.int32))
+    shape = k_cache.shape
+    if len(shape) != 4 or shape[1] != Hkv or shape[3] != d or v_cache.shape != shape:
         raise ValueError("k_cache and v_cache must be [n_pages, %d, page, %d], got %s and %s" % (
-            Hkv, d, tuple(k_cache.shape), tuple(v_cache.shape)))
-    if block_table.dim() != 2 or block_table.shape[0] != n or tuple(seq_lens.shape) != (n,):
+            Hkv, d, tuple(shape), tuple(v_cache.shape)))
+    table = block_table.shape
+    if len(table) != 2 or table[0] != n or seq_lens.shape != (n,):
         raise ValueError("block_table must be [%d, max_pages] and seq_lens [%d], got %s and %s" % (
-            n, n, tuple(block_table.shape), tuple(seq_lens.shape)))
-    for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
-        if (t is None) != (k_cache.dtype is torch.bfloat16):
-            raise ValueError("%s belongs to a float8_e4m3fn cache, and to no other" % name)
-        if t is not None:
-            _dev(t, name, torch.float32)
-            if tuple(t.shape) != tuple(k_cache.shape[:2]):
-                raise ValueError("%s must be %s, got %s" % (name, tuple(k_cache.shape[:2]), tuple(t.shape)))
-    return k_cache.shape[2], k_cache.shape[0], block_table.shape[1], _CACHE[k_cache.dtype]
+            n, n, tuple(table), tuple(seq_lens.shape)))
+    if ct == GDN_E4M3:
+        if k_scale is None or v_scale is None:
+            raise ValueError("a float8_e4m3fn cache needs k_scale and v_scale")
+        _same(dev, (k_scale, "k_scale", torch.float32), (v_scale, "v_scale", torch.float32))
+        _shaped(k_scale, "k_scale", shape[:2])
+        _shaped(v_scale, "v_scale", shape[:2])
+    elif k_scale is not None or v_scale is not None:
+        raise ValueError("k_scale and v_scale belong to a float8_e4m3fn cache")
+    return shape[2], shape[0], table[1], ct
 
 
-def _on(device, call, *args):
-    """call(*args, the current stream of `device`), with that device current."""
-    if device.index == torch.cuda.current_device():
-        return _check(call(*args, _stream(device)))
-    with torch.cuda.device(device):
-        return _check(call(*args, _stream(device)))
+def _on(dev, call, *args):
+    """call(*args, the current stream of device ``dev``), with that device current."""
+    if dev == torch._C._cuda_getDevice():
+        status = call(*args, _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream(dev).cuda_stream)
+    else:
+        with torch.cuda.device(dev):
+            status = call(*args, torch.cuda.current_stream(dev).cuda_stream)
+    if status != 0:
+        _check(status)
 
 
 def gdn_qk_norm_rope(q, k, *, q_weight=None, k_weight=None, eps=1e-6, inv_freq=None, interleaved=False, positions=None,
@@ -502,18 +495,26 @@ def gdn_qk_norm_rope(q, k, *, q_weight=None, k_weight=None, eps=1e-6, inv_freq=N
     qs, ks = _rows(q, "q", q.dtype), _rows(k, "k", q.dtype)
     B, T, H, d = q.shape
     Hkv = k.shape[2]
-    if tuple(k.shape) != (B, T, Hkv, d):
+    if k.shape != (B, T, Hkv, d):
         raise ValueError("inconsistent shapes q%s k%s" % (tuple(q.shape), tuple(k.shape)))
-    rot = _turn_args(d, q_weight, k_weight, inv_freq)
+    if q_out is None:
+        q_out = torch.empty(q.shape, device=q.device, dtype=q.dtype)
+    if k_out is None:
+        k_out = torch.empty(k.shape, device=k.device, dtype=k.dtype)
+    dev = q.get_device()
+    if k.get_device() != dev:
+        raise ValueError("q is on %s, k on %s" % (q.device, k.device))
+    _same(dev, (q_out, "q_out", q.dtype), (k_out, "k_out", q.dtype), (q_weight, "q_weight", torch.float32),
+          (k_weight, "k_weight", torch.float32), (inv_freq, "inv_freq", torch.float64), (positions, "positions", torch.int32),
+          (cu_seqlens, "cu_seqlens", torch.int32))
+    _shaped(q_out, "q_out", q.shape)
+    _shaped(k_out, "k_out", k.shape)
+    _shaped(q_weight, "q_weight", (d,))
+    _shaped(k_weight, "k_weight", (d,))
+    _shaped(positions, "positions", (B, T))
+    rot = 0 if inv_freq is None else 2 * inv_freq.numel()
     n_seqs, _ = _packed(cu_seqlens, B)
-    if positions is not None:
-        _dev(positions, "positions", torch.int32)
-        if tuple(positions.shape) != (B, T):
-            raise ValueError("positions must be [%d, %d], got %s" % (B, T, tuple(positions.shape)))
-    q_out, k_out = _out(q_out, q, "q_out", q.shape, q.dtype), _out(k_out, k, "k_out", k.shape, k.dtype)
-    _same_device(q.device, k=k, q_weight=q_weight, k_weight=k_weight, inv_freq=inv_freq, positions=positions,
-                 cu_seqlens=cu_seqlens, q_out=q_out, k_out=k_out)
-    _on(q.device, lib().gdn_qk_norm_rope, _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), B, T, H, Hkv, d, qs, ks,
+    _on(dev, lib().gdn_qk_norm_rope, _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), B, T, H, Hkv, d, qs, ks,
         _ptr(q_weight), _ptr(k_weight), float(eps), _ptr(inv_freq), rot, _ptr(positions), _ptr(cu_seqlens), n_seqs,
         _IO[q.dtype], GDN_ROPE_INTERLEAVED if interleaved else 0)
     return q_out, k_out
@@ -529,24 +530,30 @@ def gdn_kv_append(k, v, k_cache, v_cache, block_table, seq_lens, *, q=None, q_ou
     ``gdn_qk_norm_rope``.  Returns q_out (None without q).
     """
     ks, vs = _rows(k, "k", torch.bfloat16), _rows(v, "v", torch.bfloat16)
-    B, T, Hkv, d = k.shape
-    if v.shape != k.shape:
+    shape = B, T, Hkv, d = k.shape
+    if v.shape != shape:
         raise ValueError("inconsistent shapes k%s v%s" % (tuple(k.shape), tuple(v.shape)))
-    H, qs = Hkv, 0
+    dev, H, qs = k.get_device(), Hkv, 0
     if q is not None:
         qs, H = _rows(q, "q", torch.bfloat16), q.shape[2]
-        if tuple(q.shape) != (B, T, H, d):
+        if q.shape != (B, T, H, d):
             raise ValueError("inconsistent shapes q%s k%s" % (tuple(q.shape), tuple(k.shape)))
-        q_out = _out(q_out, q, "q_out", q.shape, q.dtype)
+        if q_out is None:
+            q_out = torch.empty(q.shape, device=q.device, dtype=q.dtype)
     elif q_out is not None:
         raise ValueError("q_out without q")
-    rot = _turn_args(d, q_weight, k_weight, inv_freq)
+    if v.get_device() != dev or (q is not None and q.get_device() != dev):
+        raise ValueError("q, k and v must be on one device")
+    _same(dev, (q_out, "q_out", torch.bfloat16), (q_weight, "q_weight", torch.float32), (k_weight, "k_weight", torch.float32),
+          (inv_freq, "inv_freq", torch.float64))
+    if q_out is not None:
+        _shaped(q_out, "q_out", q.shape)
+    _shaped(q_weight, "q_weight", (d,))
+    _shaped(k_weight, "k_weight", (d,))
+    rot = 0 if inv_freq is None else 2 * inv_freq.numel()
     n_seqs, n = _packed(cu_seqlens, B)
-    page, n_pages, max_pages, ct = _cache_args(k_cache, v_cache, k_scale, v_scale, block_table, seq_lens, n, Hkv, d)
-    _same_device(k.device, v=v, q=q, q_out=q_out, k_cache=k_cache, v_cache=v_cache, k_scale=k_scale, v_scale=v_scale,
-                 block_table=block_table, seq_lens=seq_lens, q_weight=q_weight, k_weight=k_weight, inv_freq=inv_freq,
-                 cu_seqlens=cu_seqlens)
-    _on(k.device, lib().gdn_kv_append, _ptr(q), _ptr(k), _ptr(v), _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale),
+    page, n_pages, max_pages, ct = _cache_args(dev, k_cache, v_cache, k_scale, v_scale, block_table, seq_lens, cu_seqlens, n, Hkv, d)
+    _on(dev, lib().gdn_kv_append, _ptr(q), _ptr(k), _ptr(v), _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale),
         _ptr(v_scale), _ptr(block_table), _ptr(seq_lens), B, T, H, Hkv, d, page, n_pages, max_pages, qs, ks, vs,
         _ptr(q_weight), _ptr(k_weight), float(eps), _ptr(inv_freq), rot, _ptr(cu_seqlens), n_seqs, GDN_BF16, ct,
         GDN_ROPE_INTERLEAVED if interleaved else 0)
@@ -568,20 +575,19 @@ def gdn_attention_paged(q, k_cache, v_cache, block_table, seq_lens, *, k_scale=N
     if q.dim() != 4:
         raise ValueError("q must be [B, T, heads, d], got %s" % (tuple(q.shape),))
     B, T, H, d = q.shape
+    dev = q.get_device()
+    if o is None:
+        o = torch.empty(q.shape, device=q.device, dtype=q.dtype)
+    _same(dev, (o, "o", torch.bfloat16), (workspace, "workspace", torch.uint8))
+    _shaped(o, "o", q.shape)
     n_seqs, n = _packed(cu_seqlens, B)
     Hkv = k_cache.shape[1] if isinstance(k_cache, torch.Tensor) and k_cache.dim() == 4 else 0
-    page, n_pages, max_pages, ct = _cache_args(k_cache, v_cache, k_scale, v_scale, block_table, seq_lens, n, Hkv, d)
-    o = _out(o, q, "o", q.shape, q.dtype)
+    page, n_pages, max_pages, ct = _cache_args(dev, k_cache, v_cache, k_scale, v_scale, block_table, seq_lens, cu_seqlens, n, Hkv, d)
     if workspace is None:
         need = gdn_attention_paged_workspace_bytes(B, T, H, Hkv, d, page, max_pages, n_seqs)
         workspace = torch.empty(need, device=q.device, dtype=torch.uint8) if need else None
-    else:
-        _dev(workspace, "workspace", torch.uint8)
-    _same_device(q.device, k_cache=k_cache, v_cache=v_cache, k_scale=k_scale, v_scale=v_scale, block_table=block_table,
-                 seq_lens=seq_lens, cu_seqlens=cu_seqlens, o=o, workspace=workspace)
-    sc = float(scale) if scale is not None else 1.0 / float(d) ** 0.5
-    ws, ws_bytes = (None, 0) if workspace is None or workspace.numel() == 0 else (_ptr(workspace), workspace.numel())
-    _on(q.device, lib().gdn_attention_paged, _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale),
+    ws_bytes = 0 if workspace is None else workspace.numel()
+    _on(dev, lib().gdn_attention_paged, _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale),
         _ptr(block_table), _ptr(seq_lens), _ptr(o), B, T, H, Hkv, d, page, n_pages, max_pages, _ptr(cu_seqlens), n_seqs,
-        GDN_BF16, ct, sc, ws, ws_bytes)
+        GDN_BF16, ct, float(scale) if scale is not None else d ** -0.5, _ptr(workspace) if ws_bytes else None, ws_bytes)
     return o

@@ -3169,17 +3169,17 @@ void rows_split(RowsParams& p, int rows, int dh) {
 }
 long rows_wgs(const RowsParams& p) { return (p.tokens * p.units + NT / 64 - 1) / (NT / 64); }
 
-template <typename IO>
+template <typename IO, bool E4M3 = false>
 void launch_rows(RowsParams p, int d, hipStream_t st) {
     rows_split(p, p.H * (p.q != nullptr) + p.HKV * ((p.k != nullptr) + (p.v != nullptr)), d);
     const dim3 grid((unsigned)rows_wgs(p));
-    if (d == 128) hipLaunchKernelGGL((k_rows<IO, 128>), grid, dim3(NT), 0, st, p);
-    else hipLaunchKernelGGL((k_rows<IO, 64>), grid, dim3(NT), 0, st, p);
+    if (d == 128) hipLaunchKernelGGL((k_rows<IO, 128, E4M3>), grid, dim3(NT), 0, st, p);
+    else hipLaunchKernelGGL((k_rows<IO, 64, E4M3>), grid, dim3(NT), 0, st, p);
 }
 
 template <int DH, int IT>
-void launch_append_e4m3(const RowsParams& p, int row_wgs, long pages, hipStream_t st) {
-    hipLaunchKernelGGL((k_append_e4m3<DH, IT>), dim3((unsigned)(row_wgs + pages * p.HKV * 2)), dim3(NT), 0, st, p, row_wgs);
+void launch_append_e4m3(const RowsParams& p, int row_wgs, long pages, int each, hipStream_t st) {
+    hipLaunchKernelGGL((k_append_e4m3<DH, IT>), dim3((unsigned)(row_wgs + pages * p.HKV * 2)), dim3(NT), 0, st, p, row_wgs, each);
 }
 
 // How gdn_attention_paged cuts a step (pure host arithmetic, so that the workspace needs no device): see PagedParams.
@@ -3906,8 +3906,14 @@ extern "C" gdn_status gdn_kv_append(const void* q, const void* k, const void* v,
         launch_rows<bf16_t>(p, d, hs);
         return launched();
     }
+    if (n_seqs == 0 && T == 1) {
+        (void)hipGetLastError();
+        launch_rows<bf16_t, true>(p, d, hs);
+        return launched();
+    }
     // pages that the new tokens can touch: n tokens lie in at most (n - 1) / page + 2
-    const long pages = n_seqs > 0 ? (long)T / page + 2L * n_seqs : (long)B * (((long)T + page - 2) / page + 1);
+    const int each = (int)(((long)T + page - 2) / page + 1);
+    const long pages = n_seqs > 0 ? (long)T / page + 2L * n_seqs : (long)B * each;
     int row_wgs = 0;
     if (q) {
         rows_split(p, H, d);
@@ -3916,14 +3922,14 @@ extern "C" gdn_status gdn_kv_append(const void* q, const void* k, const void* v,
     if (row_wgs + pages * H_kv * 2 >= (1L << 31)) return fail(GDN_ERR_UNSUPPORTED, "B*T*H_kv too large");
     (void)hipGetLastError();
     if (d == 128) {
-        if (page == 16) launch_append_e4m3<128, 1>(p, row_wgs, pages, hs);
-        else if (page == 32) launch_append_e4m3<128, 2>(p, row_wgs, pages, hs);
-        else if (page == 64) launch_append_e4m3<128, 4>(p, row_wgs, pages, hs);
-        else launch_append_e4m3<128, 8>(p, row_wgs, pages, hs);
+        if (page == 16) launch_append_e4m3<128, 1>(p, row_wgs, pages, each, hs);
+        else if (page == 32) launch_append_e4m3<128, 2>(p, row_wgs, pages, each, hs);
+        else if (page == 64) launch_append_e4m3<128, 4>(p, row_wgs, pages, each, hs);
+        else launch_append_e4m3<128, 8>(p, row_wgs, pages, each, hs);
     } else {
-        if (page <= 32) launch_append_e4m3<64, 1>(p, row_wgs, pages, hs);
-        else if (page == 64) launch_append_e4m3<64, 2>(p, row_wgs, pages, hs);
-        else launch_append_e4m3<64, 4>(p, row_wgs, pages, hs);
+        if (page <= 32) launch_append_e4m3<64, 1>(p, row_wgs, pages, each, hs);
+        else if (page == 64) launch_append_e4m3<64, 2>(p, row_wgs, pages, each, hs);
+        else launch_append_e4m3<64, 4>(p, row_wgs, pages, each, hs);
     }
     return launched();
 }

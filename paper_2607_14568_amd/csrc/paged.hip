@@ -12,6 +12,24 @@ struct StepSeqs {
     int n, T;             // sequences; tokens of a dense sequence (packed: of the call)
 };
 
+// Inclusive scans over the wave's lanes (values of 0 or more): within rows of 16 lanes, then row ends into the rows behind.
+template <typename F> __device__ __forceinline__ int wave_scan(int x, F f) {
+    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));   // row_shr:1
+    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));
+    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));
+    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));
+    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));   // row_bcast:15
+    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));   // row_bcast:31
+    return x;
+}
+__device__ __forceinline__ int scan_add(int x) { return wave_scan(x, [](int a, int b) { return a + b; }); }
+__device__ __forceinline__ int scan_max(int x) { return wave_scan(x, [](int a, int b) { return max(a, b); }); }
+__device__ __forceinline__ int last_lane(int x) { return __builtin_amdgcn_readlane(x, 63); }
+// the lane before's value (lane 0: `first`)
+__device__ __forceinline__ int lane_before(int x, int first) {
+    return __builtin_amdgcn_update_dpp(first, x, 0x138, 0xf, 0xf, false);   // wave_shr:1
+}
+
 // The tokens [beg, end) of the call that are new in sequence base + lane (none past the last sequence).  Called by a whole
 // wave, with base = 0, 64, .. and `at` (0 at first) carried along.  Packed offsets outside the contract are clamped into
 // a nondecreasing partition of [0, T].
@@ -22,15 +40,9 @@ __device__ __forceinline__ void span64(const StepSeqs& q, int base, int& at, int
         end = min(j + 1, q.n) * q.T;
         return;
     }
-    end = j < q.n ? min(max(q.cu[j + 1], at), q.T) : at;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const int y = __shfl_up(end, off, 64);
-        if (lane >= off) end = max(end, y);
-    }
-    const int y = __shfl_up(end, 1, 64);
-    beg = lane > 0 ? y : at;
-    at = __builtin_amdgcn_readlane(end, 63);
+    end = scan_max(j < q.n ? min(max(q.cu[j + 1], at), q.T) : at);
+    beg = lane_before(end, at);
+    at = last_lane(end);
 }
 
 // Sequence of token t of the call (a scalar), its place i among the sequence's new tokens and their number n; false for
@@ -75,28 +87,25 @@ __device__ __forceinline__ void angle(const Turn& t, int i, double pos, float& c
     sincospif((float)(2 * a), &sn, &cs);
 }
 
-// the angles of a chunk's 8 channels
-__device__ __forceinline__ void angles(const Turn& t, int c, int pos, float (&cs)[8], float (&sn)[8]) {
+// cos and sin of the pairs of a chunk's 8 channels, from tables [rot / 2] of a position; the sign of the sine is that of the
+// channel's own term: y = x cos + partner sin.
+__device__ __forceinline__ void angles(const Turn& t, int c, const float* tc, const float* ts, float (&cs)[8], float (&sn)[8]) {
     if (8 * c >= t.rot) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) { cs[e] = 1.f; sn[e] = 0.f; }
-        return;
-    }
-    if (t.near) {
+    } else if (t.near) {
+        const floatx4 a = f4(tc + 4 * c), b = f4(ts + 4 * c);
 #pragma unroll
-        for (int e = 0; e < 8; e += 2) {
-            angle(t, 4 * c + e / 2, pos, cs[e], sn[e]);
-            cs[e + 1] = cs[e];
-            sn[e + 1] = sn[e];
-            sn[e] = -sn[e];
+        for (int e = 0; e < 8; ++e) { cs[e] = a[e / 2]; sn[e] = e % 2 ? b[e / 2] : -b[e / 2]; }
+    } else {
+        const int hc = t.rot / 16, first = c < hc, at = 8 * (first ? c : c - hc);
+        const floatx4 a = f4(tc + at), a2 = f4(tc + at + 4), b = f4(ts + at), b2 = f4(ts + at + 4);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            cs[e] = e < 4 ? a[e] : a2[e - 4];
+            sn[e] = e < 4 ? b[e] : b2[e - 4];
+            if (first) sn[e] = -sn[e];
         }
-        return;
-    }
-    const int hc = t.rot / 16, first = c < hc;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        angle(t, 8 * (first ? c : c - hc) + e, pos, cs[e], sn[e]);
-        if (first) sn[e] = -sn[e];
     }
 }
 
@@ -165,9 +174,60 @@ __device__ __forceinline__ int page_of(const Cache& c, int s, long b) {
     return id >= 0 && id < c.n_pages ? id : -1;
 }
 
+constexpr float LOWEST = -3.402823466e38f;   // a running maximum's start: finite, so that no difference is NaN
+
+// ------------------------------------------------------------------ e4m3
+// e4m3 codes with one scale per page and head, the smallest power of two s >= 2^-100 with every finite value at most 448 s
+// (448: the type's largest).  A power of two costs a floating type no precision, and a page that later needs a larger
+// scale has its codes brought to it exactly, but for those that become subnormal (under 2^-15 of the page's largest).
+__device__ __forceinline__ float power_scale(float amax) {
+    const uint32_t u = __float_as_uint(amax);
+    const int e = (int)(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u);   // biased; 448 = 1.75 2^8
+    return __uint_as_float((uint32_t)max(e, 27) << 23);
+}
+__device__ __forceinline__ uint64_t to_e4m3(const float (&x)[8], float inv) {   // round to nearest even; not finite: NaN
+    float y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = fabsf(x[e]) <= -LOWEST ? x[e] * inv : __uint_as_float(0x7fc00000u);
+    int a = 0, b = 0;
+    a = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], a, false);
+    a = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], a, true);
+    b = __builtin_amdgcn_cvt_pk_fp8_f32(y[4], y[5], b, false);
+    b = __builtin_amdgcn_cvt_pk_fp8_f32(y[6], y[7], b, true);
+    return (uint64_t)(uint32_t)a | (uint64_t)(uint32_t)b << 32;
+}
+__device__ __forceinline__ void from_e4m3(uint64_t codes, float (&x)[8]) {
+    typedef float floatx2 __attribute__((ext_vector_type(2)));
+    const int a = (int)(uint32_t)codes, b = (int)(uint32_t)(codes >> 32);
+    const floatx2 y[4] = {__builtin_amdgcn_cvt_pk_f32_fp8(a, false), __builtin_amdgcn_cvt_pk_f32_fp8(a, true),
+                          __builtin_amdgcn_cvt_pk_f32_fp8(b, false), __builtin_amdgcn_cvt_pk_f32_fp8(b, true)};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = y[e / 2][e % 2];
+}
+
+// This lane's 8 codes of rows r0, r0 + step, .. below r1 brought to another scale (N rows' loads at a time).
+template <int N> __device__ __forceinline__ void rescale(uint8_t* codes, int pitch, int r0, int r1, int step, float ratio) {
+#pragma unroll 1
+    for (int r = r0; r < r1; r += N * step) {
+        uint64_t y[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (r + i * step < r1) y[i] = *reinterpret_cast<const uint64_t*>(codes + (r + i * step) * pitch);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (r + i * step < r1) {
+                float z[8];
+                from_e4m3(y[i], z);
+                *reinterpret_cast<uint64_t*>(codes + (r + i * step) * pitch) = to_e4m3(z, ratio);
+            }
+    }
+}
+
 // ------------------------------------------------------------------ k_rows: tokens' rows, normed and rotated
-// One wave takes `per` groups of 64 / (DH / 8) rows of one token: its q heads, its k heads and, into a bf16 cache, its v
-// heads (those as they are).  Bound by memory: every row is read once and written once.
+// One wave takes `per` groups of 64 / (DH / 8) rows of one token: its q heads, its k heads and, into a cache, its v heads
+// (those as they are); into an e4m3 cache only where a sequence has one new token, whose rows are then all there is of a
+// page's and head's new values.  Each lane forms one angle of the token's position, the wave's tables of them lie in LDS.
+// Bound by memory: every row is read once and written once.
 struct RowsParams {
     const void* q;
     const void* k;
@@ -186,19 +246,26 @@ struct RowsParams {
     Cache c;
 };
 
-template <typename IO, int DH>
-__device__ __forceinline__ void token_rows(const RowsParams& p, long wave) {
+struct __attribute__((aligned(16))) AngleTable { float c[64], s[64]; };
+
+template <typename IO, int DH, bool E4M3>
+__device__ __forceinline__ void token_rows(const RowsParams& p, long wave, AngleTable& tab) {
     constexpr int LPR = DH / 8, RPG = 64 / LPR;
     const long tok = wave / p.units;
     const int unit = (int)(wave % p.units), lane = threadIdx.x & 63, c = lane % LPR;
     if (tok >= p.tokens) return;
     int s = 0, i = 0, n = 0;
-    if (!step_seq(p.s, tok, s, i, n)) return;
+    if (!step_seq(p.s, (int)tok, s, i, n)) return;
     const int pos = p.pos ? p.pos[tok] : p.s.lens ? p.s.lens[s] - n + i : i;
     float cs[8], sn[8];
-    if (p.t.freq) angles(p.t, c, pos, cs, sn);
+    if (p.t.freq) {
+        if (lane < p.t.rot / 2) angle(p.t, lane, pos, tab.c[lane], tab.s[lane]);
+        __builtin_amdgcn_wave_barrier();   // (the wave's LDS accesses stay in order)
+        angles(p.t, c, tab.c, tab.s, cs, sn);
+    }
     const int HQ = p.q ? p.H : 0, rows = HQ + (p.k ? p.HKV : 0) + (p.v ? p.HKV : 0);
     const int id = p.k && !p.ko && pos >= 0 ? page_of(p.c, s, pos >> p.c.shift) : -1;
+    const int slot = pos & (p.c.page - 1);
     for (int g = 0; g < p.per; ++g) {
         const int j = (unit * p.per + g) * RPG + lane / LPR;
         const int kind = j < HQ ? 0 : j < HQ + p.HKV ? 1 : 2;   // q, k, v
@@ -206,129 +273,143 @@ __device__ __forceinline__ void token_rows(const RowsParams& p, long wave) {
         const IO* src = kind == 0 ? (const IO*)p.q + tok * p.qs : kind == 1 ? (const IO*)p.k + tok * p.ks : (const IO*)p.v + tok * p.vs;
         float x[8] = {};
         if (j < rows) load8(src + h * DH + 8 * c, x);
-        if (kind < 2) {
-            // (a row's lanes share their kind, and the exchanges stay inside a row)
-            turn_row<DH>(p.t, kind == 0 ? p.qw : p.kw, cs, sn, x);
-        }
+        // (a row's lanes share their kind, and the exchanges stay inside a row)
+        if (kind < 2) turn_row<DH>(p.t, kind == 0 ? p.qw : p.kw, cs, sn, x);
         if (j >= rows) continue;
         if (kind == 0) {
             store8((IO*)p.qo + (tok * p.H + h) * DH + 8 * c, x);
         } else if (p.ko) {
             store8((IO*)p.ko + (tok * p.HKV + h) * DH + 8 * c, x);
         } else if (id >= 0) {
-            IO* base = (IO*)(kind == 1 ? p.c.k : p.c.v);
-            store8(base + (((long)id * p.HKV + h) * p.c.page + (pos & (p.c.page - 1))) * DH + 8 * c, x);
+            const long at = (((long)id * p.HKV + h) << p.c.shift) * DH + 8 * c;   // of slot 0
+            if constexpr (!E4M3) {
+                store8((IO*)(kind == 1 ? p.c.k : p.c.v) + at + slot * DH, x);
+            } else {
+                float amax = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[e]) <= -LOWEST ? fabsf(x[e]) : 0.f);
+#pragma unroll
+                for (int off = 1; off < LPR; off <<= 1) amax = fmaxf(amax, __shfl_xor(amax, off, 64));
+                uint8_t* codes = (uint8_t*)(kind == 1 ? p.c.k : p.c.v) + at;
+                float* ps = (kind == 1 ? p.c.ks : p.c.vs) + (long)id * p.HKV + h;
+                float scale = power_scale(amax);
+                if (slot > 0) {
+                    const float old = *ps;
+                    if (old >= scale) {
+                        scale = old;
+                    } else {
+                        rescale<4>(codes, DH, 0, slot, 1, old / scale);
+                    }
+                }
+                *reinterpret_cast<uint64_t*>(codes + slot * DH) = to_e4m3(x, 1.f / scale);
+                if (c == 0) *ps = scale;
+            }
         }
     }
 }
 
-template <typename IO, int DH>
+template <typename IO, int DH, bool E4M3>
 __global__ __launch_bounds__(NT) void k_rows(RowsParams p) {
-    token_rows<IO, DH>(p, (long)blockIdx.x * (NT / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+    __shared__ AngleTable tab[NT / 64];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    token_rows<IO, DH, E4M3>(p, (long)blockIdx.x * (NT / 64) + wave, tab[wave]);
 }
 
 // ------------------------------------------------------------------ k_append_e4m3
-// e4m3 codes with one scale per page and head, the smallest power of two s >= 2^-100 with every finite value at most 448 s
-// (448: the type's largest).  A power of two costs a floating type no precision, and a page that later needs a larger
-// scale has its codes brought to it exactly, but for those that become subnormal (under 2^-15 of the page's largest).
-__device__ __forceinline__ float power_scale(float amax) {
-    const uint32_t u = __float_as_uint(amax);
-    const int e = (int)(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u);   // biased; 448 = 1.75 2^8
-    return __uint_as_float((uint32_t)max(e, 27) << 23);
-}
-__device__ __forceinline__ uint64_t to_e4m3(const float (&x)[8], float inv) {   // round to nearest even; not finite: NaN
-    float y[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = fabsf(x[e]) <= 3.402823466e38f ? x[e] * inv : __uint_as_float(0x7fc00000u);
-    int a = 0, b = 0;
-    a = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], a, false);
-    a = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], a, true);
-    b = __builtin_amdgcn_cvt_pk_fp8_f32(y[4], y[5], b, false);
-    b = __builtin_amdgcn_cvt_pk_fp8_f32(y[6], y[7], b, true);
-    return (uint64_t)(uint32_t)a | (uint64_t)(uint32_t)b << 32;
-}
-__device__ __forceinline__ void from_e4m3(uint64_t codes, float (&x)[8]) {
-    typedef float floatx2 __attribute__((ext_vector_type(2)));
-    const int a = (int)(uint32_t)codes, b = (int)(uint32_t)(codes >> 32);
-    const floatx2 y[4] = {__builtin_amdgcn_cvt_pk_f32_fp8(a, false), __builtin_amdgcn_cvt_pk_f32_fp8(a, true),
-                          __builtin_amdgcn_cvt_pk_f32_fp8(b, false), __builtin_amdgcn_cvt_pk_f32_fp8(b, true)};
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = y[e / 2][e % 2];
-}
-
-// The block-th page that the step's new tokens touch, over all sequences: its sequence s, the page's index b in it, the
-// positions [first, len) of the sequence's new tokens and the call's row of the first of them.  Called by a whole wave;
-// false past the last.
-__device__ __forceinline__ bool touched_block(const StepSeqs& q, int shift, long block, int& s, int& b, int& first, int& len, int& row) {
+// The block-th page that the step's new tokens touch (dense: of `each` pages that a sequence can touch): its sequence s,
+// the page's index b in it, the positions [first, len) of the sequence's new tokens and the call's row of the first of
+// them.  Called by a whole wave; false where there is none.
+__device__ __forceinline__ bool touched_block(const StepSeqs& q, int shift, int each, int block, int& s, int& b, int& first, int& len,
+                                              int& row) {
+    if (!q.cu) {
+        s = block / each;
+        len = tab(q.lens, s);
+        first = max(len - q.T, 0);   // (a token before position 0 is not written)
+        b = (first >> shift) + block % each;
+        row = s * q.T + q.T - (len - first);
+        return len > 0 && b <= (len - 1) >> shift;
+    }
     const int lane = threadIdx.x & 63;
-    int at = 0, beg, end;
-    long before = 0;
+    int at = 0, beg, end, before = 0;
     for (int base = 0; base < q.n; base += 64) {
         span64(q, base, at, beg, end);
         const int L = base + lane < q.n ? q.lens[base + lane] : 0;
-        const int f = max(L - (end - beg), 0);   // (a token before position 0 is not written)
+        const int f = max(L - (end - beg), 0);
         const int cnt = end > beg && L > 0 ? ((L - 1) >> shift) - (f >> shift) + 1 : 0;
-        long sum = cnt;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const long y = __shfl_up(sum, off, 64);
-            if (lane >= off) sum += y;
-        }
+        const int sum = scan_add(cnt);
         const uint64_t past = __builtin_amdgcn_ballot_w64(before + sum > block);
         if (past) {
             const int l = __builtin_ctzll(past);
             s = base + l;
             first = __builtin_amdgcn_readlane(f, l);
             len = __builtin_amdgcn_readlane(L, l);
-            b = (first >> shift) + (int)(block - before) + __builtin_amdgcn_readlane(cnt, l) - (int)__shfl(sum, l, 64);
-            b = __builtin_amdgcn_readfirstlane(b);
+            b = (first >> shift) + block - before - __builtin_amdgcn_readlane(sum - cnt, l);
             row = __builtin_amdgcn_readlane(end, l) - (len - first);
             return true;
         }
-        before += __shfl(sum, 63, 64);
+        before += last_lane(sum);
     }
     return false;
 }
 
 // One workgroup per (touched page, head, K or V), after `row_wgs` workgroups of the q rows.  It holds the page's new
-// tokens in registers, finds their largest value, and writes codes and scale.
+// tokens in registers, finds their largest value, and writes codes and scale.  The angle of slot r = RPP it + i of the page
+// at position a is that of a + RPP it and that of i added up, a product of two table entries: (RPP + IT) rot / 2 sines
+// for RPP IT rows.
 template <int DH, int IT>   // IT: passes of NT / (DH / 8) rows over a page
-__global__ __launch_bounds__(NT) void k_append_e4m3(RowsParams p, int row_wgs) {
-    constexpr int LPR = DH / 8, RPP = NT / LPR;
+__global__ __launch_bounds__(NT) void k_append_e4m3(RowsParams p, int row_wgs, int each) {
+    constexpr int LPR = DH / 8, RPP = NT / LPR, NP = DH / 2;
     __shared__ float red[NT / 64];
+    __shared__ __align__(16) float tc[RPP + IT][NP], ts[RPP + IT][NP];   // of i, then of a + RPP it
     const int tid = threadIdx.x, c = tid % LPR, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     if ((int)blockIdx.x < row_wgs) {
+        static_assert(sizeof(AngleTable) * (NT / 64) <= sizeof tc, "the tables of the q rows' waves");
         RowsParams r = p;
         r.k = r.v = nullptr;
-        token_rows<bf16_t, DH>(r, (long)blockIdx.x * (NT / 64) + wave);
+        token_rows<bf16_t, DH, false>(r, (long)blockIdx.x * (NT / 64) + wave, reinterpret_cast<AngleTable*>(tc)[wave]);
         return;
     }
-    const long u = (long)blockIdx.x - row_wgs;
-    const int is_v = (int)(u & 1), h = (int)(u / 2 % p.HKV);
+    const int u = (int)blockIdx.x - row_wgs;
+    const int is_v = u & 1, h = u / 2 % p.HKV;
     int s, b, first, len, row;
-    if (!touched_block(p.s, p.c.shift, u / 2 / p.HKV, s, b, first, len, row)) return;
-    const int id = page_of(p.c, s, b);
+    if (!touched_block(p.s, p.c.shift, each, u / 2 / p.HKV, s, b, first, len, row)) return;
+    const int id = __builtin_amdgcn_readfirstlane(page_of(p.c, s, b));
     if (id < 0) return;
-    const long at0 = (long)b << p.c.shift;   // position of the page's first slot
-    const int lo = (int)max(first - at0, 0L), hi = (int)min(len - at0, (long)p.c.page);   // its new slots
+    const int at0 = b << p.c.shift;   // position of the page's first slot (b lies in the table: under 2^30)
+    const int lo = max(first - at0, 0), hi = min(len - at0, p.c.page);   // its new slots
     const bf16_t* src = (const bf16_t*)(is_v ? p.v : p.k) + h * DH + 8 * c;
     const long stride = is_v ? p.vs : p.ks;
     float x[IT][8], amax = 0.f;
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
         const int r = it * RPP + tid / LPR;
-        const bool in = r >= lo && r < hi;
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[it][e] = 0.f;
-        if (in) load8(src + (row + (at0 + r - first)) * stride, x[it]);
+        if (r >= lo && r < hi) load8(src + (row + (at0 + r - first)) * stride, x[it]);
     }
     if (!is_v) {
+        const int np = p.t.rot / 2;
+        for (int z = tid; z < (RPP + IT) * np; z += NT) {
+            const int i = z / np, j = z % np;
+            angle(p.t, j, i < RPP ? i : at0 + (i - RPP) * RPP, tc[i][j], ts[i][j]);
+        }
+        __syncthreads();
+        float cs[8], sn[8];
+        if (np) angles(p.t, c, tc[tid / LPR], ts[tid / LPR], cs, sn);
 #pragma unroll
         for (int it = 0; it < IT; ++it) {
             if (it * RPP >= hi || (it + 1) * RPP <= lo) continue;   // (the whole workgroup's)
-            float cs[8], sn[8];
-            if (p.t.freq) angles(p.t, c, (int)at0 + it * RPP + tid / LPR, cs, sn);
-            turn_row<DH>(p.t, p.kw, cs, sn, x[it]);
+            float ca[8], sa[8], ct[8], st[8];
+            if (np) {
+                angles(p.t, c, tc[RPP + it], ts[RPP + it], ca, sa);
+                // both sines carry the channel's sign g: (g s)(g s') = s s' and g (s c' + c s') as wanted
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    ct[e] = cs[e] * ca[e] - sn[e] * sa[e];
+                    st[e] = sn[e] * ca[e] + cs[e] * sa[e];
+                }
+            }
+            turn_row<DH>(p.t, p.kw, ct, st, x[it]);
         }
     }
 #pragma unroll
@@ -336,7 +417,7 @@ __global__ __launch_bounds__(NT) void k_append_e4m3(RowsParams p, int row_wgs) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float m = fabsf(x[it][e]);
-            amax = fmaxf(amax, m <= 3.402823466e38f ? m : 0.f);
+            amax = fmaxf(amax, m <= -LOWEST ? m : 0.f);
         }
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) amax = fmaxf(amax, __shfl_xor(amax, off, 64));
@@ -347,19 +428,13 @@ __global__ __launch_bounds__(NT) void k_append_e4m3(RowsParams p, int row_wgs) {
     for (int w = 1; w < NT / 64; ++w) amax = fmaxf(amax, red[w]);
     float scale = power_scale(amax);
     float* ps = (is_v ? p.c.vs : p.c.ks) + (long)id * p.HKV + h;
-    uint8_t* codes = (uint8_t*)(is_v ? p.c.v : p.c.k) + ((long)id * p.HKV + h) * p.c.page * DH + 8 * c;
+    uint8_t* codes = (uint8_t*)(is_v ? p.c.v : p.c.k) + (((long)id * p.HKV + h) << p.c.shift) * DH + 8 * c;
     if (lo > 0) {   // the page holds earlier tokens of the sequence, in its old scale
         const float old = *ps;
         if (old >= scale) {
             scale = old;
         } else {
-            const float ratio = old / scale;
-            for (int r = tid / LPR; r < lo; r += RPP) {
-                uint64_t* at = (uint64_t*)(codes + r * DH);
-                float y[8];
-                from_e4m3(*at, y);
-                *at = to_e4m3(y, ratio);
-            }
+            rescale<4>(codes, DH, tid / LPR, lo, RPP, old / scale);
         }
     }
     const float inv = 1.f / scale;
@@ -419,23 +494,29 @@ template <int RB, bool BLOCK = false> __device__ __forceinline__ bool find_item(
     };
     int at = 0, c = 1 << 23;   // (2^30 keys, the most a table holds)
     if (p.spare > 0) {
-        // the sum over the row blocks of ceil(units / c), and (c = 1) of their units
+        // the sum over the row blocks of ceil(units / c) (a lane's share held to 2^24: what matters is whether it is small)
         auto count = [&](int c) {
-            long sum = 0;
-            int at = 0;
+            int sum = 0, at = 0;
             for (int base = 0; base < p.s.n; base += 64) {
                 if (base > 0 || p.s.n > 64) load(base, at);
-                sum += (long)nrb * ((units + c - 1) / c);
+                sum = (int)min((long)nrb * ((units + c - 1) / c) + sum, 1L << 24);
             }
-#pragma unroll
-            for (int off = 1; off < 64; off <<= 1) sum += __shfl_xor(sum, off, 64);
-            return __shfl(sum, 0, 64);
+            return last_lane(scan_add(sum));
         };
         load(0, at);
-        const long total = count(1);
-        c = (int)min(max((total + p.round - 1) / p.round, 1L), (long)c);
+        // N as a float, 2^-20 off at most, which the divisions below make up for
+        float total = 0.f;
+        for (int base = 0, z = 0; base < p.s.n; base += 64) {
+            if (base > 0 || p.s.n > 64) load(base, z);
+            total += (float)nrb * (float)units;
+        }
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) total += __shfl_xor(total, off, 64);
+        total *= 1.f - 0x1p-19f;
+        c = max((int)min(ceilf(total / (float)p.round), 0x1p23f), 1);
         while (c <= p.fine && count(c) > p.round) c += (c + 7) / 8;
-        if (c > p.fine) c = (int)min(max((total + p.spare - 1) / p.spare, (long)p.fine), 1L << 23);
+        if (c > p.fine) c = max((int)min(ceilf(total * (1.f + 0x1p-17f) / (float)p.spare), 0x1p23f), p.fine);
+        c = min(c, 1 << 23);
         c = __builtin_amdgcn_readfirstlane(c);
     }
     int items = 0, blocks = 0;   // before sequence base
@@ -443,12 +524,7 @@ template <int RB, bool BLOCK = false> __device__ __forceinline__ bool find_item(
     for (int base = 0; base < p.s.n; base += 64) {
         if (base > 0 || p.spare == 0 || p.s.n > 64) load(base, at);
         const int cnt = nrb * ((units + c - 1) / c);
-        int si = cnt, sb = nrb;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const int y = __shfl_up(si, off, 64), z = __shfl_up(sb, off, 64);
-            if (lane >= off) { si += y; sb += z; }
-        }
+        const int si = scan_add(cnt), sb = BLOCK ? scan_add(nrb) : 0;
         const uint64_t past = __builtin_amdgcn_ballot_w64((BLOCK ? blocks + sb : items + si) > w);
         if (past) {
             const int l = __builtin_ctzll(past);
@@ -457,8 +533,8 @@ template <int RB, bool BLOCK = false> __device__ __forceinline__ bool find_item(
             it.n = __builtin_amdgcn_readlane(end, l) - it.tok;
             it.len = __builtin_amdgcn_readlane(L, l);
             it.nrb = __builtin_amdgcn_readlane(nrb, l);
-            const int fi = items + __builtin_amdgcn_readlane(si - cnt, l), fb = blocks + __builtin_amdgcn_readlane(sb - nrb, l);
-            const int r = BLOCK ? w - fb : w - fi;
+            const int fi = items + __builtin_amdgcn_readlane(si - cnt, l);
+            const int r = w - (BLOCK ? blocks + __builtin_amdgcn_readlane(sb - nrb, l) : fi);
             it.rb = it.nrb - 1 - r % it.nrb;   // (blocks with the most keys first)
             it.chunk = r / it.nrb;
             it.first = fi + r % it.nrb;
@@ -466,8 +542,8 @@ template <int RB, bool BLOCK = false> __device__ __forceinline__ bool find_item(
             it.end = block_end<RB>(p, it.n, it.len, it.rb);
             return true;
         }
-        items += __builtin_amdgcn_readlane(si, 63);
-        blocks += __builtin_amdgcn_readlane(sb, 63);
+        items += last_lane(si);
+        blocks += last_lane(sb);
     }
     return false;
 }
@@ -517,8 +593,6 @@ __device__ __forceinline__ int fp8_pair(int src, bool high) {   // two e4m3 code
     const bf16x2 r = high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(src, 1.f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(src, 1.f, false);
     return __builtin_bit_cast(int, r);
 }
-
-constexpr float LOWEST = -3.402823466e38f;   // a running maximum's start: finite, so that no difference is NaN
 
 template <int DH, typename CT>
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_attn_rows(PagedParams p) {
