@@ -3164,7 +3164,7 @@ void launch_attention(AttnParams a, hipStream_t st) {
 // place in one wave.
 void rows_split(RowsParams& p, int rows, int dh) {
     const int groups = (rows + 512 / dh - 1) / (512 / dh);   // 64 / (dh / 8) rows each
-    p.per = (int)std::min<long>(groups, std::max<long>(1, p.tokens * groups / 8192));
+    p.per = (int)std::min<long>(groups, std::max<long>(1, p.tokens * groups / 16384));
     p.units = (groups + p.per - 1) / p.per;
 }
 long rows_wgs(const RowsParams& p) { return (p.tokens * p.units + NT / 64 - 1) / (NT / 64); }
@@ -3173,13 +3173,14 @@ template <typename IO, bool E4M3 = false>
 void launch_rows(RowsParams p, int d, hipStream_t st) {
     rows_split(p, p.H * (p.q != nullptr) + p.HKV * ((p.k != nullptr) + (p.v != nullptr)), d);
     const dim3 grid((unsigned)rows_wgs(p));
-    if (d == 128) hipLaunchKernelGGL((k_rows<IO, 128, E4M3>), grid, dim3(NT), 0, st, p);
-    else hipLaunchKernelGGL((k_rows<IO, 64, E4M3>), grid, dim3(NT), 0, st, p);
+    if (d == 128) hipLaunchKernelGGL((k_rows<IO, 128, E4M3, 2>), grid, dim3(NT), 0, st, p);
+    else hipLaunchKernelGGL((k_rows<IO, 64, E4M3, 2>), grid, dim3(NT), 0, st, p);
 }
 
 template <int DH, int IT>
 void launch_append_e4m3(const RowsParams& p, int row_wgs, long pages, int each, hipStream_t st) {
-    hipLaunchKernelGGL((k_append_e4m3<DH, IT>), dim3((unsigned)(row_wgs + pages * p.HKV * 2)), dim3(NT), 0, st, p, row_wgs, each);
+    hipLaunchKernelGGL((k_append_e4m3<DH, IT>), dim3((unsigned)(row_wgs + pages * p.HKV * 2)), dim3(NT), 0, st, p,
+                       (int)(pages * p.HKV * 2), each);
 }
 
 // How gdn_attention_paged cuts a step (pure host arithmetic, so that the workspace needs no device): see PagedParams.
@@ -3187,14 +3188,14 @@ struct PagedPlan {
     int rb;                      // rows per block
     long blocks, items;          // row blocks, and items, per key/value head at most
     int round, fine, spare;
-    int joins;                   // workgroups of k_attn_join per row block
+    int rows;                    // rows that a block can hold
 };
 PagedPlan paged_plan(int B, int T, int H, int H_kv, int page, int max_pages, int n_seqs) {
     const long G = H / H_kv;
     PagedPlan p = {};
     p.rb = T * G > 32L * std::max(n_seqs, 1) ? AQ : 16;
+    p.rows = (int)std::min<long>(T * G, p.rb);
     p.blocks = n_seqs > 0 ? (T * G) / p.rb + std::min<long>(n_seqs, T) : B * ((T * G + p.rb - 1) / p.rb);
-    p.joins = p.rb == 16 ? (int)std::min<long>(T * G, 16) : (int)(std::min<long>(T * G, AQ) + 15) / 16;
     const long units = ((long)page * max_pages + UNIT - 1) / UNIT;   // of a row block at most
     p.round = (int)std::max(1L, 2 * PLAN_CUS / H_kv);   // two workgroups per CU
     if (p.rb == 16) {
@@ -3211,6 +3212,11 @@ PagedPlan paged_plan(int B, int T, int H, int H_kv, int page, int max_pages, int
     if (p.spare == 0) p.items = p.blocks;
     return p;
 }
+Div make_div(uint32_t d) {
+    uint32_t s = 0;
+    while ((1u << s) < d) ++s;
+    return {(uint32_t)(((1ull << (31 + s)) + d - 1) / d), 31 + s};
+}
 struct PagedLayout { size_t po, total; };
 PagedLayout paged_layout(const PagedPlan& p, int H_kv, int d) {
     PagedLayout l = {0, 0};
@@ -3223,13 +3229,15 @@ PagedLayout paged_layout(const PagedPlan& p, int H_kv, int d) {
 
 template <int DH, typename CT>
 void launch_paged(const PagedParams& p, const PagedPlan& plan, hipStream_t st) {
-    const dim3 grid((unsigned)(p.items * p.HKV)), joins((unsigned)(plan.blocks * p.HKV * plan.joins));
-    if (plan.rb == 16) hipLaunchKernelGGL((k_attn_rows<DH, CT>), grid, dim3(NT), 0, st, p);
-    else hipLaunchKernelGGL((k_attn_tile<DH, CT, 1>), grid, dim3(NT_ATT), 0, st, p);
-    if (p.spare > 0) {
-        if (plan.rb == 16) hipLaunchKernelGGL((k_attn_join<DH, 16>), joins, dim3(NT), 0, st, p, plan.joins);
-        else hipLaunchKernelGGL((k_attn_join<DH, AQ>), joins, dim3(NT), 0, st, p, plan.joins);
+    const dim3 grid((unsigned)(p.items * p.HKV));
+    const long blocks = plan.blocks * p.HKV;
+    if (plan.rb == AQ) {
+        hipLaunchKernelGGL((k_attn_tile<DH, CT, 1>), grid, dim3(NT_ATT), 0, st, p);
+        if (p.spare > 0) hipLaunchKernelGGL((k_attn_join_tile<DH>), dim3((unsigned)blocks), dim3(NT_ATT), 0, st, p);
+        return;
     }
+    hipLaunchKernelGGL((k_attn_rows<DH, CT>), grid, dim3(NT), 0, st, p);
+    if (p.spare > 0) hipLaunchKernelGGL((k_attn_join<DH>), dim3((unsigned)blocks, (unsigned)plan.rows), dim3(NT), 0, st, p);
 }
 
 }  // namespace
@@ -3965,6 +3973,7 @@ extern "C" gdn_status gdn_attention_paged(const void* q, const void* k_cache, co
     p.q = static_cast<const bf16_t*>(q);
     p.o = static_cast<bf16_t*>(o);
     p.H = H; p.HKV = H_kv; p.G = H / H_kv;
+    p.by_hkv = make_div(H_kv); p.by_g = make_div(p.G);
     p.scale_log2 = scale * 1.4426950408889634f;
     p.s.cu = cu_seqlens; p.s.lens = seq_lens; p.s.n = n_seqs > 0 ? n_seqs : B; p.s.T = T;
     p.c = make_cache(k_cache, v_cache, k_scale, v_scale, block_table, page, n_pages, max_pages);

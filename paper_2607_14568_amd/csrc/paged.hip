@@ -79,12 +79,14 @@ struct Turn {
     float eps;
 };
 
-// cos and sin of pos * freq[i], the angle in float64 (a float32 product is off by 2^-24 of an angle of up to 10^5
-// radians), reduced there to within half a turn before it is rounded
+// cos and sin of pos * freq[i]: the angle in float64 (a float32 product is off by 2^-24 of an angle of up to 10^5 radians),
+// in turns, reduced to within half a turn and rounded (2^-26 turns, 2^-23.3 radians); the sine unit takes turns and is off by
+// up to 2^-22.9 there (measured over 2^20 angles; sincospif: 2^-24.3, at several times the instructions).
 __device__ __forceinline__ void angle(const Turn& t, int i, double pos, float& cs, float& sn) {
     double a = pos * t.freq[i] * 0.15915494309189535;
     a -= rint(a);
-    sincospif((float)(2 * a), &sn, &cs);
+    cs = __builtin_amdgcn_cosf((float)a);
+    sn = __builtin_amdgcn_sinf((float)a);
 }
 
 // cos and sin of the pairs of a chunk's 8 channels, from tables [rot / 2] of a position; the sign of the sine is that of the
@@ -136,17 +138,26 @@ __device__ __forceinline__ void turn_row(const Turn& t, const float* w, const fl
     }
 }
 
-template <typename IO> __device__ __forceinline__ void load8(const IO* p, float (&x)[8]) {
-    if constexpr (sizeof(IO) == 2) {
-        const short8 v = *reinterpret_cast<const short8*>(p);
+// 8 channels as they lie in memory
+template <typename IO> struct Chunk8;
+template <> struct Chunk8<bf16_t> {
+    short8 v;
+    __device__ __forceinline__ void load(const bf16_t* p) { v = *reinterpret_cast<const short8*>(p); }
+    __device__ __forceinline__ void zero() { v = short8{}; }
+    __device__ __forceinline__ void get(float (&x)[8]) const {
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = bf(v[e]);
-    } else {
-        const floatx4 a = f4(p), b = f4(p + 4);
+    }
+};
+template <> struct Chunk8<float> {
+    floatx4 a, b;
+    __device__ __forceinline__ void load(const float* p) { a = f4(p); b = f4(p + 4); }
+    __device__ __forceinline__ void zero() { a = b = floatx4{}; }
+    __device__ __forceinline__ void get(float (&x)[8]) const {
 #pragma unroll
         for (int e = 0; e < 4; ++e) { x[e] = a[e]; x[4 + e] = b[e]; }
     }
-}
+};
 template <typename IO> __device__ __forceinline__ void store8(IO* p, const float (&x)[8]) {
     const floatx4 a = {x[0], x[1], x[2], x[3]}, b = {x[4], x[5], x[6], x[7]};
     if constexpr (sizeof(IO) == 2) {
@@ -248,7 +259,7 @@ struct RowsParams {
 
 struct __attribute__((aligned(16))) AngleTable { float c[64], s[64]; };
 
-template <typename IO, int DH, bool E4M3>
+template <typename IO, int DH, bool E4M3, int AHEAD, bool QONLY = false>
 __device__ __forceinline__ void token_rows(const RowsParams& p, long wave, AngleTable& tab) {
     constexpr int LPR = DH / 8, RPG = 64 / LPR;
     const long tok = wave / p.units;
@@ -263,16 +274,29 @@ __device__ __forceinline__ void token_rows(const RowsParams& p, long wave, Angle
         __builtin_amdgcn_wave_barrier();   // (the wave's LDS accesses stay in order)
         angles(p.t, c, tab.c, tab.s, cs, sn);
     }
-    const int HQ = p.q ? p.H : 0, rows = HQ + (p.k ? p.HKV : 0) + (p.v ? p.HKV : 0);
-    const int id = p.k && !p.ko && pos >= 0 ? page_of(p.c, s, pos >> p.c.shift) : -1;
+    const int HQ = p.q ? p.H : 0, rows = QONLY ? p.H : HQ + p.HKV + (p.v ? p.HKV : 0);
+    const int id = !QONLY && !p.ko && pos >= 0 ? page_of(p.c, s, pos >> p.c.shift) : -1;
     const int slot = pos & (p.c.page - 1);
-    for (int g = 0; g < p.per; ++g) {
-        const int j = (unit * p.per + g) * RPG + lane / LPR;
-        const int kind = j < HQ ? 0 : j < HQ + p.HKV ? 1 : 2;   // q, k, v
+    // AHEAD groups' rows are loaded before the first is used
+    for (int g0 = 0; g0 < p.per; g0 += AHEAD) {
+    Chunk8<IO> in[AHEAD];
+#pragma unroll
+    for (int z = 0; z < AHEAD; ++z) {
+        const int j = (unit * p.per + g0 + z) * RPG + lane / LPR;
+        const IO* src = QONLY || j < HQ ? (const IO*)p.q + tok * p.qs + j * DH
+                        : j < HQ + p.HKV ? (const IO*)p.k + tok * p.ks + (j - HQ) * DH
+                                         : (const IO*)p.v + tok * p.vs + (j - HQ - p.HKV) * DH;
+        in[z].zero();
+        if (g0 + z < p.per && j < rows) in[z].load(src + 8 * c);
+    }
+#pragma unroll
+    for (int z = 0; z < AHEAD; ++z) {
+        const int j = (unit * p.per + g0 + z) * RPG + lane / LPR;
+        const int kind = QONLY || j < HQ ? 0 : j < HQ + p.HKV ? 1 : 2;   // q, k, v
         const int h = kind == 0 ? j : kind == 1 ? j - HQ : j - HQ - p.HKV;
-        const IO* src = kind == 0 ? (const IO*)p.q + tok * p.qs : kind == 1 ? (const IO*)p.k + tok * p.ks : (const IO*)p.v + tok * p.vs;
-        float x[8] = {};
-        if (j < rows) load8(src + h * DH + 8 * c, x);
+        if (g0 + z >= p.per) break;
+        float x[8];
+        in[z].get(x);
         // (a row's lanes share their kind, and the exchanges stay inside a row)
         if (kind < 2) turn_row<DH>(p.t, kind == 0 ? p.qw : p.kw, cs, sn, x);
         if (j >= rows) continue;
@@ -306,13 +330,14 @@ __device__ __forceinline__ void token_rows(const RowsParams& p, long wave, Angle
             }
         }
     }
+    }
 }
 
-template <typename IO, int DH, bool E4M3>
+template <typename IO, int DH, bool E4M3, int AHEAD>
 __global__ __launch_bounds__(NT) void k_rows(RowsParams p) {
     __shared__ AngleTable tab[NT / 64];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    token_rows<IO, DH, E4M3>(p, (long)blockIdx.x * (NT / 64) + wave, tab[wave]);
+    token_rows<IO, DH, E4M3, AHEAD>(p, (long)blockIdx.x * (NT / 64) + wave, tab[wave]);
 }
 
 // ------------------------------------------------------------------ k_append_e4m3
@@ -352,24 +377,22 @@ __device__ __forceinline__ bool touched_block(const StepSeqs& q, int shift, int 
     return false;
 }
 
-// One workgroup per (touched page, head, K or V), after `row_wgs` workgroups of the q rows.  It holds the page's new
+// One workgroup per (touched page, head, K or V), `page_wgs` in all, ahead of those of the q rows.  It holds the page's new
 // tokens in registers, finds their largest value, and writes codes and scale.  The angle of slot r = RPP it + i of the page
 // at position a is that of a + RPP it and that of i added up, a product of two table entries: (RPP + IT) rot / 2 sines
 // for RPP IT rows.
 template <int DH, int IT>   // IT: passes of NT / (DH / 8) rows over a page
-__global__ __launch_bounds__(NT) void k_append_e4m3(RowsParams p, int row_wgs, int each) {
+__global__ __launch_bounds__(NT) void k_append_e4m3(RowsParams p, int page_wgs, int each) {
     constexpr int LPR = DH / 8, RPP = NT / LPR, NP = DH / 2;
     __shared__ float red[NT / 64];
     __shared__ __align__(16) float tc[RPP + IT][NP], ts[RPP + IT][NP];   // of i, then of a + RPP it
     const int tid = threadIdx.x, c = tid % LPR, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    if ((int)blockIdx.x < row_wgs) {
+    if ((int)blockIdx.x >= page_wgs) {
         static_assert(sizeof(AngleTable) * (NT / 64) <= sizeof tc, "the tables of the q rows' waves");
-        RowsParams r = p;
-        r.k = r.v = nullptr;
-        token_rows<bf16_t, DH, false>(r, (long)blockIdx.x * (NT / 64) + wave, reinterpret_cast<AngleTable*>(tc)[wave]);
+        token_rows<bf16_t, DH, false, 2, true>(p, (long)((int)blockIdx.x - page_wgs) * (NT / 64) + wave, reinterpret_cast<AngleTable*>(tc)[wave]);
         return;
     }
-    const int u = (int)blockIdx.x - row_wgs;
+    const int u = (int)blockIdx.x;
     const int is_v = u & 1, h = u / 2 % p.HKV;
     int s, b, first, len, row;
     if (!touched_block(p.s, p.c.shift, each, u / 2 / p.HKV, s, b, first, len, row)) return;
@@ -379,14 +402,14 @@ __global__ __launch_bounds__(NT) void k_append_e4m3(RowsParams p, int row_wgs, i
     const int lo = max(first - at0, 0), hi = min(len - at0, p.c.page);   // its new slots
     const bf16_t* src = (const bf16_t*)(is_v ? p.v : p.k) + h * DH + 8 * c;
     const long stride = is_v ? p.vs : p.ks;
-    float x[IT][8], amax = 0.f;
+    Chunk8<bf16_t> in[IT];
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
         const int r = it * RPP + tid / LPR;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[it][e] = 0.f;
-        if (r >= lo && r < hi) load8(src + (row + (at0 + r - first)) * stride, x[it]);
+        in[it].zero();
+        if (r >= lo && r < hi) in[it].load(src + (row + (at0 + r - first)) * stride);
     }
+    float x[IT][8], amax = 0.f;
     if (!is_v) {
         const int np = p.t.rot / 2;
         for (int z = tid; z < (RPP + IT) * np; z += NT) {
@@ -398,6 +421,7 @@ __global__ __launch_bounds__(NT) void k_append_e4m3(RowsParams p, int row_wgs, i
         if (np) angles(p.t, c, tc[tid / LPR], ts[tid / LPR], cs, sn);
 #pragma unroll
         for (int it = 0; it < IT; ++it) {
+            in[it].get(x[it]);
             if (it * RPP >= hi || (it + 1) * RPP <= lo) continue;   // (the whole workgroup's)
             float ca[8], sa[8], ct[8], st[8];
             if (np) {
@@ -411,6 +435,9 @@ __global__ __launch_bounds__(NT) void k_append_e4m3(RowsParams p, int row_wgs, i
             }
             turn_row<DH>(p.t, p.kw, ct, st, x[it]);
         }
+    } else {
+#pragma unroll
+        for (int it = 0; it < IT; ++it) in[it].get(x[it]);
     }
 #pragma unroll
     for (int it = 0; it < IT; ++it)
@@ -451,15 +478,28 @@ __global__ __launch_bounds__(NT) void k_append_e4m3(RowsParams p, int row_wgs, i
 // The query rows of a sequence and key/value head, r = i G + g for new token i and the g-th of the head's G query heads, go
 // in blocks of RB.  A block's keys are cut into chunks of c units of UNIT keys, c from the step's lengths, which the host
 // does not know: the least with which all items, (row block, chunk) pairs, are resident at once (`round` of them per
-// key/value head); where that is more than `fine` units, max(fine, N / spare) with N the units of all row blocks, which
-// gives at most N / c + (row blocks) items.  So the long sequences of a batch are cut and the short ones are not.  A block of
+// key/value head); where that is more than `fine` units and the lengths leave a fifth of them idle, max(fine, N / spare) with
+// N the units of all row blocks, which gives at most N / c + (row blocks) items.  So the long sequences of a batch are cut and the short ones are not.  A block of
 // one chunk writes its output, one of several partial sums, which k_attn_join adds up in order.
 constexpr int UNIT = 128;
+
+// x / d for 0 <= x < 2^31 by one product: m = ceil(2^sh / d), sh = 31 + ceil(log2 d); m d - 2^sh < d <= 2^(sh - 31), so that x
+// times it stays below 2^sh.
+struct Div { uint32_t m, sh; };
+__device__ __forceinline__ int div_by(int x, Div d) { return (int)(((uint64_t)(uint32_t)x * d.m) >> d.sh); }
+// ceil(x / c) for 0 <= x < 2^24, 1 <= c: the quotient by a reciprocal is off by less than one
+__device__ __forceinline__ int ceil_div(int x, int c, float rc) {
+    int q = (int)((float)x * rc);
+    q += (long)q * c < x;
+    q += (long)q * c < x;
+    return q - ((long)(q - 1) * c >= x && q > 0);
+}
 
 struct PagedParams {
     const bf16_t* q;
     bf16_t* o;
     int H, HKV, G;
+    Div by_hkv, by_g;
     float scale_log2;
     int items;             // per key/value head (the grid)
     int round, fine, spare; // see above; spare 0: no cuts
@@ -472,13 +512,19 @@ struct PagedParams {
 struct Item {
     int s, tok, n, len;    // sequence, its first new token's row, new tokens, length with them
     int rb, nrb;           // row block, of how many
-    int c, chunk, first;   // keys per chunk; chunk of the item; item of the row block's chunk 0 (chunk j: first + j nrb)
+    int c, chunks, chunk, first;   // keys per chunk, chunks, chunk of the item; the sequence's first item (see item_of)
     int end;               // keys that the row block's last row sees
 };
 
+// Item of chunk j of the row block: chunk by chunk, even ones from the block with the most keys down, odd ones up, so that
+// two items a CU have about the same keys together.
+__device__ __forceinline__ int item_of(const Item& it, int j) {
+    return it.first + j * it.nrb + (j % 2 ? it.rb : it.nrb - 1 - it.rb);
+}
+
 // The keys that row block rb of a sequence sees: those of its last row.
 template <int RB> __device__ __forceinline__ int block_end(const PagedParams& p, int n, int len, int rb) {
-    const int i = min((rb * RB + RB - 1) / p.G, n - 1);
+    const int i = min(div_by(rb * RB + RB - 1, p.by_g), n - 1);
     return min(max(len - n + i + 1, 0), p.c.max_pages << p.c.shift);
 }
 
@@ -496,10 +542,11 @@ template <int RB, bool BLOCK = false> __device__ __forceinline__ bool find_item(
     if (p.spare > 0) {
         // the sum over the row blocks of ceil(units / c) (a lane's share held to 2^24: what matters is whether it is small)
         auto count = [&](int c) {
+            const float rc = 1.f / (float)c;
             int sum = 0, at = 0;
             for (int base = 0; base < p.s.n; base += 64) {
                 if (base > 0 || p.s.n > 64) load(base, at);
-                sum = (int)min((long)nrb * ((units + c - 1) / c) + sum, 1L << 24);
+                sum = (int)min((long)nrb * ceil_div(units, c, rc) + sum, 1L << 24);
             }
             return last_lane(scan_add(sum));
         };
@@ -514,8 +561,14 @@ template <int RB, bool BLOCK = false> __device__ __forceinline__ bool find_item(
         for (int off = 1; off < 64; off <<= 1) total += __shfl_xor(total, off, 64);
         total *= 1.f - 0x1p-19f;
         c = max((int)min(ceilf(total / (float)p.round), 0x1p23f), 1);
-        while (c <= p.fine && count(c) > p.round) c += (c + 7) / 8;
-        if (c > p.fine) c = max((int)min(ceilf(total * (1.f + 0x1p-17f) / (float)p.spare), 0x1p23f), p.fine);
+        auto uneven = [&](int c) { return c > p.fine && total < 0.8f * (float)c * (float)p.round; };
+        bool fits;
+        for (;;) {
+            fits = count(c) <= p.round;
+            if (fits || c >= 1 << 23 || uneven(c)) break;
+            c += (c + 7) / 8;
+        }
+        if (!fits || uneven(c)) c = max((int)min(ceilf(total * (1.f + 0x1p-17f) / (float)p.spare), 0x1p23f), p.fine);
         c = min(c, 1 << 23);
         c = __builtin_amdgcn_readfirstlane(c);
     }
@@ -523,7 +576,7 @@ template <int RB, bool BLOCK = false> __device__ __forceinline__ bool find_item(
     at = 0;
     for (int base = 0; base < p.s.n; base += 64) {
         if (base > 0 || p.spare == 0 || p.s.n > 64) load(base, at);
-        const int cnt = nrb * ((units + c - 1) / c);
+        const int cnt = nrb * ceil_div(units, c, 1.f / (float)c);
         const int si = scan_add(cnt), sb = BLOCK ? scan_add(nrb) : 0;
         const uint64_t past = __builtin_amdgcn_ballot_w64((BLOCK ? blocks + sb : items + si) > w);
         if (past) {
@@ -535,11 +588,22 @@ template <int RB, bool BLOCK = false> __device__ __forceinline__ bool find_item(
             it.nrb = __builtin_amdgcn_readlane(nrb, l);
             const int fi = items + __builtin_amdgcn_readlane(si - cnt, l);
             const int r = w - (BLOCK ? blocks + __builtin_amdgcn_readlane(sb - nrb, l) : fi);
-            it.rb = it.nrb - 1 - r % it.nrb;   // (blocks with the most keys first)
-            it.chunk = r / it.nrb;
-            it.first = fi + r % it.nrb;
-            it.c = c * UNIT;
+            int z = 0;
+            it.chunk = r;
+            if (it.nrb > 1) {
+                it.chunk = r / it.nrb;
+                z = r - it.chunk * it.nrb;
+            }
+            it.rb = it.chunk % 2 ? z : it.nrb - 1 - z;   // see item_of
+            it.first = fi;
             it.end = block_end<RB>(p, it.n, it.len, it.rb);
+            it.chunks = 1;
+            it.c = max(it.end, 1);
+            if (it.end > c * UNIT) {   // as many chunks as chunks of c units make, all of one size
+                it.chunks = (it.end + c * UNIT - 1) / (c * UNIT);
+                it.c = ((it.end + it.chunks - 1) / it.chunks + UNIT - 1) / UNIT * UNIT;
+                it.chunks = (it.end + it.c - 1) / it.c;
+            }
             return true;
         }
         items += last_lane(si);
@@ -565,15 +629,17 @@ template <bool SCALED> struct PageWalk {
             vs = p.c.vs[at];
         }
     }
-    __device__ __forceinline__ int page(const PagedParams& p, int hk, int b) {
-        if (b - first >= 64) load(p, hk, b);
-        return __builtin_amdgcn_readlane(id, b - first);
+    __device__ __forceinline__ void reach(const PagedParams& p, int hk, int b, int b_last) {   // up to 64 pages b .. b_last
+        if (b_last - first >= 64) load(p, hk, b);
     }
+    __device__ __forceinline__ int page(int b) const { return __builtin_amdgcn_readlane(id, b - first); }
+    __device__ __forceinline__ float kscale(int b) const { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, ks), b - first)); }
+    __device__ __forceinline__ float vscale(int b) const { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, vs), b - first)); }
 };
 
 // ------------------------------------------------------------------ k_attn_rows: few rows, many keys
 // Attention of blocks of up to 16 rows; bound by the cache's bytes.  A wave takes 32 keys a step, K and V from memory
-// straight into its registers, one step ahead of their use, without LDS or barriers; the workgroup's four waves take the
+// straight into its registers, 16 KB of steps ahead of their use, without LDS or barriers; the workgroup's waves take the
 // chunk's steps in turn and add up at the end.
 //   S^T = K Q^T: the A operand's row 4 a + b of 16-key half t is key 16 t + 4 b + a, so that a lane's results st[t][e] are
 // keys 16 t + 4 e + lg of query l16.
@@ -594,25 +660,96 @@ __device__ __forceinline__ int fp8_pair(int src, bool high) {   // two e4m3 code
     return __builtin_bit_cast(int, r);
 }
 
+// One row over keys k0 .. k1 - 1 by one wave without the matrix units: 64 / (DH / 8) keys at a time, each over DH / 8 lanes,
+// with a running softmax for each place among them.  o: this lane's 8 channels, the same in all places; m, l of the row.
+template <int DH, typename CT>
+__device__ __forceinline__ void plain_row(const PagedParams& p, const Item& it, int hk, int row, int k0, int k1, float& m, float& l,
+                                          float (&o)[8]) {
+    constexpr int LPR = DH / 8, KPI = 64 / LPR;
+    const int lane = threadIdx.x & 63, c = lane % LPR, qi = div_by(row, p.by_g);
+    const int last = it.len - it.n + qi;
+    float q[8];
+    Chunk8<bf16_t> y;
+    y.load(p.q + ((long)(it.tok + qi) * p.H + hk * p.G + row - qi * p.G) * DH + 8 * c);
+    y.get(q);
+    m = LOWEST;
+    l = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = 0.f;
+#pragma unroll 1
+    for (int j = k0 + lane / LPR; j - lane / LPR <= min(last, k1 - 1); j += KPI) {
+        const int id = j <= min(last, k1 - 1) ? page_of(p.c, it.s, j >> p.c.shift) : -1;
+        float dot = 0.f, v[8] = {}, ks = 1.f, vs = 1.f;
+        if (id >= 0) {
+            const long at = ((((long)id * p.HKV + hk) << p.c.shift) + (j & (p.c.page - 1))) * DH + 8 * c;
+            float k[8];
+            if constexpr (sizeof(CT) == 2) {
+                y.load((const bf16_t*)p.c.k + at);
+                y.get(k);
+                y.load((const bf16_t*)p.c.v + at);
+                y.get(v);
+            } else {
+                from_e4m3(*(const uint64_t*)((const uint8_t*)p.c.k + at), k);
+                from_e4m3(*(const uint64_t*)((const uint8_t*)p.c.v + at), v);
+                ks = p.c.ks[(long)id * p.HKV + hk];
+                vs = p.c.vs[(long)id * p.HKV + hk];
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dot += q[e] * k[e];
+        }
+#pragma unroll
+        for (int off = 1; off < LPR; off <<= 1) dot += __shfl_xor(dot, off, 64);
+        const float x = id >= 0 ? dot * (ks * p.scale_log2) : -INFINITY;
+        const float mn = fmaxf(m, x), a = __builtin_amdgcn_exp2f(m - mn), w = __builtin_amdgcn_exp2f(x - mn);
+        m = mn;
+        l = l * a + w;
+        if (id >= 0) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = o[e] * a + w * vs * v[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] *= a;
+        }
+    }
+    float M = m;
+#pragma unroll
+    for (int off = LPR; off < 64; off <<= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
+    const float a = __builtin_amdgcn_exp2f(m - M);
+    m = M;
+    l *= a;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] *= a;
+#pragma unroll
+    for (int off = LPR; off < 64; off <<= 1) {
+        l += __shfl_xor(l, off, 64);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] += __shfl_xor(o[e], off, 64);
+    }
+}
+
 template <int DH, typename CT>
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_attn_rows(PagedParams p) {
     constexpr int NW = NT / 64, RB = 16, CW = DH / 16, ESZ = sizeof(CT), NKB = DH / 32, NK = DH * ESZ / 64, VD = CW * ESZ / 4;
     constexpr bool E4M3 = ESZ == 1;
-    __shared__ float lds_o[NW][RB][DH];
+    __shared__ __align__(16) float lds_o[NW][RB][DH + 4];   // (rows 4 banks apart: 16 rows' 16-byte accesses meet no bank twice)
     __shared__ float2 lds_ml[NW][RB];
+    __shared__ int redo;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, lg = lane >> 4;
-    const int hk = (int)(blockIdx.x % p.HKV);
+    const int w = div_by(blockIdx.x, p.by_hkv), hk = (int)blockIdx.x - w * p.HKV;
     Item it;
-    if (!find_item<RB>(p, (int)(blockIdx.x / p.HKV), it)) return;
+    if (!find_item<RB>(p, w, it) || it.chunk >= it.chunks) return;
     const int k0 = it.chunk * it.c, k1 = min(it.end - k0, it.c) + k0;   // the item's keys
-    if (it.chunk > 0 && k0 >= it.end) return;
     const int rows = min(it.n * p.G - it.rb * RB, RB);
-    const int row = it.rb * RB + l16, qi = row / p.G, h = hk * p.G + row % p.G;
-    const int last = it.len - it.n + qi, last0 = it.len - it.n + it.rb * RB / p.G;   // this lane's row, and the block's first
+    const int row = it.rb * RB + l16, qi = div_by(row, p.by_g);
+    const int last = it.len - it.n + qi, last0 = it.len - it.n + div_by(it.rb * RB, p.by_g);   // this lane's row, and the block's first
+    PageWalk<E4M3> walk;
+    walk.row = p.c.table + (long)it.s * p.c.max_pages;
+    const int start = k0 + 32 * wave;
+    if (start < k1) walk.load(p, hk, start >> p.c.shift);
     bf16x8 qf[NKB] = {};
     if (l16 < rows) {
-        const bf16_t* src = p.q + ((long)(it.tok + qi) * p.H + h) * DH;
+        const bf16_t* src = p.q + ((long)(it.tok + qi) * p.H + hk * p.G + row - qi * p.G) * DH;
 #pragma unroll
         for (int kb = 0; kb < NKB; ++kb)
             qf[kb] = *reinterpret_cast<const bf16x8*>(src + (E4M3 ? 64 * (kb / 2) + 16 * lg + 8 * (kb % 2) : 32 * kb + 8 * lg));
@@ -624,18 +761,16 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
     const int koff = (4 * (l16 & 3) + (l16 >> 2)) * DH * ESZ + 16 * lg, voff = lg * DH * ESZ + l16 * CW * ESZ;
 
     typedef RowsStep<DH, CT> Step;
-    PageWalk<E4M3> walk;
-    walk.row = p.c.table + (long)it.s * p.c.max_pages;
-    if (k1 > k0) walk.load(p, hk, (k0 + 32 * wave) >> p.c.shift);
     auto load = [&](Step& x, int kb) {
+        walk.reach(p, hk, kb >> p.c.shift, (kb + 16) >> p.c.shift);
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const int key = kb + 16 * t, b = key >> p.c.shift;
-            const int id = key < k1 ? walk.page(p, hk, b) : -1;
+            const int id = key < k1 ? walk.page(b) : -1;
             x.there[t] = id >= 0;
             if constexpr (E4M3) {
-                x.ks[t] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, walk.ks), b - walk.first));
-                x.vs[t] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, walk.vs), b - walk.first));
+                x.ks[t] = walk.kscale(b);
+                x.vs[t] = walk.vscale(b);
             }
             const long at = ((((long)max(id, 0) * p.HKV + hk) << p.c.shift) + (key & (p.c.page - 1))) * DH * ESZ;
             const uint32_t bytes = id >= 0 ? (uint32_t)min(k1 - key, 16) * DH * ESZ : 0;   // rows past the item's read as zeros
@@ -676,8 +811,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
             }
             st[t] *= E4M3 ? x.ks[t] * p.scale_log2 : p.scale_log2;
         }
-        const bool masked = kb + 31 > last0 || kb + 32 > k1 || !x.there[0] || !x.there[1];
-        if (masked) {
+        if (kb + 31 > last0 || kb + 32 > k1 || !x.there[0] || !x.there[1]) {   // some key is masked for some row
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -698,64 +832,22 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
             l *= a;
             m = mn;
         }
-        floatx4 w[2];
+        floatx4 wt[2];
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < 2; ++t) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                w[t][e] = __builtin_amdgcn_exp2f(st[t][e] - m);
-                l += w[t][e];
+                wt[t][e] = __builtin_amdgcn_exp2f(st[t][e] - m);
+                l += wt[t][e];
             }
+            if constexpr (E4M3) wt[t] *= x.vs[t];
+        }
+        const bf16x8 pf = pack_bf16(wt[0], wt[1]);
         int vb[8][CW / 2];   // bf16 pairs of channels
 #pragma unroll
         for (int j = 0; j < 8; ++j)
 #pragma unroll
             for (int i = 0; i < CW / 2; ++i) vb[j][i] = E4M3 ? fp8_pair(x.v[j][i / 2], i % 2) : x.v[j][E4M3 ? 0 : i];
-        if (masked && it.n > 1) {
-            // A weight of 0 does not hide a value that is not finite (0 x NaN): such values of keys that some rows do not
-            // see are taken out here and made NaN in the rows that do.
-            bool odd = false;
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-#pragma unroll
-                for (int i = 0; i < CW / 2; ++i)
-                    odd = odd || (vb[j][i] & 0x7f800000) == 0x7f800000 || (vb[j][i] & 0x7f80) == 0x7f80;
-            if (__builtin_amdgcn_ballot_w64(odd)) {
-                floatx4 seen[2];
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) seen[t][e] = st[t][e] == -INFINITY ? 0.f : 1.f;
-                const bf16x8 sf = pack_bf16(seen[0], seen[1]);
-#pragma unroll
-                for (int n = 0; n < CW; ++n) {
-                    int bad[4];
-#pragma unroll
-                    for (int jj = 0; jj < 4; ++jj) {
-                        bad[jj] = 0;
-#pragma unroll
-                        for (int z = 0; z < 2; ++z) {
-                            const int sh = 16 * (n % 2);
-                            int& d = vb[2 * jj + z][n / 2];
-                            if (((d >> sh) & 0x7f80) == 0x7f80) {
-                                d &= ~(0xffff << sh);
-                                bad[jj] |= 0x3f80 << (16 * z);
-                            }
-                        }
-                    }
-                    const floatx4 hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                        __builtin_bit_cast(bf16x8, int4v{bad[0], bad[1], bad[2], bad[3]}), sf, floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (hit[e] != 0.f) acc[n][e] = __uint_as_float(0x7fc00000u);
-                }
-            }
-        }
-        if constexpr (E4M3) {
-            w[0] *= x.vs[0];
-            w[1] *= x.vs[1];
-        }
-        const bf16x8 pf = pack_bf16(w[0], w[1]);
 #pragma unroll
         for (int n = 0; n < CW; ++n) {
             int4v va;
@@ -765,55 +857,79 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
             acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va), pf, acc[n], 0, 0, 0);
         }
     };
-    // DEPTH steps' loads are in flight: 16 KB a wave
+    // DEPTH - 1 steps' loads are in flight while one is used
     constexpr int DEPTH = 256 / (DH * ESZ) + 1, NEXT = 32 * NW;
     Step ring[DEPTH];
-#pragma unroll
-    for (int z = 0; z < DEPTH - 1; ++z)
-        if (k0 + 32 * wave + NEXT * z < k1) load(ring[z], k0 + 32 * wave + NEXT * z);
-    for (int kb = k0 + 32 * wave; kb < k1; kb += NEXT * DEPTH) {
+    for (int kb = start - (DEPTH - 1) * NEXT; kb < k1; kb += NEXT * DEPTH) {
 #pragma unroll
         for (int z = 0; z < DEPTH; ++z) {
-            const int at = kb + NEXT * z;
-            if (at >= k1) break;
-            if (at + NEXT * (DEPTH - 1) < k1) load(ring[(z + DEPTH - 1) % DEPTH], at + NEXT * (DEPTH - 1));
-            compute(ring[z], at);
+            const int at = kb + NEXT * z, ahead = at + NEXT * (DEPTH - 1);
+            if (ahead < k1) load(ring[(z + DEPTH - 1) % DEPTH], ahead);
+            if (at >= start && at < k1) compute(ring[z], at);
         }
     }
-    // the four waves' sums: acc[n][e] is channel CW (4 lg + e) + n of query l16
+    // the waves' sums: acc[n][e] is channel CW (4 lg + e) + n of query l16
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
-    if (lg == 0) lds_ml[wave][l16] = float2{m, l};
+    if (l16 < rows) {
+        if (lg == 0) lds_ml[wave][l16] = float2{m, l};
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
+        for (int e = 0; e < 4; ++e)
 #pragma unroll
-        for (int n = 0; n < CW; ++n) lds_o[wave][l16][CW * (4 * lg + e) + n] = acc[n][e];
+            for (int n = 0; n < CW; n += 4)
+                *reinterpret_cast<floatx4*>(&lds_o[wave][l16][CW * (4 * lg + e) + n]) = floatx4{acc[n][e], acc[n + 1][e], acc[n + 2][e], acc[n + 3][e]};
+    }
+    if (k1 - 1 > last0) {
+        // Some rows do not see some of the item's keys, but their weight of 0 does not hide a value that is not finite (0 x NaN):
+        // where that left a sum that is not finite, the rows are done again without the matrix units.
+        if (tid == 0) redo = 0;
+        __syncthreads();
+        float sum = 0.f;
+#pragma unroll
+        for (int n = 0; n < CW; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum += 0.f * acc[n][e];
+        if (l16 < rows && sum != 0.f) redo = 1;   // (0, or NaN)
+        __syncthreads();
+        if (redo) {
+#pragma unroll 1
+            for (int r = wave; r < rows; r += NW) {
+                float o[8];
+                plain_row<DH, CT>(p, it, hk, it.rb * RB + r, k0, k1, m, l, o);
+                if (lane < NW) lds_ml[lane][r] = lane == 0 ? float2{m, l} : float2{LOWEST, 0.f};
+                if (lane < DH / 8)
+#pragma unroll
+                    for (int z = 0; z < NW; ++z)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) lds_o[z][r][8 * lane + e] = z == 0 ? o[e] : 0.f;
+            }
+        }
+    }
     __syncthreads();
     const int r = tid / 16, c0 = (tid % 16) * CW;
     if (r >= rows) return;
-    float M = LOWEST, wt[NW], sum = 0.f, o[CW] = {};
+    float M = LOWEST, sum = 0.f;
+    floatx4 o[CW / 4] = {};
 #pragma unroll
-    for (int w = 0; w < NW; ++w) M = fmaxf(M, lds_ml[w][r].x);
+    for (int z = 0; z < NW; ++z) M = fmaxf(M, lds_ml[z][r].x);
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
-        wt[w] = __builtin_amdgcn_exp2f(lds_ml[w][r].x - M);
-        sum += wt[w] * lds_ml[w][r].y;
+    for (int z = 0; z < NW; ++z) {
+        const float a = __builtin_amdgcn_exp2f(lds_ml[z][r].x - M);
+        sum += a * lds_ml[z][r].y;
 #pragma unroll
-        for (int n = 0; n < CW; ++n) o[n] += wt[w] * lds_o[w][r][c0 + n];
+        for (int n = 0; n < CW / 4; ++n) o[n] += a * f4(&lds_o[z][r][c0 + 4 * n]);
     }
-    if (it.end <= it.c) {   // the only chunk
+    if (it.chunks == 1) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;   // no key: zeros
-        const int rr = it.rb * RB + r;
-        bf16_t* dst = p.o + ((long)(it.tok + rr / p.G) * p.H + hk * p.G + rr % p.G) * DH + c0;
+        const int rr = it.rb * RB + r, i = div_by(rr, p.by_g);
+        bf16_t* dst = p.o + ((long)(it.tok + i) * p.H + hk * p.G + rr - i * p.G) * DH + c0;
 #pragma unroll
-        for (int n = 0; n < CW; n += 4)
-            *reinterpret_cast<bf16x4*>(dst + n) =
-                __builtin_convertvector((floatx4{o[n] * inv, o[n + 1] * inv, o[n + 2] * inv, o[n + 3] * inv}), bf16x4);
+        for (int n = 0; n < CW / 4; ++n) *reinterpret_cast<bf16x4*>(dst + 4 * n) = __builtin_convertvector(o[n] * inv, bf16x4);
     } else {
         const long slot = (long)blockIdx.x * RB + r;
         if (c0 == 0) p.pml[slot] = float2{M, sum};
 #pragma unroll
-        for (int n = 0; n < CW; n += 4) *reinterpret_cast<floatx4*>(p.po + slot * DH + c0 + n) = floatx4{o[n], o[n + 1], o[n + 2], o[n + 3]};
+        for (int n = 0; n < CW / 4; ++n) *reinterpret_cast<floatx4*>(p.po + slot * DH + c0 + 4 * n) = o[n];
     }
 }
 
@@ -830,27 +946,27 @@ __global__ __launch_bounds__(NT_ATT / QT) __attribute__((amdgpu_waves_per_eu(4 /
     __shared__ int odd;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, lg = lane >> 4;
-    const int hk = (int)(blockIdx.x % p.HKV);
+    const int w = div_by(blockIdx.x, p.by_hkv), hk = (int)blockIdx.x - w * p.HKV;
     Item it;
-    if (!find_item<RB>(p, (int)(blockIdx.x / p.HKV), it)) return;
+    if (!find_item<RB>(p, w, it) || it.chunk >= it.chunks) return;
     const int k0 = it.chunk * it.c, k1 = min(it.end - k0, it.c) + k0;
-    if (it.chunk > 0 && k0 >= it.end) return;
     const int rows = it.n * p.G, base = it.len - it.n;   // rows of the sequence; position of its first new token
     const int r0 = it.rb * RB + 16 * QT * wave;          // this wave's first row
-    const int wlast = r0 < rows ? base + min(r0 + 16 * QT - 1, rows - 1) / p.G : -1;   // the last key that its rows see
+    const int wlast = r0 < rows ? base + div_by(min(r0 + 16 * QT - 1, rows - 1), p.by_g) : -1;   // the last key that its rows see
     auto swz = [](int r) {
         return NCH == 16 ? (4 * (r & 3)) | (2 * ((r >> 2) & 1)) | ((r >> 3) & 1)
                          : (4 * ((r >> 1) & 1)) | (2 * ((r >> 2) & 1)) | ((r >> 3) & 1);
     };
     auto kq = [swz](int r, int cc) { return r * DH + (((cc >> 3) ^ swz(r)) << 3) + (cc & 7); };
 
-    int last[QT];   // of this lane's rows
+    int last[QT], first[QT];   // the last keys of this lane's rows, and of a tile's first row
     bf16x8 qf[QT][NKB];
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
-        const int r = r0 + 16 * u + l16, qi = r / p.G;
+        const int r = r0 + 16 * u + l16, qi = div_by(r, p.by_g);
         last[u] = base + qi;
-        const bf16_t* src = p.q + ((long)(it.tok + qi) * p.H + hk * p.G + r % p.G) * DH;
+        first[u] = base + div_by(r0 + 16 * u, p.by_g);
+        const bf16_t* src = p.q + ((long)(it.tok + qi) * p.H + hk * p.G + r - qi * p.G) * DH;
 #pragma unroll
         for (int kb = 0; kb < NKB; ++kb) {
             qf[u][kb] = bf16x8{};
@@ -864,14 +980,14 @@ __global__ __launch_bounds__(NT_ATT / QT) __attribute__((amdgpu_waves_per_eu(4 /
     struct Block { int there; float ks[E4M3 ? 4 : 1], vs[E4M3 ? 4 : 1]; } cur, nxt;   // there: bit t, the page of keys 16 t ..
     auto look = [&](Block& x, int kb) {
         x.there = 0;
+        walk.reach(p, hk, kb >> p.c.shift, (kb + AKB - 1) >> p.c.shift);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             const int key = kb + 16 * t, b = key >> p.c.shift;
-            const int id = key < k1 ? walk.page(p, hk, b) : -1;
-            x.there |= (id >= 0) << t;
+            x.there |= (key < k1 && walk.page(b) >= 0) << t;
             if constexpr (E4M3) {
-                x.ks[t] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, walk.ks), b - walk.first));
-                x.vs[t] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, walk.vs), b - walk.first));
+                x.ks[t] = walk.kscale(b);
+                x.vs[t] = walk.vscale(b);
             }
         }
     };
@@ -879,7 +995,7 @@ __global__ __launch_bounds__(NT_ATT / QT) __attribute__((amdgpu_waves_per_eu(4 /
     // holds it, else of the 16 rows around row r.  Rows past the item's keys, and of pages that are not there, read as zeros.
     auto describe = [&](int kb, int r, __amdgpu_buffer_rsrc_t& rk, __amdgpu_buffer_rsrc_t& rv) {
         const int g = p.c.page >= AKB ? 0 : r & ~15, span = p.c.page >= AKB ? AKB : 16, key = kb + g;
-        const int id = key < k1 ? walk.page(p, hk, key >> p.c.shift) : -1;
+        const int id = key < k1 ? walk.page(key >> p.c.shift) : -1;
         const long at = (((((long)max(id, 0) * p.HKV + hk) << p.c.shift) + (key & (p.c.page - 1))) - g) * DH * ESZ;
         const uint32_t bytes = id >= 0 ? (uint32_t)(g + min(k1 - key, span)) * DH * ESZ : 0;
         rk = rsrc((const char*)p.c.k + at, bytes);
@@ -949,7 +1065,7 @@ __global__ __launch_bounds__(NT_ATT / QT) __attribute__((amdgpu_waves_per_eu(4 /
     }
     // A weight of 0 does not hide a value that is not finite (0 x NaN).  In the blocks from `part` on, where some rows do not
     // see a key that others see, such values are taken out, and the rows that see them are made NaN at the end.
-    const int all = base + it.rb * RB / p.G;   // the last key that every row sees
+    const int all = base + div_by(it.rb * RB, p.by_g);   // the last key that every row sees
     const int part = all < k0 ? k0 : k0 + (all + 1 - k0) / AKB * AKB;
     if (tid == 0) odd = 0;
     auto block = [&](const int kb, auto SLOT) {
@@ -1000,7 +1116,7 @@ __global__ __launch_bounds__(NT_ATT / QT) __attribute__((amdgpu_waves_per_eu(4 /
             bf16x8 pf[QT][2];
 #pragma unroll
             for (int u = 0; u < QT; ++u) {
-                const bool diag = !whole || kb + AKB - 1 > base + (r0 + 16 * u) / p.G;   // some key is masked for this tile
+                const bool diag = !whole || kb + AKB - 1 > first[u];   // some key is masked for this tile
                 if constexpr (E4M3) {
 #pragma unroll
                     for (int t = 0; t < 4; ++t) st[u][t] *= cur.ks[t];
@@ -1095,9 +1211,10 @@ __global__ __launch_bounds__(NT_ATT / QT) __attribute__((amdgpu_waves_per_eu(4 /
         l[u] += __shfl_xor(l[u], 32, 64);
         const int r = r0 + 16 * u + l16;
         if (r >= rows) continue;
-        if (it.end <= it.c) {   // the only chunk
+        if (it.chunks == 1) {
             const float inv = l[u] == 0.f ? 0.f : 1.f / l[u];   // no key: zeros
-            bf16_t* dst = p.o + ((long)(it.tok + r / p.G) * p.H + hk * p.G + r % p.G) * DH + 4 * lg;
+            const int i = div_by(r, p.by_g);
+            bf16_t* dst = p.o + ((long)(it.tok + i) * p.H + hk * p.G + r - i * p.G) * DH + 4 * lg;
 #pragma unroll
             for (int t = 0; t < NDT; ++t) *reinterpret_cast<bf16x4*>(dst + 16 * t) = __builtin_convertvector(oacc[u][t] * inv, bf16x4);
         } else {
@@ -1111,56 +1228,96 @@ __global__ __launch_bounds__(NT_ATT / QT) __attribute__((amdgpu_waves_per_eu(4 /
 
 // ------------------------------------------------------------------ k_attn_join
 // The sum of a row's chunks' partial sums, over loads of 4 channels a lane, lanes and waves in a fixed order (so that the
-// result does not depend on which chunk ended first).  Rows of 16-row blocks may have many chunks: a workgroup a row, its
-// waves sharing them.  Those of 128-row blocks have few: a wave a row, 16 rows a workgroup.
-template <int DH, int RB>
-__global__ __launch_bounds__(NT) void k_attn_join(PagedParams p, int groups) {   // workgroups per row block
-    constexpr int LPR = DH / 4, SUB = 64 / LPR, NW = NT / 64;   // lanes per row; chunks that a wave's load takes at once
-    constexpr int ROWS = RB == 16 ? 1 : 16, SHARE = RB == 16 ? NW : 1;   // rows per workgroup, waves per row
-    __shared__ float red[NW][DH];
+// result does not depend on which chunk ended first).  (The last workgroup of a block adding up at its end, found by flags
+// stored past the caches, was slower: 64 sequences e4m3 81 us against 78, 16 sequences' 4 tokens 38 against 23.)
+// Blocks of 16 rows may have many chunks: a workgroup a row (blockIdx.y), its waves sharing
+// them.
+template <int DH>
+__global__ __launch_bounds__(NT) void k_attn_join(PagedParams p) {
+    constexpr int RB = 16, LPR = DH / 4, SUB = 64 / LPR, NW = NT / 64;   // lanes per row; chunks that a wave's load takes at once
+    __shared__ __align__(16) float red[NW][DH];
     __shared__ float reds[NW];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int u = blockIdx.x / groups, hk = u % p.HKV, c4 = 4 * (lane % LPR);
+    const int w = div_by(blockIdx.x, p.by_hkv), hk = (int)blockIdx.x - w * p.HKV, c4 = 4 * (lane % LPR), r = blockIdx.y;
     Item it;
-    if (!find_item<RB, true>(p, u / p.HKV, it) || it.end <= it.c) return;
-    const int chunks = (it.end + it.c - 1) / it.c;
-    for (int i = SHARE == 1 ? wave : 0; i < ROWS; i += NW) {
-        const int r = (int)(blockIdx.x % groups) * ROWS + i, rr = it.rb * RB + r;
-        if (rr >= it.n * p.G) return;
-        auto slot = [&](int j) { return ((long)(it.first + j * it.nrb) * p.HKV + hk) * RB + r; };
-        float M = LOWEST, sum = 0.f;
-        for (int j0 = 0; j0 < chunks; j0 += 64) M = fmaxf(M, j0 + lane < chunks ? p.pml[slot(j0 + lane)].x : LOWEST);
+    if (!find_item<RB, true>(p, w, it) || it.chunks == 1) return;
+    const int rr = it.rb * RB + r, chunks = it.chunks;
+    if (rr >= it.n * p.G) return;
+    auto slot = [&](int j) { return ((long)item_of(it, j) * p.HKV + hk) * RB + r; };
+    float M = LOWEST, sum = 0.f;
+    for (int j0 = 0; j0 < chunks; j0 += 64) M = fmaxf(M, j0 + lane < chunks ? p.pml[slot(j0 + lane)].x : LOWEST);
 #pragma unroll
-        for (int off = 1; off < 64; off <<= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
-        floatx4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-        for (int j = (SHARE == 1 ? 0 : wave * SUB) + lane / LPR; j < chunks; j += SHARE * SUB) {
-            const float2 ml = p.pml[slot(j)];
-            const float w = __builtin_amdgcn_exp2f(ml.x - M);
-            sum += w * ml.y;
-            o += w * f4(p.po + slot(j) * DH + c4);
-        }
+    for (int off = 1; off < 64; off <<= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
+    floatx4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int j = wave * SUB + lane / LPR; j < chunks; j += NW * SUB) {
+        const float2 ml = p.pml[slot(j)];
+        const float w = __builtin_amdgcn_exp2f(ml.x - M);
+        sum += w * ml.y;
+        o += w * f4(p.po + slot(j) * DH + c4);
+    }
 #pragma unroll
-        for (int off = LPR; off < 64; off <<= 1) {
-            sum += __shfl_xor(sum, off, 64);
+    for (int off = LPR; off < 64; off <<= 1) {
+        sum += __shfl_xor(sum, off, 64);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], off, 64);
-        }
-        if constexpr (SHARE > 1) {
-            if (lane < LPR) *reinterpret_cast<floatx4*>(&red[wave][c4]) = o;
-            if (lane == 0) reds[wave] = sum;
-            __syncthreads();
-            if (wave != 0) return;
-            sum = reds[0];
-            o = f4(&red[0][c4]);
+        for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], off, 64);
+    }
+    if (lane < LPR) *reinterpret_cast<floatx4*>(&red[wave][c4]) = o;
+    if (lane == 0) reds[wave] = sum;
+    __syncthreads();
+    if (wave != 0 || lane >= LPR) return;
+    sum = reds[0];
+    o = f4(&red[0][c4]);
 #pragma unroll
-            for (int w = 1; w < NW; ++w) {
-                sum += reds[w];
-                o += f4(&red[w][c4]);
+    for (int w = 1; w < NW; ++w) {
+        sum += reds[w];
+        o += f4(&red[w][c4]);
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const int i = div_by(rr, p.by_g);
+    bf16_t* dst = p.o + ((long)(it.tok + i) * p.H + hk * p.G + rr - i * p.G) * DH + c4;
+    *reinterpret_cast<bf16x4*>(dst) = __builtin_convertvector(o * inv, bf16x4);
+}
+
+// Blocks of 128 rows have few chunks, mostly two: DH / 4 lanes a row, all of a workgroup's rows loaded at once.
+template <int DH>
+__global__ __launch_bounds__(NT_ATT) void k_attn_join_tile(PagedParams p) {
+    constexpr int RB = AQ, LPR = DH / 4, NG = NT_ATT / LPR, PASS = RB / NG;
+    const int g = threadIdx.x / LPR, c4 = 4 * (threadIdx.x % LPR);
+    const int w = div_by(blockIdx.x, p.by_hkv), hk = (int)blockIdx.x - w * p.HKV;
+    Item it;
+    if (!find_item<RB, true>(p, w, it) || it.chunks == 1) return;
+    const int rows = min(it.n * p.G - it.rb * RB, RB), chunks = it.chunks;
+    float m[PASS], sum[PASS];
+    floatx4 o[PASS];
+#pragma unroll
+    for (int i = 0; i < PASS; ++i) {
+        m[i] = LOWEST;
+        sum[i] = 0.f;
+        o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    for (int j = 0; j < chunks; ++j) {
+        const long slot = ((long)item_of(it, j) * p.HKV + hk) * RB;
+#pragma unroll
+        for (int i = 0; i < PASS; ++i) {
+            const int r = g + i * NG;
+            if (r < rows) {
+                const float2 ml = p.pml[slot + r];
+                const floatx4 y = f4(p.po + (slot + r) * DH + c4);
+                const float M = fmaxf(m[i], ml.x), a = __builtin_amdgcn_exp2f(m[i] - M), w = __builtin_amdgcn_exp2f(ml.x - M);
+                sum[i] = sum[i] * a + w * ml.y;
+                o[i] = o[i] * a + w * y;
+                m[i] = M;
             }
         }
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        bf16_t* dst = p.o + ((long)(it.tok + rr / p.G) * p.H + hk * p.G + rr % p.G) * DH + c4;
-        if (lane < LPR) *reinterpret_cast<bf16x4*>(dst) = __builtin_convertvector(o * inv, bf16x4);
+    }
+#pragma unroll
+    for (int i = 0; i < PASS; ++i) {
+        const int r = g + i * NG, rr = it.rb * RB + r;
+        if (r >= rows) break;
+        const float inv = sum[i] == 0.f ? 0.f : 1.f / sum[i];
+        const int qi = div_by(rr, p.by_g);
+        bf16_t* dst = p.o + ((long)(it.tok + qi) * p.H + hk * p.G + rr - qi * p.G) * DH + c4;
+        *reinterpret_cast<bf16x4*>(dst) = __builtin_convertvector(o[i] * inv, bf16x4);
     }
 }
