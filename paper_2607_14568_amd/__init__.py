@@ -406,18 +406,34 @@ def gdn_attention_prefill(q, k, v, *, scale=None, cu_seqlens=None, o=None):
     return o
 
 
-def _same(dev, *tensors):
-    """Each (tensor or None, name, dtype): contiguous, of that type, on device number ``dev``."""
-    for t, name, dtype in tensors:
-        if t is None:
-            continue
-        if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
-            _dev(t, name, dtype)
-            raise ValueError("%s is on %s, the call's first tensor on device %d" % (name, t.device, dev))
+# The serving operators are called once or twice a layer and token, where a microsecond counts: one pass over a call's
+# tensors checks them and takes their addresses, and what is wrong is only looked for once something is.
+_BF16, _F32, _F64, _I32 = torch.bfloat16, torch.float32, torch.float64, torch.int32
+
+
+def _addresses(dev, tensors, names, dtypes):
+    """The addresses (None for None) of contiguous tensors of these types on device number ``dev``."""
+    out = []
+    try:
+        for t, dtype in zip(tensors, dtypes):
+            if t is None:
+                out.append(None)
+            elif t.dtype is dtype and t.get_device() == dev and t.is_contiguous():
+                out.append(t.data_ptr())
+            else:
+                break
+        else:
+            return out
+    except AttributeError:   # no tensor
+        pass
+    name, dtype = names[len(out)], dtypes[len(out)]
+    t = _dev(tensors[len(out)], name, dtype)
+    raise ValueError("%s is on %s, the call's first tensor on device %d" % (name, t.device, dev))
 
 
 def _rows(t, name, dtype):
-    """Elements between neighbouring tokens of t [B,T,heads,d]: a token's rows contiguous, tokens equally far apart."""
+    """(address, elements between neighbouring tokens, device) of t [B,T,heads,d]: a token's rows contiguous, tokens
+    equally far apart."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError("%s must be a CUDA (HIP) tensor" % name)
     if t.dtype is not dtype:
@@ -425,50 +441,18 @@ def _rows(t, name, dtype):
     if t.dim() != 4:
         raise ValueError("%s must be [B, T, heads, d], got %s" % (name, tuple(t.shape)))
     B, T, h, d = t.shape
-    if t.is_contiguous():
-        return h * d
-    sb, st, sh, sd = t.stride()
-    if (sd != 1 and d > 1) or (sh != d and h > 1) or (B > 1 and T > 1 and sb != T * st):
-        raise ValueError("%s: a token's rows must be contiguous and the tokens equally far apart" % name)
-    return st if T > 1 else sb if B > 1 else h * d
+    step = h * d
+    if not t.is_contiguous():
+        sb, st, sh, sd = t.stride()
+        if (sd != 1 and d > 1) or (sh != d and h > 1) or (B > 1 and T > 1 and sb != T * st):
+            raise ValueError("%s: a token's rows must be contiguous and the tokens equally far apart" % name)
+        step = st if T > 1 else sb if B > 1 else step
+    return t.data_ptr(), step, t.get_device()
 
 
 def _shaped(t, name, shape):
     if t is not None and t.shape != shape:
         raise ValueError("%s must be %s, got %s" % (name, tuple(shape), tuple(t.shape)))
-
-
-def _packed(cu_seqlens, B):
-    """(n_seqs of the C call, sequences)."""
-    if cu_seqlens is None:
-        return 0, B
-    n_seqs = cu_seqlens.numel() - 1
-    return n_seqs, n_seqs
-
-
-def _cache_args(dev, k_cache, v_cache, k_scale, v_scale, block_table, seq_lens, cu_seqlens, n, Hkv, d):
-    ct = _CACHE.get(k_cache.dtype) if isinstance(k_cache, torch.Tensor) else None
-    if ct is None:
-        raise TypeError("k_cache must be bfloat16 or float8_e4m3fn")
-    _same(dev, (k_cache, "k_cache", k_cache.dtype), (v_cache, "v_cache", k_cache.dtype), (block_table, "block_table", torch.int32),
-          (seq_lens, "seq_lens", torch.int32), (cu_seqlens, "cu_seqlens", torch.int32))
-    shape = k_cache.shape
-    if len(shape) != 4 or shape[1] != Hkv or shape[3] != d or v_cache.shape != shape:
-        raise ValueError("k_cache and v_cache must be [n_pages, %d, page, %d], got %s and %s" % (
-            Hkv, d, tuple(shape), tuple(v_cache.shape)))
-    table = block_table.shape
-    if len(table) != 2 or table[0] != n or seq_lens.shape != (n,):
-        raise ValueError("block_table must be [%d, max_pages] and seq_lens [%d], got %s and %s" % (
-            n, n, tuple(table), tuple(seq_lens.shape)))
-    if ct == GDN_E4M3:
-        if k_scale is None or v_scale is None:
-            raise ValueError("a float8_e4m3fn cache needs k_scale and v_scale")
-        _same(dev, (k_scale, "k_scale", torch.float32), (v_scale, "v_scale", torch.float32))
-        _shaped(k_scale, "k_scale", shape[:2])
-        _shaped(v_scale, "v_scale", shape[:2])
-    elif k_scale is not None or v_scale is not None:
-        raise ValueError("k_scale and v_scale belong to a float8_e4m3fn cache")
-    return shape[2], shape[0], table[1], ct
 
 
 def _on(dev, call, *args):
@@ -482,6 +466,9 @@ def _on(dev, call, *args):
         _check(status)
 
 
+_NORM_NAMES = ("q_out", "k_out", "q_weight", "k_weight", "inv_freq", "positions", "cu_seqlens")
+
+
 def gdn_qk_norm_rope(q, k, *, q_weight=None, k_weight=None, eps=1e-6, inv_freq=None, interleaved=False, positions=None,
                      cu_seqlens=None, q_out=None, k_out=None):
     """Norms of queries and keys per head and the position rotation; see ``gdn_qk_norm_rope`` in include/gdn.h.
@@ -492,32 +479,63 @@ def gdn_qk_norm_rope(q, k, *, q_weight=None, k_weight=None, eps=1e-6, inv_freq=N
     """
     if not isinstance(q, torch.Tensor) or q.dtype not in _IO:
         raise TypeError("q must be float32 or bfloat16")
-    qs, ks = _rows(q, "q", q.dtype), _rows(k, "k", q.dtype)
-    B, T, H, d = q.shape
+    io = q.dtype
+    qp, qs, dev = _rows(q, "q", io)
+    kp, ks, kdev = _rows(k, "k", io)
+    shape = B, T, H, d = q.shape
     Hkv = k.shape[2]
     if k.shape != (B, T, Hkv, d):
         raise ValueError("inconsistent shapes q%s k%s" % (tuple(q.shape), tuple(k.shape)))
-    if q_out is None:
-        q_out = torch.empty(q.shape, device=q.device, dtype=q.dtype)
-    if k_out is None:
-        k_out = torch.empty(k.shape, device=k.device, dtype=k.dtype)
-    dev = q.get_device()
-    if k.get_device() != dev:
+    if kdev != dev:
         raise ValueError("q is on %s, k on %s" % (q.device, k.device))
-    _same(dev, (q_out, "q_out", q.dtype), (k_out, "k_out", q.dtype), (q_weight, "q_weight", torch.float32),
-          (k_weight, "k_weight", torch.float32), (inv_freq, "inv_freq", torch.float64), (positions, "positions", torch.int32),
-          (cu_seqlens, "cu_seqlens", torch.int32))
-    _shaped(q_out, "q_out", q.shape)
+    if q_out is None:
+        q_out = torch.empty(shape, device=q.device, dtype=io)
+    if k_out is None:
+        k_out = torch.empty(k.shape, device=k.device, dtype=io)
+    qo, ko, qw, kw, fp, pos, cu = _addresses(dev, (q_out, k_out, q_weight, k_weight, inv_freq, positions, cu_seqlens),
+                                             _NORM_NAMES, (io, io, _F32, _F32, _F64, _I32, _I32))
+    _shaped(q_out, "q_out", shape)
     _shaped(k_out, "k_out", k.shape)
     _shaped(q_weight, "q_weight", (d,))
     _shaped(k_weight, "k_weight", (d,))
     _shaped(positions, "positions", (B, T))
-    rot = 0 if inv_freq is None else 2 * inv_freq.numel()
-    n_seqs, _ = _packed(cu_seqlens, B)
-    _on(dev, lib().gdn_qk_norm_rope, _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), B, T, H, Hkv, d, qs, ks,
-        _ptr(q_weight), _ptr(k_weight), float(eps), _ptr(inv_freq), rot, _ptr(positions), _ptr(cu_seqlens), n_seqs,
-        _IO[q.dtype], GDN_ROPE_INTERLEAVED if interleaved else 0)
+    _on(dev, lib().gdn_qk_norm_rope, qp, kp, qo, ko, B, T, H, Hkv, d, qs, ks, qw, kw, eps, fp,
+        0 if inv_freq is None else 2 * inv_freq.numel(), pos, cu, 0 if cu is None else cu_seqlens.numel() - 1, _IO[io],
+        GDN_ROPE_INTERLEAVED if interleaved else 0)
     return q_out, k_out
+
+
+_CACHE_NAMES = ("k_cache", "v_cache", "block_table", "seq_lens", "cu_seqlens", "k_scale", "v_scale")
+
+
+def _cache_args(dev, k_cache, v_cache, block_table, seq_lens, cu_seqlens, k_scale, v_scale, B, Hkv, d):
+    """Addresses of the cache and its tables, and its sizes; Hkv None: the cache's."""
+    ct = _CACHE.get(k_cache.dtype) if isinstance(k_cache, torch.Tensor) else None
+    if ct is None:
+        raise TypeError("k_cache must be bfloat16 or float8_e4m3fn")
+    kind = k_cache.dtype
+    at = _addresses(dev, (k_cache, v_cache, block_table, seq_lens, cu_seqlens, k_scale, v_scale), _CACHE_NAMES,
+                    (kind, kind, _I32, _I32, _I32, _F32, _F32))
+    shape, table = k_cache.shape, block_table.shape
+    n_seqs = 0 if cu_seqlens is None else cu_seqlens.numel() - 1
+    n = B if cu_seqlens is None else n_seqs
+    if len(shape) != 4 or shape[3] != d or (Hkv is not None and shape[1] != Hkv) or v_cache.shape != shape:
+        raise ValueError("k_cache and v_cache must be [n_pages, %s, page, %d], got %s and %s" % (
+            "H_kv" if Hkv is None else Hkv, d, tuple(shape), tuple(v_cache.shape)))
+    if len(table) != 2 or table[0] != n or seq_lens.shape != (n,):
+        raise ValueError("block_table must be [%d, max_pages] and seq_lens [%d], got %s and %s" % (
+            n, n, tuple(table), tuple(seq_lens.shape)))
+    if ct == GDN_E4M3:
+        if k_scale is None or v_scale is None:
+            raise ValueError("a float8_e4m3fn cache needs k_scale and v_scale")
+        _shaped(k_scale, "k_scale", shape[:2])
+        _shaped(v_scale, "v_scale", shape[:2])
+    elif k_scale is not None or v_scale is not None:
+        raise ValueError("k_scale and v_scale belong to a float8_e4m3fn cache")
+    return at, shape[1], shape[2], shape[0], table[1], n_seqs, ct
+
+
+_APPEND_NAMES = ("q_out", "q_weight", "k_weight", "inv_freq")
 
 
 def gdn_kv_append(k, v, k_cache, v_cache, block_table, seq_lens, *, q=None, q_out=None, k_scale=None, v_scale=None,
@@ -529,39 +547,43 @@ def gdn_kv_append(k, v, k_cache, v_cache, block_table, seq_lens, *, q=None, q_ou
     the latter; ``block_table`` [n,max_pages] and ``seq_lens`` [n] (with the new tokens) int32.  Norm and rotation as
     ``gdn_qk_norm_rope``.  Returns q_out (None without q).
     """
-    ks, vs = _rows(k, "k", torch.bfloat16), _rows(v, "v", torch.bfloat16)
+    kp, ks, dev = _rows(k, "k", _BF16)
+    vp, vs, vdev = _rows(v, "v", _BF16)
     shape = B, T, Hkv, d = k.shape
     if v.shape != shape:
         raise ValueError("inconsistent shapes k%s v%s" % (tuple(k.shape), tuple(v.shape)))
-    dev, H, qs = k.get_device(), Hkv, 0
+    qp, qs, qdev, H = None, 0, dev, Hkv
     if q is not None:
-        qs, H = _rows(q, "q", torch.bfloat16), q.shape[2]
+        qp, qs, qdev = _rows(q, "q", _BF16)
+        H = q.shape[2]
         if q.shape != (B, T, H, d):
             raise ValueError("inconsistent shapes q%s k%s" % (tuple(q.shape), tuple(k.shape)))
         if q_out is None:
-            q_out = torch.empty(q.shape, device=q.device, dtype=q.dtype)
+            q_out = torch.empty(q.shape, device=q.device, dtype=_BF16)
+        elif q_out.shape != q.shape:
+            _shaped(q_out, "q_out", q.shape)
     elif q_out is not None:
         raise ValueError("q_out without q")
-    if v.get_device() != dev or (q is not None and q.get_device() != dev):
+    if vdev != dev or qdev != dev:
         raise ValueError("q, k and v must be on one device")
-    _same(dev, (q_out, "q_out", torch.bfloat16), (q_weight, "q_weight", torch.float32), (k_weight, "k_weight", torch.float32),
-          (inv_freq, "inv_freq", torch.float64))
-    if q_out is not None:
-        _shaped(q_out, "q_out", q.shape)
-    _shaped(q_weight, "q_weight", (d,))
-    _shaped(k_weight, "k_weight", (d,))
-    rot = 0 if inv_freq is None else 2 * inv_freq.numel()
-    n_seqs, n = _packed(cu_seqlens, B)
-    page, n_pages, max_pages, ct = _cache_args(dev, k_cache, v_cache, k_scale, v_scale, block_table, seq_lens, cu_seqlens, n, Hkv, d)
-    _on(dev, lib().gdn_kv_append, _ptr(q), _ptr(k), _ptr(v), _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale),
-        _ptr(v_scale), _ptr(block_table), _ptr(seq_lens), B, T, H, Hkv, d, page, n_pages, max_pages, qs, ks, vs,
-        _ptr(q_weight), _ptr(k_weight), float(eps), _ptr(inv_freq), rot, _ptr(cu_seqlens), n_seqs, GDN_BF16, ct,
+    qo, qw, kw, fp = _addresses(dev, (q_out, q_weight, k_weight, inv_freq), _APPEND_NAMES, (_BF16, _F32, _F32, _F64))
+    if qw is not None and q_weight.numel() != d:
+        _shaped(q_weight, "q_weight", (d,))
+    if kw is not None and k_weight.numel() != d:
+        _shaped(k_weight, "k_weight", (d,))
+    (kc, vc, table, lens, cu, ksc, vsc), _, page, n_pages, max_pages, n_seqs, ct = _cache_args(
+        dev, k_cache, v_cache, block_table, seq_lens, cu_seqlens, k_scale, v_scale, B, Hkv, d)
+    _on(dev, lib().gdn_kv_append, qp, kp, vp, qo, kc, vc, ksc, vsc, table, lens, B, T, H, Hkv, d, page, n_pages, max_pages,
+        qs, ks, vs, qw, kw, eps, fp, 0 if fp is None else 2 * inv_freq.numel(), cu, n_seqs, GDN_BF16, ct,
         GDN_ROPE_INTERLEAVED if interleaved else 0)
     return q_out
 
 
 def gdn_attention_paged_workspace_bytes(B, T, H, H_kv, d, page, max_pages, n_seqs=0) -> int:
     return int(lib().gdn_attention_paged_workspace_bytes(B, T, H, H_kv, d, page, max_pages, n_seqs))
+
+
+_ATTENTION_NAMES = ("q", "o", "workspace")
 
 
 def gdn_attention_paged(q, k_cache, v_cache, block_table, seq_lens, *, k_scale=None, v_scale=None, scale=None,
@@ -571,23 +593,22 @@ def gdn_attention_paged(q, k_cache, v_cache, block_table, seq_lens, *, k_scale=N
     q [B,T,H,d] bf16, T new tokens for each of B sequences, or packed (B == 1) with ``cu_seqlens`` int32 [n+1]; the cache
     and its tables as ``gdn_kv_append``, which has put the new tokens there; ``scale`` defaults to 1/sqrt(d).  Returns o.
     """
-    _dev(q, "q", torch.bfloat16)
+    _dev(q, "q", _BF16)
     if q.dim() != 4:
         raise ValueError("q must be [B, T, heads, d], got %s" % (tuple(q.shape),))
-    B, T, H, d = q.shape
+    shape = B, T, H, d = q.shape
     dev = q.get_device()
     if o is None:
-        o = torch.empty(q.shape, device=q.device, dtype=q.dtype)
-    _same(dev, (o, "o", torch.bfloat16), (workspace, "workspace", torch.uint8))
-    _shaped(o, "o", q.shape)
-    n_seqs, n = _packed(cu_seqlens, B)
-    Hkv = k_cache.shape[1] if isinstance(k_cache, torch.Tensor) and k_cache.dim() == 4 else 0
-    page, n_pages, max_pages, ct = _cache_args(dev, k_cache, v_cache, k_scale, v_scale, block_table, seq_lens, cu_seqlens, n, Hkv, d)
+        o = torch.empty(shape, device=q.device, dtype=_BF16)
+    (kc, vc, table, lens, cu, ksc, vsc), Hkv, page, n_pages, max_pages, n_seqs, ct = _cache_args(
+        dev, k_cache, v_cache, block_table, seq_lens, cu_seqlens, k_scale, v_scale, B, None, d)
     if workspace is None:
-        need = gdn_attention_paged_workspace_bytes(B, T, H, Hkv, d, page, max_pages, n_seqs)
+        need = lib().gdn_attention_paged_workspace_bytes(B, T, H, Hkv, d, page, max_pages, n_seqs)
         workspace = torch.empty(need, device=q.device, dtype=torch.uint8) if need else None
-    ws_bytes = 0 if workspace is None else workspace.numel()
-    _on(dev, lib().gdn_attention_paged, _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale),
-        _ptr(block_table), _ptr(seq_lens), _ptr(o), B, T, H, Hkv, d, page, n_pages, max_pages, _ptr(cu_seqlens), n_seqs,
-        GDN_BF16, ct, float(scale) if scale is not None else d ** -0.5, _ptr(workspace) if ws_bytes else None, ws_bytes)
+    qp, op, ws = _addresses(dev, (q, o, workspace), _ATTENTION_NAMES, (_BF16, _BF16, torch.uint8))
+    if o.shape != shape:
+        _shaped(o, "o", shape)
+    size = 0 if ws is None else workspace.numel()
+    _on(dev, lib().gdn_attention_paged, qp, kc, vc, ksc, vsc, table, lens, op, B, T, H, Hkv, d, page, n_pages, max_pages, cu,
+        n_seqs, GDN_BF16, ct, d ** -0.5 if scale is None else scale, ws if size else None, size)
     return o

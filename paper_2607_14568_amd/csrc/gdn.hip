@@ -3233,7 +3233,7 @@ void launch_paged(const PagedParams& p, const PagedPlan& plan, hipStream_t st) {
     const long blocks = plan.blocks * p.HKV;
     if (plan.rb == AQ) {
         hipLaunchKernelGGL((k_attn_tile<DH, CT, 1>), grid, dim3(NT_ATT), 0, st, p);
-        if (p.spare > 0) hipLaunchKernelGGL((k_attn_join_tile<DH>), dim3((unsigned)blocks), dim3(NT_ATT), 0, st, p);
+        if (p.spare > 0) hipLaunchKernelGGL((k_attn_join_tile<DH>), dim3((unsigned)blocks, (unsigned)(plan.rows + 31) / 32), dim3(NT), 0, st, p);
         return;
     }
     hipLaunchKernelGGL((k_attn_rows<DH, CT>), grid, dim3(NT), 0, st, p);

@@ -942,7 +942,8 @@ template <int DH, typename CT, int QT>
 __global__ __launch_bounds__(NT_ATT / QT) __attribute__((amdgpu_waves_per_eu(4 / QT))) void k_attn_tile(PagedParams p) {
     constexpr bool E4M3 = sizeof(CT) == 1;
     constexpr int RB = AQ, NTH = NT_ATT / QT, NW = NTH / 64, NCH = DH / 8, RPI = 64 / NCH, NKB = DH / 32, NDT = DH / 16, ESZ = sizeof(CT);
-    __shared__ AttnLds<DH> lds;
+    // (a variable per ring slot: the compiler then sees that reads of one do not wait for the copies into the other)
+    __shared__ __align__(16) bf16_t k_even[AKB * DH], v_even[AKB * DH], k_odd[AKB * DH], v_odd[AKB * DH];
     __shared__ int odd;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, lg = lane >> 4;
@@ -1030,8 +1031,8 @@ __global__ __launch_bounds__(NT_ATT / QT) __attribute__((amdgpu_waves_per_eu(4 /
                 const int first = RPI * (wave + NW * c), r = first + lane / NCH;
                 if (c == 0 || p.c.page < AKB) describe(kb, first, rk, rv);
                 const int off = r * DH * 2 + (((lane % NCH) ^ swz(r)) << 4);
-                bdma16(rk, &lds.k[sl][first * DH], off);
-                bdma16(rv, &lds.v[sl][first * DH], off);
+                bdma16(rk, &(sl ? k_odd : k_even)[first * DH], off);
+                bdma16(rv, &(sl ? v_odd : v_even)[first * DH], off);
             }
         }
     };
@@ -1047,12 +1048,22 @@ __global__ __launch_bounds__(NT_ATT / QT) __attribute__((amdgpu_waves_per_eu(4 /
                                       fp8_pair(kc[c][2 * z + 1], false), fp8_pair(kc[c][2 * z + 1], true)};
                     const int4v v4 = {fp8_pair(vc[c][2 * z], false), fp8_pair(vc[c][2 * z], true),
                                       fp8_pair(vc[c][2 * z + 1], false), fp8_pair(vc[c][2 * z + 1], true)};
-                    *reinterpret_cast<int4v*>(&lds.k[sl][kq(r, cc + 8 * z)]) = k4;
-                    *reinterpret_cast<int4v*>(&lds.v[sl][kq(r, cc + 8 * z)]) = v4;
+                    *reinterpret_cast<int4v*>(&(sl ? k_odd : k_even)[kq(r, cc + 8 * z)]) = k4;
+                    *reinterpret_cast<int4v*>(&(sl ? v_odd : v_even)[kq(r, cc + 8 * z)]) = v4;
                 }
             }
         }
     };
+    // The queries have to be there before the loop: a load still in flight at its head would make every block wait for the next
+    // block's copies.
+#pragma unroll
+    for (int u = 0; u < QT; ++u)
+#pragma unroll
+        for (int kb = 0; kb < NKB; ++kb) {
+            int4v x = __builtin_bit_cast(int4v, qf[u][kb]);
+            asm volatile("" : "+v"(x));
+            qf[u][kb] = __builtin_bit_cast(bf16x8, x);
+        }
     const float sl2 = p.scale_log2;
     float m[QT], l[QT];
     floatx4 oacc[QT][NDT];
@@ -1081,7 +1092,7 @@ __global__ __launch_bounds__(NT_ATT / QT) __attribute__((amdgpu_waves_per_eu(4 /
             bool found = false;
 #pragma unroll
             for (int c = 0; c < AKB * DH / 8 / NTH; ++c) {
-                int4v* at = reinterpret_cast<int4v*>(&lds.v[SL][(tid + NTH * c) * 8]);
+                int4v* at = reinterpret_cast<int4v*>(&(SL ? v_odd : v_even)[(tid + NTH * c) * 8]);
                 int4v x = *at;
                 bool any = false;
 #pragma unroll
@@ -1097,8 +1108,8 @@ __global__ __launch_bounds__(NT_ATT / QT) __attribute__((amdgpu_waves_per_eu(4 /
             lds_barrier();
         }
         if (kb <= wlast) {
-            const bf16_t* sk = lds.k[SL];
-            const bf16_t* sv = lds.v[SL];
+            const bf16_t* sk = SL ? k_odd : k_even;
+            const bf16_t* sv = SL ? v_odd : v_even;
             floatx4 st[QT][4];   // S^T of query tile u: keys 16 t + 4 lg + e, query l16
 #pragma unroll
             for (int u = 0; u < QT; ++u)
@@ -1279,11 +1290,11 @@ __global__ __launch_bounds__(NT) void k_attn_join(PagedParams p) {
     *reinterpret_cast<bf16x4*>(dst) = __builtin_convertvector(o * inv, bf16x4);
 }
 
-// Blocks of 128 rows have few chunks, mostly two: DH / 4 lanes a row, all of a workgroup's rows loaded at once.
+// Blocks of 128 rows have few chunks, mostly two: DH / 4 lanes a row, 32 rows (blockIdx.y) a workgroup, all loaded at once.
 template <int DH>
-__global__ __launch_bounds__(NT_ATT) void k_attn_join_tile(PagedParams p) {
-    constexpr int RB = AQ, LPR = DH / 4, NG = NT_ATT / LPR, PASS = RB / NG;
-    const int g = threadIdx.x / LPR, c4 = 4 * (threadIdx.x % LPR);
+__global__ __launch_bounds__(NT) void k_attn_join_tile(PagedParams p) {
+    constexpr int RB = AQ, LPR = DH / 4, NG = NT / LPR, ROWS = 32, PASS = ROWS / NG;
+    const int g = blockIdx.y * ROWS + threadIdx.x / LPR, c4 = 4 * (threadIdx.x % LPR);
     const int w = div_by(blockIdx.x, p.by_hkv), hk = (int)blockIdx.x - w * p.HKV;
     Item it;
     if (!find_item<RB, true>(p, w, it) || it.chunks == 1) return;

@@ -99,7 +99,7 @@ def test_rows_of_a_projection():
         is_cuda = True
 
     def rows(t):
-        return gdn._rows(t.as_subclass(Cuda), "q", torch.float32)
+        return gdn._rows(t.as_subclass(Cuda), "q", torch.float32)[1]
     wide = torch.zeros(2, 3, 10, 64)
     assert rows(wide) == 640 and rows(wide[:, :, 2:6]) == 640 and rows(wide[:1, :, 2:6]) == 640 and rows(wide[:, :1, 2:6]) == 1920
     assert rows(wide[:1, :1, 2:6]) == 256
