@@ -3160,12 +3160,15 @@ void launch_attention(AttnParams a, hipStream_t st) {
         hipLaunchKernelGGL((k_attn_causal<DH, 1>), dim3((unsigned)wgs), dim3(NT_ATT), 0, st, a);
 }
 
-// Row groups per wave of k_rows: few tokens spread their heads over waves (latency), many keep a token's angles and
-// place in one wave.
+// Row groups per wave of k_rows: one while they do not fill the chip's wave slots (latency), then two or more, up to about
+// 16384 waves, so that a token's angles and place are formed fewer times.  Waves of 2 against 1 group: packed q and k of
+// 60 to 2900 tokens, 20 heads of 64, 11.3 us against 12.0, q of 4133 tokens into an e4m3 cache 18.3 against 20.5; of 3
+// against 6: q and k of 10240 tokens, 24 heads of 128, 30.2 against 32.1.
 void rows_split(RowsParams& p, int rows, int dh) {
-    const int groups = (rows + 512 / dh - 1) / (512 / dh);   // 64 / (dh / 8) rows each
-    p.per = (int)std::min<long>(groups, std::max<long>(1, p.tokens * groups / 16384));
-    p.units = (groups + p.per - 1) / p.per;
+    const long groups = (rows + 512 / dh - 1) / (512 / dh), work = p.tokens * groups;   // 64 / (dh / 8) rows a group
+    const long per = work <= 8192 ? 1 : std::min(groups, std::max(2L, work / 16384));
+    p.units = (int)((groups + per - 1) / per);
+    p.per = (int)((groups + p.units - 1) / p.units);
 }
 long rows_wgs(const RowsParams& p) { return (p.tokens * p.units + NT / 64 - 1) / (NT / 64); }
 
@@ -3193,7 +3196,12 @@ struct PagedPlan {
 PagedPlan paged_plan(int B, int T, int H, int H_kv, int page, int max_pages, int n_seqs) {
     const long G = H / H_kv;
     PagedPlan p = {};
-    p.rb = T * G > 32L * std::max(n_seqs, 1) ? AQ : 16;
+    // Blocks of 16 rows read the keys once per block, from the caches; they are the faster ones where a sequence has one, or
+    // all of them are few.  us in blocks of 16 and of 128 rows: 32 tokens of one sequence, 16 heads over 8 (32 blocks) over 4096
+    // keys 18.2 and 23.2, over 32768 52.9 and 42.9; 64 tokens (64 blocks) 24.0 and 24.5, 88 and 49; 2 sequences of 16, 16
+    // heads over 4 (32 blocks), over 1000 to 8000 keys 16.0 and 23.8; 16 of 8 (128 blocks) 52 and 34.
+    const long few = n_seqs > 0 ? (T * G) / 16 + std::min<long>(n_seqs, T) : B * ((T * G + 15) / 16);
+    p.rb = T * G <= 16L * std::max(n_seqs, 1) || few * H_kv <= 32 ? 16 : AQ;
     p.rows = (int)std::min<long>(T * G, p.rb);
     p.blocks = n_seqs > 0 ? (T * G) / p.rb + std::min<long>(n_seqs, T) : B * ((T * G + p.rb - 1) / p.rb);
     const long units = ((long)page * max_pages + UNIT - 1) / UNIT;   // of a row block at most
@@ -3232,8 +3240,8 @@ void launch_paged(const PagedParams& p, const PagedPlan& plan, hipStream_t st) {
     const dim3 grid((unsigned)(p.items * p.HKV));
     const long blocks = plan.blocks * p.HKV;
     if (plan.rb == AQ) {
-        hipLaunchKernelGGL((k_attn_tile<DH, CT, 1>), grid, dim3(NT_ATT), 0, st, p);
-        if (p.spare > 0) hipLaunchKernelGGL((k_attn_join_tile<DH>), dim3((unsigned)blocks, (unsigned)(plan.rows + 31) / 32), dim3(NT), 0, st, p);
+        hipLaunchKernelGGL((k_attn_tile<DH, CT>), grid, dim3(NT), 0, st, p);
+        if (p.spare > 0) hipLaunchKernelGGL((k_attn_join_tile<DH>), dim3((unsigned)blocks, (unsigned)(plan.rows + 15) / 16), dim3(NT), 0, st, p);
         return;
     }
     hipLaunchKernelGGL((k_attn_rows<DH, CT>), grid, dim3(NT), 0, st, p);

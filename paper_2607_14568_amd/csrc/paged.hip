@@ -560,7 +560,7 @@ template <int RB, bool BLOCK = false> __device__ __forceinline__ bool find_item(
 #pragma unroll
         for (int off = 1; off < 64; off <<= 1) total += __shfl_xor(total, off, 64);
         total *= 1.f - 0x1p-19f;
-        c = max((int)min(ceilf(total / (float)p.round), 0x1p23f), 1);
+        c = max((int)min(ceilf(total / (float)p.round), 0x1p23f), RB == 16 ? 1 : 4);   // (a tile's chunk of fewer keys is mostly joining)
         auto uneven = [&](int c) { return c > p.fine && total < 0.8f * (float)c * (float)p.round; };
         bool fits;
         for (;;) {
@@ -636,6 +636,31 @@ template <bool SCALED> struct PageWalk {
     __device__ __forceinline__ float kscale(int b) const { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, ks), b - first)); }
     __device__ __forceinline__ float vscale(int b) const { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, vs), b - first)); }
 };
+
+// Eight e4m3 codes times their scale as bf16: exact for a power of two, which is what gdn_kv_append makes a scale (the
+// instruction multiplies by the scale's exponent); any other one's products are rounded to bf16, as keys and values that
+// were cached in bf16 are.
+__device__ __forceinline__ int4v fp8_scaled(int a, int b, float scale) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    if ((__float_as_uint(scale) & 0x7fffff) == 0)
+        return int4v{__builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false)),
+                     __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true)),
+                     __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false)),
+                     __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true))};
+    float x[8];
+    from_e4m3((uint64_t)(uint32_t)a | (uint64_t)(uint32_t)b << 32, x);
+    return __builtin_bit_cast(int4v, pack_bf16(floatx4{x[0], x[1], x[2], x[3]} * scale, floatx4{x[4], x[5], x[6], x[7]} * scale));
+}
+
+// c + the eight values
+__device__ __forceinline__ float sum_bf16(bf16x8 w, float c) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    typedef float floatx2 __attribute__((ext_vector_type(2)));
+    const bf16x2 one = __builtin_convertvector((floatx2{1.f, 1.f}), bf16x2);
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) c = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{w[i], w[i + 1]}, one, c, false);
+    return c;
+}
 
 // ------------------------------------------------------------------ k_attn_rows: few rows, many keys
 // Attention of blocks of up to 16 rows; bound by the cache's bytes.  A wave takes 32 keys a step, K and V from memory
@@ -937,11 +962,11 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
 // Attention of blocks of 128 rows; bound by the matrix units and the softmax beside them.  Blocks of 64 keys and values
 // lie in a double-buffered LDS ring (16-byte chunks XOR-swizzled as in k_attn_causal, whose products, running softmax and
 // operand orders these are): a bf16 cache is copied there without registers, e4m3 codes are loaded a block ahead, made
-// bf16 once (exactly) and stored; their scales multiply the scores and the weights.
-template <int DH, typename CT, int QT>
-__global__ __launch_bounds__(NT_ATT / QT) __attribute__((amdgpu_waves_per_eu(4 / QT))) void k_attn_tile(PagedParams p) {
+// bf16 with their scale and stored.
+template <int DH, typename CT>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2))) void k_attn_tile(PagedParams p) {
     constexpr bool E4M3 = sizeof(CT) == 1;
-    constexpr int RB = AQ, NTH = NT_ATT / QT, NW = NTH / 64, NCH = DH / 8, RPI = 64 / NCH, NKB = DH / 32, NDT = DH / 16, ESZ = sizeof(CT);
+    constexpr int RB = AQ, QT = 2, NW = NT / 64, NCH = DH / 8, RPI = 64 / NCH, NKB = DH / 32, NDT = DH / 16, ESZ = sizeof(CT);
     // (a variable per ring slot: the compiler then sees that reads of one do not wait for the copies into the other)
     __shared__ __align__(16) bf16_t k_even[AKB * DH], v_even[AKB * DH], k_odd[AKB * DH], v_odd[AKB * DH];
     __shared__ int odd;
@@ -977,45 +1002,49 @@ __global__ __launch_bounds__(NT_ATT / QT) __attribute__((amdgpu_waves_per_eu(4 /
     PageWalk<E4M3> walk;
     walk.row = p.c.table + (long)it.s * p.c.max_pages;
     if (k1 > k0) walk.load(p, hk, k0 >> p.c.shift);
-    // what a block's keys need when they are used, taken when their copies are sent off
-    struct Block { int there; float ks[E4M3 ? 4 : 1], vs[E4M3 ? 4 : 1]; } cur, nxt;   // there: bit t, the page of keys 16 t ..
-    auto look = [&](Block& x, int kb) {
-        x.there = 0;
+    int there = 0, next_there = 0;   // bit t: keys 16 t .. of the block, and of the next one, are the item's and their page is there
+    auto look = [&](int kb) {
         walk.reach(p, hk, kb >> p.c.shift, (kb + AKB - 1) >> p.c.shift);
+        if (p.c.page >= AKB) {
+            next_there = walk.page(kb >> p.c.shift) >= 0 ? 15 : 0;
+        } else {
+            next_there = 0;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int key = kb + 16 * t, b = key >> p.c.shift;
-            x.there |= (key < k1 && walk.page(b) >= 0) << t;
-            if constexpr (E4M3) {
-                x.ks[t] = walk.kscale(b);
-                x.vs[t] = walk.vscale(b);
-            }
+            for (int t = 0; t < 4; ++t) next_there |= (kb + 16 * t < k1 && walk.page((kb + 16 * t) >> p.c.shift) >= 0) << t;
         }
     };
     // Rows of the block at key kb by descriptors whose offset 0 would be the block's first row: of the whole block where a page
     // holds it, else of the 16 rows around row r.  Rows past the item's keys, and of pages that are not there, read as zeros.
-    auto describe = [&](int kb, int r, __amdgpu_buffer_rsrc_t& rk, __amdgpu_buffer_rsrc_t& rv) {
+    auto describe = [&](int kb, int r, __amdgpu_buffer_rsrc_t& rk, __amdgpu_buffer_rsrc_t& rv, float& ks, float& vs) {
         const int g = p.c.page >= AKB ? 0 : r & ~15, span = p.c.page >= AKB ? AKB : 16, key = kb + g;
         const int id = key < k1 ? walk.page(key >> p.c.shift) : -1;
+        if constexpr (E4M3) {
+            ks = walk.kscale(key >> p.c.shift);
+            vs = walk.vscale(key >> p.c.shift);
+        }
         const long at = (((((long)max(id, 0) * p.HKV + hk) << p.c.shift) + (key & (p.c.page - 1))) - g) * DH * ESZ;
         const uint32_t bytes = id >= 0 ? (uint32_t)(g + min(k1 - key, span)) * DH * ESZ : 0;
         rk = rsrc((const char*)p.c.k + at, bytes);
         rv = rsrc((const char*)p.c.v + at, bytes);
     };
     constexpr int NCW = AKB / RPI / NW;                   // bf16: this wave's 1 KB copies of K, and of V
-    constexpr int PB = AKB * DH / NTH < 16 ? 8 : 16;      // e4m3: bytes of a piece, and this thread's pieces of K, and of V
-    constexpr int NCB = AKB * DH / PB / NTH;
+    constexpr int PB = AKB * DH / NT < 16 ? 8 : 16;      // e4m3: bytes of a piece, and this thread's pieces of K, and of V
+    constexpr int NCB = AKB * DH / PB / NT;
     static_assert(NCW >= 1 && NCB >= 1, "every thread copies the same share");
     int4v kc[E4M3 ? NCB : 1], vc[E4M3 ? NCB : 1];
+    float kscale[E4M3 ? NCB : 1], vscale[E4M3 ? NCB : 1];   // of these pieces' page
     auto issue = [&](int kb, auto SLOT) {
         constexpr int sl = decltype(SLOT)::value;
         __amdgpu_buffer_rsrc_t rk, rv;
+        float ks = 1.f, vs = 1.f;
         if constexpr (E4M3) {
 #pragma unroll
             for (int c = 0; c < NCB; ++c) {
                 const int row = 64 * (wave + NW * c) * PB / DH;   // the first of the wave's rows
-                if (c == 0 || p.c.page < AKB) describe(kb, row, rk, rv);
-                const int off = (tid + NTH * c) * PB;
+                if (c == 0 || p.c.page < AKB) describe(kb, row, rk, rv, ks, vs);
+                kscale[c] = ks;
+                vscale[c] = vs;
+                const int off = (tid + NT * c) * PB;
                 if constexpr (PB == 16) {
                     kc[c] = __builtin_bit_cast(int4v, bload16(rk, off));
                     vc[c] = __builtin_bit_cast(int4v, bload16(rv, off));
@@ -1029,7 +1058,7 @@ __global__ __launch_bounds__(NT_ATT / QT) __attribute__((amdgpu_waves_per_eu(4 /
 #pragma unroll
             for (int c = 0; c < NCW; ++c) {
                 const int first = RPI * (wave + NW * c), r = first + lane / NCH;
-                if (c == 0 || p.c.page < AKB) describe(kb, first, rk, rv);
+                if (c == 0 || p.c.page < AKB) describe(kb, first, rk, rv, ks, vs);
                 const int off = r * DH * 2 + (((lane % NCH) ^ swz(r)) << 4);
                 bdma16(rk, &(sl ? k_odd : k_even)[first * DH], off);
                 bdma16(rv, &(sl ? v_odd : v_even)[first * DH], off);
@@ -1041,13 +1070,10 @@ __global__ __launch_bounds__(NT_ATT / QT) __attribute__((amdgpu_waves_per_eu(4 /
         if constexpr (E4M3) {
 #pragma unroll
             for (int c = 0; c < NCB; ++c) {
-                const int piece = tid + NTH * c, r = piece * PB / DH, cc = piece * PB % DH;
+                const int piece = tid + NT * c, r = piece * PB / DH, cc = piece * PB % DH;
 #pragma unroll
                 for (int z = 0; z < PB / 8; ++z) {
-                    const int4v k4 = {fp8_pair(kc[c][2 * z], false), fp8_pair(kc[c][2 * z], true),
-                                      fp8_pair(kc[c][2 * z + 1], false), fp8_pair(kc[c][2 * z + 1], true)};
-                    const int4v v4 = {fp8_pair(vc[c][2 * z], false), fp8_pair(vc[c][2 * z], true),
-                                      fp8_pair(vc[c][2 * z + 1], false), fp8_pair(vc[c][2 * z + 1], true)};
+                    const int4v k4 = fp8_scaled(kc[c][2 * z], kc[c][2 * z + 1], kscale[c]), v4 = fp8_scaled(vc[c][2 * z], vc[c][2 * z + 1], vscale[c]);
                     *reinterpret_cast<int4v*>(&(sl ? k_odd : k_even)[kq(r, cc + 8 * z)]) = k4;
                     *reinterpret_cast<int4v*>(&(sl ? v_odd : v_even)[kq(r, cc + 8 * z)]) = v4;
                 }
@@ -1083,16 +1109,16 @@ __global__ __launch_bounds__(NT_ATT / QT) __attribute__((amdgpu_waves_per_eu(4 /
         constexpr int SL = decltype(SLOT)::value;
         if constexpr (!E4M3) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's copies of the block
         lds_barrier();   // everyone's; the other slot is no longer read
-        cur = nxt;
+        there = next_there;
         if (kb + AKB < k1) {
-            look(nxt, kb + AKB);
+            look(kb + AKB);
             issue(kb + AKB, Ic<1 - SL>{});
         }
         if (kb >= part) {
             bool found = false;
 #pragma unroll
-            for (int c = 0; c < AKB * DH / 8 / NTH; ++c) {
-                int4v* at = reinterpret_cast<int4v*>(&(SL ? v_odd : v_even)[(tid + NTH * c) * 8]);
+            for (int c = 0; c < AKB * DH / 8 / NT; ++c) {
+                int4v* at = reinterpret_cast<int4v*>(&(SL ? v_odd : v_even)[(tid + NT * c) * 8]);
                 int4v x = *at;
                 bool any = false;
 #pragma unroll
@@ -1123,61 +1149,62 @@ __global__ __launch_bounds__(NT_ATT / QT) __attribute__((amdgpu_waves_per_eu(4 /
 #pragma unroll
                     for (int u = 0; u < QT; ++u) st[u][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qf[u][i], st[u][t], 0, 0, 0);
                 }
-            const bool whole = kb + AKB <= k1 && cur.there == 15;
+            const bool whole = kb + AKB <= k1 && there == 15;
+            float fs[QT], sum[QT];   // the weights are 2^(fs x - m); a lane's sum of them
             bf16x8 pf[QT][2];
+            auto weigh = [&](int u) {
+                sum[u] = 0.f;
+#pragma unroll
+                for (int kk = 0; kk < 2; ++kk) {
+                    floatx4 w[2];
+#pragma unroll
+                    for (int y = 0; y < 2; ++y)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) w[y][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[u][2 * kk + y][e], fs[u], -m[u]));
+                    pf[u][kk] = pack_bf16(w[0], w[1]);
+                    sum[u] = sum_bf16(pf[u][kk], sum[u]);   // the rounded weights, which the products take
+                }
+            };
+            bool up = false;
 #pragma unroll
             for (int u = 0; u < QT; ++u) {
-                const bool diag = !whole || kb + AKB - 1 > first[u];   // some key is masked for this tile
-                if constexpr (E4M3) {
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) st[u][t] *= cur.ks[t];
-                }
-                // bm: the block's largest scaled score of this lane's query; the weights are 2^(fs x - m)
-                float bm, fs = sl2;
-                if (!diag && sl2 >= 0.f) {
-                    bm = st[u][0][0];
-#pragma unroll
-                    for (int t = 0; t < 4; ++t)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) bm = fmaxf(bm, st[u][t][e]);
-                    bm *= sl2;
-                } else {
-                    bm = -INFINITY;
+                fs[u] = sl2;
+                if (!whole || kb + AKB - 1 > first[u]) {   // some key is masked for this tile
+                    fs[u] = 1.f;
 #pragma unroll
                     for (int t = 0; t < 4; ++t)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const int key = kb + 16 * t + 4 * lg + e;
-                            const float x = key > last[u] || key >= k1 || !((cur.there >> t) & 1) ? -INFINITY : st[u][t][e] * sl2;
-                            st[u][t][e] = x;
-                            bm = fmaxf(bm, x);
+                            st[u][t][e] = key > last[u] || key >= k1 || !((there >> t) & 1) ? -INFINITY : st[u][t][e] * sl2;
                         }
-                    fs = 1.f;
                 }
-                // the reference m moves only when a score passes it by more than 8 (weights stay below 2^8)
-                if (__builtin_amdgcn_ballot_w64(bm > m[u] + 8.f)) {
+                weigh(u);
+                up = up || sum[u] > 4096.f;
+            }
+            // The reference m has to keep up with the scores only so far that the weights stay representable: it moves when
+            // a lane's 16 weights sum to more than 2^12 (from a first m below every score: infinitely much), and only then is
+            // a maximum taken, and the block's weights formed again.
+            if (__builtin_amdgcn_ballot_w64(up)) {
+#pragma unroll
+                for (int u = 0; u < QT; ++u) {
+                    float bm = m[u];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) bm = fmaxf(bm, st[u][t][e] * fs[u]);
                     bm = fmaxf(bm, __shfl_xor(bm, 16, 64));
                     bm = fmaxf(bm, __shfl_xor(bm, 32, 64));
-                    const float mn = bm > m[u] + 8.f ? bm : m[u], a = __builtin_amdgcn_exp2f(m[u] - mn);
+                    const float a = __builtin_amdgcn_exp2f(m[u] - bm);
 #pragma unroll
                     for (int t = 0; t < NDT; ++t) oacc[u][t] *= a;
                     l[u] *= a;
-                    m[u] = mn;
+                    m[u] = bm;
+                    weigh(u);
                 }
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        st[u][t][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[u][t][e], fs, -m[u]));
-                        l[u] += st[u][t][e];
-                    }
-                if constexpr (E4M3) {
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) st[u][t] *= cur.vs[t];
-                }
-                pf[u][0] = pack_bf16(st[u][0], st[u][1]);
-                pf[u][1] = pack_bf16(st[u][2], st[u][3]);
             }
+#pragma unroll
+            for (int u = 0; u < QT; ++u) l[u] += sum[u];
 #pragma unroll
             for (int t = 0; t < NDT; ++t)
 #pragma unroll
@@ -1191,7 +1218,7 @@ __global__ __launch_bounds__(NT_ATT / QT) __attribute__((amdgpu_waves_per_eu(4 /
         if (kb + AKB < k1) stage(Ic<1 - SL>{});
     };
     if (k0 < k1) {
-        look(nxt, k0);
+        look(k0);
         issue(k0, Ic<0>{});
         stage(Ic<0>{});
     }
@@ -1290,38 +1317,39 @@ __global__ __launch_bounds__(NT) void k_attn_join(PagedParams p) {
     *reinterpret_cast<bf16x4*>(dst) = __builtin_convertvector(o * inv, bf16x4);
 }
 
-// Blocks of 128 rows have few chunks, mostly two: DH / 4 lanes a row, 32 rows (blockIdx.y) a workgroup, all loaded at once.
+// Blocks of 128 rows have few chunks, mostly two: DH / 4 lanes a row, 16 rows (blockIdx.y) a workgroup.
 template <int DH>
 __global__ __launch_bounds__(NT) void k_attn_join_tile(PagedParams p) {
-    constexpr int RB = AQ, LPR = DH / 4, NG = NT / LPR, ROWS = 32, PASS = ROWS / NG;
+    constexpr int RB = AQ, LPR = DH / 4, NG = NT / LPR, ROWS = 16, PASS = ROWS / NG;
     const int g = blockIdx.y * ROWS + threadIdx.x / LPR, c4 = 4 * (threadIdx.x % LPR);
     const int w = div_by(blockIdx.x, p.by_hkv), hk = (int)blockIdx.x - w * p.HKV;
     Item it;
     if (!find_item<RB, true>(p, w, it) || it.chunks == 1) return;
     const int rows = min(it.n * p.G - it.rb * RB, RB), chunks = it.chunks;
-    float m[PASS], sum[PASS];
+    auto slot = [&](int j, int r) { return ((long)item_of(it, j) * p.HKV + hk) * RB + r; };
+    float M[PASS], sum[PASS];
     floatx4 o[PASS];
 #pragma unroll
     for (int i = 0; i < PASS; ++i) {
-        m[i] = LOWEST;
+        M[i] = LOWEST;
         sum[i] = 0.f;
         o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+        const int r = g + i * NG;
+        for (int j = threadIdx.x % LPR; j < chunks && r < rows; j += LPR) M[i] = fmaxf(M[i], p.pml[slot(j, r)].x);
+#pragma unroll
+        for (int off = 1; off < LPR; off <<= 1) M[i] = fmaxf(M[i], __shfl_xor(M[i], off, 64));
     }
-    for (int j = 0; j < chunks; ++j) {
-        const long slot = ((long)item_of(it, j) * p.HKV + hk) * RB;
+#pragma unroll 8
+    for (int j = 0; j < chunks; ++j)
 #pragma unroll
         for (int i = 0; i < PASS; ++i) {
-            const int r = g + i * NG;
-            if (r < rows) {
-                const float2 ml = p.pml[slot + r];
-                const floatx4 y = f4(p.po + (slot + r) * DH + c4);
-                const float M = fmaxf(m[i], ml.x), a = __builtin_amdgcn_exp2f(m[i] - M), w = __builtin_amdgcn_exp2f(ml.x - M);
-                sum[i] = sum[i] * a + w * ml.y;
-                o[i] = o[i] * a + w * y;
-                m[i] = M;
-            }
+            const int r = min(g + i * NG, rows - 1);   // (rows past the block's are not written)
+            const float2 ml = p.pml[slot(j, r)];
+            const floatx4 y = f4(p.po + slot(j, r) * DH + c4);
+            const float w = __builtin_amdgcn_exp2f(ml.x - M[i]);
+            sum[i] += w * ml.y;
+            o[i] += w * y;
         }
-    }
 #pragma unroll
     for (int i = 0; i < PASS; ++i) {
         const int r = g + i * NG, rr = it.rb * RB + r;
