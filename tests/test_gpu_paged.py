@@ -332,6 +332,79 @@ def test_rising_scores(cache):
     pc.check_attention(o, q, kc, table, lens, None, None, "rising")
 
 
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("n,new", [(32, 1), (8, 17)])
+def test_many_pages_uncut(cache, n, new):
+    """Enough sequences and heads that no sequence is cut: walks over more than 64 pages of 16 tokens, in both kernels."""
+    lens = [3000] + [int(x) for x in np.random.default_rng(n).integers(new, 200, n - 1)]
+    assert gdn.gdn_attention_paged_workspace_bytes(n, new, 64, 64, 64, 16, 189) == 0
+    _run_attention("many pages %d" % n, cache, 16, 64, 64, 64, lens, [new] * n, seed=n)
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("new", [1, 5, 40, 200])
+def test_one_long_sequence_is_cut(cache, new):
+    """A long sequence among short ones, over many chunks (whose walks pass 64 pages of 16 tokens)."""
+    need = gdn.gdn_attention_paged_workspace_bytes(3, new, 4, 1, 128, 16, 1300)
+    assert need > 0
+    _run_attention("cut %d" % new, cache, 16, 128, 4, 1, [20000 + new, new, 1500], [new] * 3, seed=70 + new)
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_scales_that_are_no_powers_of_two(new):
+    """Scales that gdn_kv_append does not make.  Many rows' kernel rounds code x scale to bf16, keys off by 2^-8 of themselves: a
+    score by d = 2^-8 sum |q k| scale at most, weights by e^2d - 1; values by 2^-8 more."""
+    print("case: odd scales", new, flush=True)
+    q, kc, table, lens, _ = _attention_case("e4m3", 32, 128, 4, 2, [300, 90], [new] * 2, seed=25)
+    g = torch.Generator().manual_seed(3)
+    for i in (2, 3):
+        kc[i].mul_((1 + torch.rand(kc[i].shape, generator=g)).cuda())
+    o = pc.attend(q, kc, table, lens)
+    H, d = q.shape[2:]
+    k = pc.values(kc[0].float().nan_to_num(), kc[2])
+    args = f64(table).astype(int), f64(lens).astype(int), None, *q.shape[:2], d ** -0.5
+    ref, a = paged.attention(f64(q).reshape(-1, H, d), k, pc.values(kc[1].float().nan_to_num(), kc[3]), *args)
+    most = np.abs(k).max((2,)).max(0)                                # [H_kv, d]
+    delta = 2.0 ** -8 * (np.abs(f64(q).reshape(-1, H, d)) * np.repeat(most, H // 2, 0)).sum(-1, keepdims=True) * d ** -0.5
+    off = np.abs(f64(o).reshape(ref.shape) - ref) / (((np.exp(2 * delta) - 1) + 4.5 * 2.0 ** -8) * a)
+    print("  largest error %.3f of the bound" % off.max())
+    assert (off <= 1).all()
+    if new == 1:
+        pc.check_attention(o, q, (kc[0].float().nan_to_num().to(kc[0].dtype), kc[1].float().nan_to_num().to(kc[1].dtype), kc[2], kc[3]),
+                           table, lens, None, None, "odd scales, few rows")
+
+
+@pytest.mark.parametrize("cache,new", [("bf16", 1), ("e4m3", 1), ("bf16", 40), ("e4m3", 40)])
+def test_a_cache_past_32_bits(cache, new):
+    """Pages whose bytes and elements lie past 2^32 and 2^31: appended to and read like any other."""
+    H, Hkv, d, page, lens = 4, 2, 128, 64, [200, 64, 77]
+    size = 2 if cache == "bf16" else 1
+    n_pages = (2 ** 32 + 2 ** 28) // (Hkv * page * d)
+    print("case: large cache", cache, new, n_pages, flush=True)
+    kind = torch.bfloat16 if cache == "bf16" else torch.float8_e4m3fn
+    big = [torch.empty(n_pages * Hkv * page * d * size, dtype=torch.uint8, device="cuda").view(kind).view(n_pages, Hkv, page, d)
+           for _ in range(2)]
+    assert big[0].numel() > 2 ** 32
+    scales = [torch.full((n_pages, Hkv), 1.0, device="cuda") if size == 1 else None for _ in range(2)]
+    table, few = pc.pages_for(lens, page, 5, extra=0)
+    small = cuda(*pc.make_cache(few, Hkv, page, d, cache, 6))        # the same pages at small numbers
+    high = np.where(table >= 0, table + n_pages - few, -1).astype(np.int32)
+    for i in range(2):
+        big[i][n_pages - few:] = small[i]
+        if size == 1:
+            scales[i][n_pages - few:] = small[2 + i]
+    q, k, v = _fused(7, 3, new, [H, Hkv, Hkv], d, torch.bfloat16)
+    at = torch.tensor(lens, dtype=torch.int32).cuda()
+    outs = []
+    for c, tab in ((small, table), (big + scales, high)):
+        tab = torch.from_numpy(tab).cuda()
+        qt = gdn.gdn_kv_append(k, v, c[0], c[1], tab, at, q=q, k_scale=c[2], v_scale=c[3], inv_freq=pc.freqs(64).cuda())
+        outs.append(pc.attend(qt, c, tab, at))
+    assert torch.equal(*outs)
+    for i in range(2):
+        assert torch.equal(big[i][n_pages - few:].view(torch.uint8), small[i].view(torch.uint8))
+
+
 # ------------------------------------------------------------------ together
 @pytest.mark.parametrize("cache", ["bf16", "e4m3"])
 def test_a_prompt_and_its_next_tokens(cache):

@@ -76,6 +76,20 @@ def test_attention_refuses(kw, code):
     assert _attention(**kw) == code
 
 
+def test_workspace():
+    """Needed where a sequence may be cut, never for arguments that are refused; missing, small and misaligned ones."""
+    need = gdn.gdn_attention_paged_workspace_bytes
+    sizes = dict(B=1, T=1, H=16, Hkv=8, max_pages=500)
+    n = need(1, 1, 16, 8, 128, 64, 500)
+    assert n > 0 and need(1, 1, 16, 8, 128, 64, 1) == 0 and need(4096, 1, 16, 8, 128, 64, 500) == 0
+    assert need(1, 64, 16, 8, 128, 64, 500, 8) > 0 and need(1, 2048, 16, 8, 128, 64, 500) > 0
+    for bad in [(0, 1, 16, 8, 128, 64, 500), (1, 1, 16, 3, 128, 64, 500), (1, 1, 16, 8, 96, 64, 500), (1, 1, 16, 8, 128, 0, 500),
+                (2, 1, 16, 8, 128, 64, 500, 2), (1, 1, 16, 8, 128, 64, 0), (1, 0, 16, 8, 128, 64, 500)]:
+        assert need(*bad) == 0, bad
+    assert _attention(**sizes) == 3 and _attention(**sizes, ws=A, ws_bytes=n - 1) == 3
+    assert _attention(**sizes, ws=A + 16, ws_bytes=n) == INVALID
+
+
 def test_nothing_to_do():
     assert _norm(T=0, q=None, qo=None) == 0 and _append(T=0, k=None) == 0 and _attention(T=0, q=None) == 0
 
