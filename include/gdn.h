@@ -438,7 +438,8 @@ gdn_status gdn_qk_norm_rope(const void* q, const void* k, void* q_out, void* k_o
  *                     page that is not there: appending writes nothing to it, attention leaves
  *                     its keys out.  So are positions from max_pages * page on.
  *   seq_lens          [n] int32 DEVICE: tokens of each sequence with this step's new ones (n = B
- *                     or n_seqs): the i-th of m new tokens stands at position seq_lens[s] - m + i
+ *                     or n_seqs; a negative one counts as 0): the i-th of m new tokens stands at position
+ *                     seq_lens[s] - m + i; a position below 0 has no page and sees no key
  *   cu_seqlens, n_seqs  the new tokens packed as in gdn_attention_prefill (a padded batch: T rows
  *                     of which cu_seqlens[n_seqs] are used; rows behind the last sequence are
  *                     neither read nor written), or NULL and 0: T new tokens for each of B sequences

@@ -3172,16 +3172,18 @@ void rows_split(RowsParams& p, int rows, int dh) {
 }
 long rows_wgs(const RowsParams& p) { return (p.tokens * p.units + NT / 64 - 1) / (NT / 64); }
 
+// Workgroups of NT threads that a launch can have (2^32 threads).
+bool grid_fits(long wgs) { return wgs < (1L << 32) / NT; }
+
 template <typename IO, bool E4M3 = false>
-void launch_rows(RowsParams p, int d, hipStream_t st) {
-    rows_split(p, p.H * (p.q != nullptr) + p.HKV * ((p.k != nullptr) + (p.v != nullptr)), d);
+void launch_rows(const RowsParams& p, int d, hipStream_t st) {
     const dim3 grid((unsigned)rows_wgs(p));
     if (d == 128) hipLaunchKernelGGL((k_rows<IO, 128, E4M3, 2>), grid, dim3(NT), 0, st, p);
     else hipLaunchKernelGGL((k_rows<IO, 64, E4M3, 2>), grid, dim3(NT), 0, st, p);
 }
 
 template <int DH, int IT>
-void launch_append_e4m3(const RowsParams& p, int row_wgs, long pages, int each, hipStream_t st) {
+void launch_append_e4m3(const RowsParams& p, long row_wgs, long pages, int each, hipStream_t st) {
     hipLaunchKernelGGL((k_append_e4m3<DH, IT>), dim3((unsigned)(row_wgs + pages * p.HKV * 2)), dim3(NT), 0, st, p,
                        (int)(pages * p.HKV * 2), each);
 }
@@ -3878,6 +3880,8 @@ extern "C" gdn_status gdn_qk_norm_rope(const void* q, const void* k, void* q_out
     p.pos = positions;
     p.t.freq = inv_freq; p.t.rot = rot; p.t.near = (flags & GDN_ROPE_INTERLEAVED) != 0; p.t.eps = eps;
     p.s.cu = cu_seqlens; p.s.n = n_seqs > 0 ? n_seqs : B; p.s.T = T;
+    rows_split(p, H + H_kv, d);
+    if (!grid_fits(rows_wgs(p))) return fail(GDN_ERR_UNSUPPORTED, "B*T*(H+H_kv) too large");
     hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
     (void)hipGetLastError();
     if (io_dtype == GDN_BF16) launch_rows<bf16_t>(p, d, hs);
@@ -3917,25 +3921,23 @@ extern "C" gdn_status gdn_kv_append(const void* q, const void* k, const void* v,
     p.s.cu = cu_seqlens; p.s.lens = seq_lens; p.s.n = n_seqs > 0 ? n_seqs : B; p.s.T = T;
     p.c = make_cache(k_cache, v_cache, k_scale, v_scale, block_table, page, n_pages, max_pages);
     hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
-    if (cache_dtype == GDN_BF16) {
+    if (cache_dtype == GDN_BF16 || (n_seqs == 0 && T == 1)) {
+        rows_split(p, (q ? H : 0) + 2 * H_kv, d);
+        if (!grid_fits(rows_wgs(p))) return fail(GDN_ERR_UNSUPPORTED, "B*T*(H+2*H_kv) too large");
         (void)hipGetLastError();
-        launch_rows<bf16_t>(p, d, hs);
-        return launched();
-    }
-    if (n_seqs == 0 && T == 1) {
-        (void)hipGetLastError();
-        launch_rows<bf16_t, true>(p, d, hs);
+        if (cache_dtype == GDN_BF16) launch_rows<bf16_t>(p, d, hs);
+        else launch_rows<bf16_t, true>(p, d, hs);
         return launched();
     }
     // pages that the new tokens can touch: n tokens lie in at most (n - 1) / page + 2
     const int each = (int)(((long)T + page - 2) / page + 1);
     const long pages = n_seqs > 0 ? (long)T / page + 2L * n_seqs : (long)B * each;
-    int row_wgs = 0;
+    long row_wgs = 0;
     if (q) {
         rows_split(p, H, d);
-        row_wgs = (int)rows_wgs(p);
+        row_wgs = rows_wgs(p);
     }
-    if (row_wgs + pages * H_kv * 2 >= (1L << 31)) return fail(GDN_ERR_UNSUPPORTED, "B*T*H_kv too large");
+    if (!grid_fits(row_wgs + pages * H_kv * 2)) return fail(GDN_ERR_UNSUPPORTED, "B*T*H_kv too large");
     (void)hipGetLastError();
     if (d == 128) {
         if (page == 16) launch_append_e4m3<128, 1>(p, row_wgs, pages, each, hs);
@@ -3986,6 +3988,7 @@ extern "C" gdn_status gdn_attention_paged(const void* q, const void* k_cache, co
     p.s.cu = cu_seqlens; p.s.lens = seq_lens; p.s.n = n_seqs > 0 ? n_seqs : B; p.s.T = T;
     p.c = make_cache(k_cache, v_cache, k_scale, v_scale, block_table, page, n_pages, max_pages);
     const PagedPlan plan = paged_plan(B, T, H, H_kv, page, max_pages, n_seqs);
+    if (!grid_fits(plan.items * H_kv)) return fail(GDN_ERR_UNSUPPORTED, "B*T*H too large");
     const PagedLayout lay = paged_layout(plan, H_kv, d);
     p.items = (int)plan.items; p.round = plan.round; p.fine = plan.fine; p.spare = plan.spare;
     p.pml = reinterpret_cast<float2*>(workspace);

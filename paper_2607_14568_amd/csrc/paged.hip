@@ -8,7 +8,7 @@
 // ------------------------------------------------------------------ sequences of a step
 struct StepSeqs {
     const int32_t* cu;    // packed: offsets [n + 1] of the new tokens; null: T tokens each
-    const int32_t* lens;  // tokens with the new ones [n]; null: no cache (positions from 0)
+    const int32_t* lens;  // tokens with the new ones [n] (below 0 as 0); null: no cache (positions from 0)
     int n, T;             // sequences; tokens of a dense sequence (packed: of the call)
 };
 
@@ -267,7 +267,7 @@ __device__ __forceinline__ void token_rows(const RowsParams& p, long wave, Angle
     if (tok >= p.tokens) return;
     int s = 0, i = 0, n = 0;
     if (!step_seq(p.s, (int)tok, s, i, n)) return;
-    const int pos = p.pos ? p.pos[tok] : p.s.lens ? p.s.lens[s] - n + i : i;
+    const int pos = p.pos ? p.pos[tok] : p.s.lens ? max(p.s.lens[s], 0) - n + i : i;
     float cs[8], sn[8];
     if (p.t.freq) {
         if (lane < p.t.rot / 2) angle(p.t, lane, pos, tab.c[lane], tab.s[lane]);
@@ -348,7 +348,7 @@ __device__ __forceinline__ bool touched_block(const StepSeqs& q, int shift, int 
                                               int& row) {
     if (!q.cu) {
         s = block / each;
-        len = tab(q.lens, s);
+        len = max(tab(q.lens, s), 0);
         first = max(len - q.T, 0);   // (a token before position 0 is not written)
         b = (first >> shift) + block % each;
         row = s * q.T + q.T - (len - first);
@@ -358,7 +358,7 @@ __device__ __forceinline__ bool touched_block(const StepSeqs& q, int shift, int 
     int at = 0, beg, end, before = 0;
     for (int base = 0; base < q.n; base += 64) {
         span64(q, base, at, beg, end);
-        const int L = base + lane < q.n ? q.lens[base + lane] : 0;
+        const int L = base + lane < q.n ? max(q.lens[base + lane], 0) : 0;
         const int f = max(L - (end - beg), 0);
         const int cnt = end > beg && L > 0 ? ((L - 1) >> shift) - (f >> shift) + 1 : 0;
         const int sum = scan_add(cnt);
@@ -534,9 +534,9 @@ template <int RB, bool BLOCK = false> __device__ __forceinline__ bool find_item(
     int beg, end, L, nrb, units;   // of sequence base + lane
     auto load = [&](int base, int& at) {
         span64(p.s, base, at, beg, end);
-        L = base + lane < p.s.n ? p.s.lens[base + lane] : 0;
+        L = base + lane < p.s.n ? max(p.s.lens[base + lane], 0) : 0;
         nrb = ((end - beg) * p.G + RB - 1) / RB;
-        units = max((min(max(L, 0), cap) + UNIT - 1) / UNIT, 1);
+        units = max((min(L, cap) + UNIT - 1) / UNIT, 1);
     };
     int at = 0, c = 1 << 23;   // (2^30 keys, the most a table holds)
     if (p.spare > 0) {
@@ -624,9 +624,11 @@ template <bool SCALED> struct PageWalk {
         id = b + lane < p.c.max_pages ? row[b + lane] : -1;
         if (id < 0 || id >= p.c.n_pages) id = -1;
         if constexpr (SCALED) {
-            const long at = (long)max(id, 0) * p.HKV + hk;
-            ks = p.c.ks[at];
-            vs = p.c.vs[at];
+            ks = vs = 1.f;
+            if (id >= 0) {
+                ks = p.c.ks[(long)id * p.HKV + hk];
+                vs = p.c.vs[(long)id * p.HKV + hk];
+            }
         }
     }
     __device__ __forceinline__ void reach(const PagedParams& p, int hk, int b, int b_last) {   // up to 64 pages b .. b_last
@@ -793,9 +795,9 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
             const int key = kb + 16 * t, b = key >> p.c.shift;
             const int id = key < k1 ? walk.page(b) : -1;
             x.there[t] = id >= 0;
-            if constexpr (E4M3) {
-                x.ks[t] = walk.kscale(b);
-                x.vs[t] = walk.vscale(b);
+            if constexpr (E4M3) {   // (a page that holds none of the item's keys may have any scale)
+                x.ks[t] = id >= 0 ? walk.kscale(b) : 1.f;
+                x.vs[t] = id >= 0 ? walk.vscale(b) : 1.f;
             }
             const long at = ((((long)max(id, 0) * p.HKV + hk) << p.c.shift) + (key & (p.c.page - 1))) * DH * ESZ;
             const uint32_t bytes = id >= 0 ? (uint32_t)min(k1 - key, 16) * DH * ESZ : 0;   // rows past the item's read as zeros
@@ -1018,9 +1020,9 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2))) void k_
     auto describe = [&](int kb, int r, __amdgpu_buffer_rsrc_t& rk, __amdgpu_buffer_rsrc_t& rv, float& ks, float& vs) {
         const int g = p.c.page >= AKB ? 0 : r & ~15, span = p.c.page >= AKB ? AKB : 16, key = kb + g;
         const int id = key < k1 ? walk.page(key >> p.c.shift) : -1;
-        if constexpr (E4M3) {
-            ks = walk.kscale(key >> p.c.shift);
-            vs = walk.vscale(key >> p.c.shift);
+        if constexpr (E4M3) {   // (a page that holds none of the item's keys may have any scale)
+            ks = id >= 0 ? walk.kscale(key >> p.c.shift) : 1.f;
+            vs = id >= 0 ? walk.vscale(key >> p.c.shift) : 1.f;
         }
         const long at = (((((long)max(id, 0) * p.HKV + hk) << p.c.shift) + (key & (p.c.page - 1))) - g) * DH * ESZ;
         const uint32_t bytes = id >= 0 ? (uint32_t)(g + min(k1 - key, span)) * DH * ESZ : 0;

@@ -285,6 +285,51 @@ def test_pages_that_are_not_there(cache, new):
     assert not o[2].any()
 
 
+@pytest.mark.parametrize("page", [16, 32, 128])
+@pytest.mark.parametrize("new", [1, 5, 40, 100])
+def test_pages_ahead_hold_anything(page, new):
+    """Pages that hold none of a sequence's keys, page 0 and one that the table already names among them, with scales and codes
+    that are not numbers."""
+    print("case: pages ahead", page, new, flush=True)
+    lens = [max(new, 7), new + page, 3 * page + 3, 2 * page + 16]
+    q, kc, table, at, _ = _attention_case("e4m3", page, 64, 4, 2, lens, [new] * 4, seed=12)
+    used = {int(x) for s, L in enumerate(lens) for x in table[s, :-(-L // page)]}
+    free = [i for i in range(kc[0].shape[0]) if i not in used]
+    if 0 in used:                                       # page 0 changes places with a free one
+        for t in kc:
+            t.view(torch.uint8 if t.dtype is torch.float8_e4m3fn else t.dtype)[free[0]] = \
+                t.view(torch.uint8 if t.dtype is torch.float8_e4m3fn else t.dtype)[0].clone()
+        table[table == 0] = free[0]
+        free[0] = 0
+    for i in free:
+        kc[0][i], kc[1][i], kc[2][i], kc[3][i] = float("nan"), float("nan"), float("inf"), float("nan")
+    for s, L in enumerate(lens):
+        table[s, -(-L // page):] = free[1]
+    o = pc.attend(q, kc, table, at)
+    pc.check_attention(o, q, kc, table, at, None, None, "pages ahead")
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("new", [1, 3])
+def test_lengths_that_are_none(cache, new):
+    """The lowest and the highest numbers as lengths: nothing is written, rows of no key are zeros."""
+    print("case: lengths", cache, new, flush=True)
+    lens = [-2 ** 31, 2 ** 31 - 1, 0]
+    q, kc, table, _, _ = _attention_case(cache, 16, 64, 4, 2, [20] * 3, [new] * 3, seed=13)
+    at = torch.tensor(lens, dtype=torch.int32).cuda()
+    before = [None if t is None else t.clone() for t in kc]
+    k = normal(14, 3, new, 2, 64).cuda()
+    gdn.gdn_kv_append(k, k, kc[0], kc[1], table, at, k_scale=kc[2], v_scale=kc[3])
+    for x, y in zip(before, kc):
+        assert x is None or torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+    for i in range(2):
+        kc[i] = kc[i].float().nan_to_num().to(kc[i].dtype)
+    o = torch.full_like(q, 7.0)
+    pc.attend(q, kc, table, at, o=o)
+    pc.check_attention(o, q, kc, table, torch.tensor([0, 2 ** 31 - 1, 0]), None, None, "lengths")
+    assert not o[0].any() and not o[2].any()
+
+
 @pytest.mark.parametrize("new", [1, 40])
 @pytest.mark.parametrize("scale", [0.0, -0.2, 2.0])
 def test_scales(scale, new):
