@@ -1276,7 +1276,6 @@ template <int DH>
 __global__ __launch_bounds__(NT) void k_attn_join(PagedParams p) {
     constexpr int RB = 16, LPR = DH / 4, SUB = 64 / LPR, NW = NT / 64;   // lanes per row; chunks that a wave's load takes at once
     __shared__ __align__(16) float red[NW][DH];
-    __shared__ float reds[NW];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int w = div_by(blockIdx.x, p.by_hkv), hk = (int)blockIdx.x - w * p.HKV, c4 = 4 * (lane % LPR), r = blockIdx.y;
     Item it;
@@ -1284,35 +1283,45 @@ __global__ __launch_bounds__(NT) void k_attn_join(PagedParams p) {
     const int rr = it.rb * RB + r, chunks = it.chunks;
     if (rr >= it.n * p.G) return;
     auto slot = [&](int j) { return ((long)item_of(it, j) * p.HKV + hk) * RB + r; };
+    constexpr int EACH = 64 / (NW * SUB);   // loads of a wave for 64 chunks, all sent off before the first is used
+    const int mine = wave * SUB + lane / LPR;
     float M = LOWEST, sum = 0.f;
-    for (int j0 = 0; j0 < chunks; j0 += 64) M = fmaxf(M, j0 + lane < chunks ? p.pml[slot(j0 + lane)].x : LOWEST);
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
     floatx4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int j = wave * SUB + lane / LPR; j < chunks; j += NW * SUB) {
-        const float2 ml = p.pml[slot(j)];
-        const float w = __builtin_amdgcn_exp2f(ml.x - M);
-        sum += w * ml.y;
-        o += w * f4(p.po + slot(j) * DH + c4);
+    for (int j0 = 0; j0 < chunks; j0 += 64) {
+        floatx4 y[EACH];
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            const int j = j0 + k * NW * SUB + mine;
+            y[k] = floatx4{0.f, 0.f, 0.f, 0.f};
+            if (j < chunks) y[k] = f4(p.po + slot(j) * DH + c4);
+        }
+        float2 ml = {LOWEST, 0.f};   // of chunk j0 + lane
+        if (j0 + lane < chunks) ml = p.pml[slot(j0 + lane)];
+        float top = fmaxf(M, ml.x);
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+        const float a = __builtin_amdgcn_exp2f(M - top), w = __builtin_amdgcn_exp2f(ml.x - top);
+        sum = sum * a + w * ml.y;
+        o *= a;
+        M = top;
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            const float z = __shfl(w, k * NW * SUB + mine, 64);
+            if (j0 + k * NW * SUB + mine < chunks) o += z * y[k];
+        }
     }
 #pragma unroll
-    for (int off = LPR; off < 64; off <<= 1) {
-        sum += __shfl_xor(sum, off, 64);
+    for (int off = 1; off < 64; off <<= 1) sum += __shfl_xor(sum, off, 64);   // (in every wave)
+#pragma unroll
+    for (int off = LPR; off < 64; off <<= 1)
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], off, 64);
-    }
     if (lane < LPR) *reinterpret_cast<floatx4*>(&red[wave][c4]) = o;
-    if (lane == 0) reds[wave] = sum;
     __syncthreads();
     if (wave != 0 || lane >= LPR) return;
-    sum = reds[0];
     o = f4(&red[0][c4]);
 #pragma unroll
-    for (int w = 1; w < NW; ++w) {
-        sum += reds[w];
-        o += f4(&red[w][c4]);
-    }
+    for (int z = 1; z < NW; ++z) o += f4(&red[z][c4]);
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     const int i = div_by(rr, p.by_g);
     bf16_t* dst = p.o + ((long)(it.tok + i) * p.H + hk * p.G + rr - i * p.G) * DH + c4;
