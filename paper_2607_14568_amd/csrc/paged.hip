@@ -82,8 +82,9 @@ struct Turn {
 // cos and sin of pos * freq[i]: the angle in float64 (a float32 product is off by 2^-24 of an angle of up to 10^5 radians),
 // in half turns, reduced to within one and rounded (2^-25 half turns, 2^-23.3 radians).  (The sine unit takes turns and is off
 // by 2^-22.9, against 2^-24.3; with it a prompt's rows in an e4m3 cache are 4 % faster, the others the same.)
-__device__ __forceinline__ void angle(const Turn& t, int i, double pos, float& cs, float& sn) {
-    double a = pos * t.freq[i] * 0.15915494309189535;
+__device__ __forceinline__ double turns(const Turn& t, int i) { return t.freq[i] * 0.15915494309189535; }   // per position
+__device__ __forceinline__ void angle(double turns, double pos, float& cs, float& sn) {
+    double a = pos * turns;
     a -= rint(a);
     sincospif((float)(2 * a), &sn, &cs);
 }
@@ -110,8 +111,24 @@ __device__ __forceinline__ void angles(const Turn& t, int c, const float* tc, co
     }
 }
 
+// x from another lane of the 16 of its DPP row
+template <int CTRL> __device__ __forceinline__ float dpp(float x) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+constexpr int XOR1 = 0xb1, XOR2 = 0x4e, REVERSE4 = 0x1b, MIRROR8 = 0x141, MIRROR16 = 0x140, ROTATE8 = 0x128;
+// sums and maxima over LPR = 8 or 16 neighbouring lanes, in each of them
+template <int LPR, typename F> __device__ __forceinline__ float over_row(float x, F f) {
+    x = f(x, dpp<XOR1>(x));
+    x = f(x, dpp<XOR2>(x));
+    x = f(x, dpp<MIRROR8>(x));
+    if constexpr (LPR == 16) x = f(x, dpp<MIRROR16>(x));
+    return x;
+}
+
 // x: this lane's 8 channels; w: their weights or null; cs, sn: from angles() (used when t.freq).  y = x w / sqrt(mean(x^2)
-// + eps), then (a, b) -> (a cos - b sin, b cos + a sin) over the pairs: every channel is x cs + partner sn.
+// + eps), then (a, b) -> (a cos - b sin, b cos + a sin) over the pairs: every channel is x cs + partner sn.  (Lanes exchange
+// through DPP; by ds_bpermute a prompt of 4133 tokens took
+// 18.4 us into an e4m3 cache, 17.2 so.)
 template <int DH>
 __device__ __forceinline__ void turn_row(const Turn& t, const float* w, const float (&cs)[8], const float (&sn)[8], float (&x)[8]) {
     constexpr int LPR = DH / 8;
@@ -120,18 +137,32 @@ __device__ __forceinline__ void turn_row(const Turn& t, const float* w, const fl
         float ss = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) ss += x[e] * x[e];
-#pragma unroll
-        for (int off = 1; off < LPR; off <<= 1) ss += __shfl_xor(ss, off, 64);
+        ss = over_row<LPR>(ss, [](float a, float b) { return a + b; });
         const float r = 1.f / sqrtf(ss * (1.f / DH) + t.eps);
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] *= r * w[8 * c + e];
     }
     if (t.freq) {
-        const int hc = t.rot / 16;
-        const int from = t.near ? lane : c < hc ? lane + hc : c < 2 * hc ? lane - hc : lane;
+        const int hc = t.rot / 16;   // partners are hc lanes apart
         float y[8];
+        if (t.near) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = t.near ? x[e ^ 1] : __shfl(x[e], from, 64);
+            for (int e = 0; e < 8; ++e) y[e] = x[e ^ 1];
+        } else if (LPR == 16 && hc == 8) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = dpp<ROTATE8>(x[e]);
+        } else if (hc == 4) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = dpp<REVERSE4>(dpp<MIRROR8>(x[e]));
+        } else {
+            const int from = c < hc ? lane + hc : c < 2 * hc ? lane - hc : lane;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = __shfl(x[e], from, 64);
+        }
+        if (!t.near && c >= 2 * hc) {   // (no partner: nothing of another channel, not even 0 times it)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = 0.f;
+        }
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = x[e] * cs[e] + y[e] * sn[e];
     }
@@ -269,7 +300,7 @@ __device__ __forceinline__ void token_rows(const RowsParams& p, long wave, Angle
     const int pos = p.pos ? p.pos[tok] : p.s.lens ? max(p.s.lens[s], 0) - n + i : i;
     float cs[8], sn[8];
     if (p.t.freq) {
-        if (lane < p.t.rot / 2) angle(p.t, lane, pos, tab.c[lane], tab.s[lane]);
+        if (lane < p.t.rot / 2) angle(turns(p.t, lane), pos, tab.c[lane], tab.s[lane]);
         __builtin_amdgcn_wave_barrier();   // (the wave's LDS accesses stay in order)
         angles(p.t, c, tab.c, tab.s, cs, sn);
     }
@@ -311,8 +342,7 @@ __device__ __forceinline__ void token_rows(const RowsParams& p, long wave, Angle
                 float amax = 0.f;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[e]) <= -LOWEST ? fabsf(x[e]) : 0.f);
-#pragma unroll
-                for (int off = 1; off < LPR; off <<= 1) amax = fmaxf(amax, __shfl_xor(amax, off, 64));
+                amax = over_row<LPR>(amax, [](float a, float b) { return fmaxf(a, b); });
                 uint8_t* codes = (uint8_t*)(kind == 1 ? p.c.k : p.c.v) + at;
                 float* ps = (kind == 1 ? p.c.ks : p.c.vs) + (long)id * p.HKV + h;
                 float scale = power_scale(amax);
@@ -411,9 +441,14 @@ __global__ __launch_bounds__(NT) void k_append_e4m3(RowsParams p, int page_wgs, 
     float x[IT][8], amax = 0.f;
     if (!is_v) {
         const int np = p.t.rot / 2;
-        for (int z = tid; z < (RPP + IT) * np; z += NT) {
-            const int i = z / np, j = z % np;
-            angle(p.t, j, i < RPP ? i : at0 + (i - RPP) * RPP, tc[i][j], ts[i][j]);
+        const int j = tid % NP;
+        if (j < np) {
+            const double f = turns(p.t, j);
+#pragma unroll
+            for (int i = 0; i < RPP + IT; i += NT / NP) {
+                const int r = i + tid / NP;
+                if (r < RPP + IT) angle(f, r < RPP ? r : at0 + (r - RPP) * RPP, tc[r][j], ts[r][j]);
+            }
         }
         __syncthreads();
         float cs[8], sn[8];
@@ -445,8 +480,7 @@ __global__ __launch_bounds__(NT) void k_append_e4m3(RowsParams p, int page_wgs, 
             const float m = fabsf(x[it][e]);
             amax = fmaxf(amax, m <= -LOWEST ? m : 0.f);
         }
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) amax = fmaxf(amax, __shfl_xor(amax, off, 64));
+    amax = __builtin_bit_cast(float, last_lane(scan_max(__builtin_bit_cast(int, amax))));   // (0 or more: in order as integers)
     if ((tid & 63) == 0) red[wave] = amax;
     __syncthreads();
     amax = red[0];
