@@ -159,7 +159,7 @@ __device__ __forceinline__ void turn_row(const Turn& t, const float* w, const fl
 #pragma unroll
             for (int e = 0; e < 8; ++e) y[e] = __shfl(x[e], from, 64);
         }
-        if (!t.near && c >= 2 * hc) {   // (no partner: nothing of another channel, not even 0 times it)
+        if (8 * c >= t.rot) {   // (no partner: nothing of another channel, not even 0 times it)
 #pragma unroll
             for (int e = 0; e < 8; ++e) y[e] = 0.f;
         }
@@ -290,13 +290,13 @@ struct RowsParams {
 struct __attribute__((aligned(16))) AngleTable { float c[64], s[64]; };
 
 template <typename IO, int DH, bool E4M3, int AHEAD, bool QONLY = false>
-__device__ __forceinline__ void token_rows(const RowsParams& p, long wave, AngleTable& tab) {
+__device__ __forceinline__ void token_rows(const RowsParams& p, int wave, AngleTable& tab) {
     constexpr int LPR = DH / 8, RPG = 64 / LPR;
-    const long tok = wave / p.units;
-    const int unit = (int)(wave % p.units), lane = threadIdx.x & 63, c = lane % LPR;
-    if (tok >= p.tokens) return;
+    const int token = wave / p.units, unit = wave - token * p.units, lane = threadIdx.x & 63, c = lane % LPR;
+    if (token >= p.tokens) return;
+    const long tok = token;
     int s = 0, i = 0, n = 0;
-    if (!step_seq(p.s, (int)tok, s, i, n)) return;
+    if (!step_seq(p.s, token, s, i, n)) return;
     const int pos = p.pos ? p.pos[tok] : p.s.lens ? max(p.s.lens[s], 0) - n + i : i;
     float cs[8], sn[8];
     if (p.t.freq) {
@@ -309,56 +309,56 @@ __device__ __forceinline__ void token_rows(const RowsParams& p, long wave, Angle
     const int slot = pos & (p.c.page - 1);
     // AHEAD groups' rows are loaded before the first is used
     for (int g0 = 0; g0 < p.per; g0 += AHEAD) {
-    Chunk8<IO> in[AHEAD];
+        Chunk8<IO> in[AHEAD];
 #pragma unroll
-    for (int z = 0; z < AHEAD; ++z) {
-        const int j = (unit * p.per + g0 + z) * RPG + lane / LPR;
-        const IO* src = QONLY || j < HQ ? (const IO*)p.q + tok * p.qs + j * DH
-                        : j < HQ + p.HKV ? (const IO*)p.k + tok * p.ks + (j - HQ) * DH
-                                         : (const IO*)p.v + tok * p.vs + (j - HQ - p.HKV) * DH;
-        in[z].zero();
-        if (g0 + z < p.per && j < rows) in[z].load(src + 8 * c);
-    }
+        for (int z = 0; z < AHEAD; ++z) {
+            const int j = (unit * p.per + g0 + z) * RPG + lane / LPR;
+            const IO* src = QONLY || j < HQ ? (const IO*)p.q + tok * p.qs + j * DH
+                            : j < HQ + p.HKV ? (const IO*)p.k + tok * p.ks + (j - HQ) * DH
+                                             : (const IO*)p.v + tok * p.vs + (j - HQ - p.HKV) * DH;
+            in[z].zero();
+            if (g0 + z < p.per && j < rows) in[z].load(src + 8 * c);
+        }
 #pragma unroll
-    for (int z = 0; z < AHEAD; ++z) {
-        const int j = (unit * p.per + g0 + z) * RPG + lane / LPR;
-        const int kind = QONLY || j < HQ ? 0 : j < HQ + p.HKV ? 1 : 2;   // q, k, v
-        const int h = kind == 0 ? j : kind == 1 ? j - HQ : j - HQ - p.HKV;
-        if (g0 + z >= p.per) break;
-        float x[8];
-        in[z].get(x);
-        // (a row's lanes share their kind, and the exchanges stay inside a row)
-        if (kind < 2) turn_row<DH>(p.t, kind == 0 ? p.qw : p.kw, cs, sn, x);
-        if (j >= rows) continue;
-        if (kind == 0) {
-            store8((IO*)p.qo + (tok * p.H + h) * DH + 8 * c, x);
-        } else if (p.ko) {
-            store8((IO*)p.ko + (tok * p.HKV + h) * DH + 8 * c, x);
-        } else if (id >= 0) {
-            const long at = (((long)id * p.HKV + h) << p.c.shift) * DH + 8 * c;   // of slot 0
-            if constexpr (!E4M3) {
-                store8((IO*)(kind == 1 ? p.c.k : p.c.v) + at + slot * DH, x);
-            } else {
-                float amax = 0.f;
+        for (int z = 0; z < AHEAD; ++z) {
+            const int j = (unit * p.per + g0 + z) * RPG + lane / LPR;
+            const int kind = QONLY || j < HQ ? 0 : j < HQ + p.HKV ? 1 : 2;   // q, k, v
+            const int h = kind == 0 ? j : kind == 1 ? j - HQ : j - HQ - p.HKV;
+            if (g0 + z >= p.per) break;
+            float x[8];
+            in[z].get(x);
+            // (a row's lanes share their kind, and the exchanges stay inside a row)
+            if (kind < 2) turn_row<DH>(p.t, kind == 0 ? p.qw : p.kw, cs, sn, x);
+            if (j >= rows) continue;
+            if (kind == 0) {
+                store8((IO*)p.qo + (tok * p.H + h) * DH + 8 * c, x);
+            } else if (p.ko) {
+                store8((IO*)p.ko + (tok * p.HKV + h) * DH + 8 * c, x);
+            } else if (id >= 0) {
+                const long at = (((long)id * p.HKV + h) << p.c.shift) * DH + 8 * c;   // of slot 0
+                if constexpr (!E4M3) {
+                    store8((IO*)(kind == 1 ? p.c.k : p.c.v) + at + slot * DH, x);
+                } else {
+                    float amax = 0.f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[e]) <= -LOWEST ? fabsf(x[e]) : 0.f);
-                amax = over_row<LPR>(amax, [](float a, float b) { return fmaxf(a, b); });
-                uint8_t* codes = (uint8_t*)(kind == 1 ? p.c.k : p.c.v) + at;
-                float* ps = (kind == 1 ? p.c.ks : p.c.vs) + (long)id * p.HKV + h;
-                float scale = power_scale(amax);
-                if (slot > 0) {
-                    const float old = *ps;
-                    if (old >= scale) {
-                        scale = old;
-                    } else {
-                        rescale<4>(codes, DH, 0, slot, 1, old / scale);
+                    for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[e]) <= -LOWEST ? fabsf(x[e]) : 0.f);
+                    amax = over_row<LPR>(amax, [](float a, float b) { return fmaxf(a, b); });
+                    uint8_t* codes = (uint8_t*)(kind == 1 ? p.c.k : p.c.v) + at;
+                    float* ps = (kind == 1 ? p.c.ks : p.c.vs) + (long)id * p.HKV + h;
+                    float scale = power_scale(amax);
+                    if (slot > 0) {
+                        const float old = *ps;
+                        if (old >= scale) {
+                            scale = old;
+                        } else {
+                            rescale<4>(codes, DH, 0, slot, 1, old / scale);
+                        }
                     }
+                    *reinterpret_cast<uint64_t*>(codes + slot * DH) = to_e4m3(x, 1.f / scale);
+                    if (c == 0) *ps = scale;
                 }
-                *reinterpret_cast<uint64_t*>(codes + slot * DH) = to_e4m3(x, 1.f / scale);
-                if (c == 0) *ps = scale;
             }
         }
-    }
     }
 }
 
@@ -366,7 +366,7 @@ template <typename IO, int DH, bool E4M3, int AHEAD>
 __global__ __launch_bounds__(NT) void k_rows(RowsParams p) {
     __shared__ AngleTable tab[NT / 64];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    token_rows<IO, DH, E4M3, AHEAD>(p, (long)blockIdx.x * (NT / 64) + wave, tab[wave]);
+    token_rows<IO, DH, E4M3, AHEAD>(p, (int)blockIdx.x * (NT / 64) + wave, tab[wave]);
 }
 
 // ------------------------------------------------------------------ k_append_e4m3
@@ -418,11 +418,11 @@ __global__ __launch_bounds__(NT) void k_append_e4m3(RowsParams p, int page_wgs, 
     const int tid = threadIdx.x, c = tid % LPR, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     if ((int)blockIdx.x >= page_wgs) {
         static_assert(sizeof(AngleTable) * (NT / 64) <= sizeof tc, "the tables of the q rows' waves");
-        token_rows<bf16_t, DH, false, 2, true>(p, (long)((int)blockIdx.x - page_wgs) * (NT / 64) + wave, reinterpret_cast<AngleTable*>(tc)[wave]);
+        token_rows<bf16_t, DH, false, 2, true>(p, ((int)blockIdx.x - page_wgs) * (NT / 64) + wave, reinterpret_cast<AngleTable*>(tc)[wave]);
         return;
     }
     const int u = (int)blockIdx.x;
-    const int is_v = u & 1, h = u / 2 % p.HKV;
+    const int is_v = u & 1, h = u / 2 % p.HKV;   // (a page's K and V of all heads side by side)
     int s, b, first, len, row;
     if (!touched_block(p.s, p.c.shift, each, u / 2 / p.HKV, s, b, first, len, row)) return;
     const int id = __builtin_amdgcn_readfirstlane(page_of(p.c, s, b));

@@ -83,6 +83,20 @@ def test_norm_rope_special_values():
     assert not got[0, 0, 0].any() and bad.tolist() == [[False, False], [True, False], [False, True]]
 
 
+@pytest.mark.parametrize("d,rot", [(128, 64), (128, 32), (128, 16), (64, 32), (64, 16), (128, 128)])
+@pytest.mark.parametrize("near", [False, True])
+def test_rotation_stays_in_its_pairs(d, rot, near):
+    """Without a norm, a value that is not finite reaches its pair and no other channel."""
+    for at in (0, rot - 1, rot, d - 1):
+        if at >= d:
+            continue
+        q = normal(6, 1, 2, 3, d, dtype=torch.float32)
+        q[0, 1, 1, at] = float("nan")
+        got, _ = gdn.gdn_qk_norm_rope(q.cuda(), q.cuda(), inv_freq=pc.freqs(rot).cuda(), interleaved=near)
+        pair = {at} if at >= rot else {at, at ^ 1} if near else {at, (at + rot // 2) % rot}
+        assert {tuple(x) for x in torch.isnan(got).nonzero().tolist()} == {(0, 1, 1, c) for c in pair}, at
+
+
 # ------------------------------------------------------------------ gdn_kv_append
 def _append_case(cache, page, d, H, Hkv, lens, new, cu, rot, near, seed, T=None):
     n, packed = len(lens), cu is not None
