@@ -3178,8 +3178,8 @@ bool grid_fits(long wgs) { return wgs < (1L << 32) / NT; }
 template <typename IO, bool E4M3 = false>
 void launch_rows(const RowsParams& p, int d, hipStream_t st) {
     const dim3 grid((unsigned)rows_wgs(p));
-    if (d == 128) hipLaunchKernelGGL((k_rows<IO, 128, E4M3, 2>), grid, dim3(NT), 0, st, p);
-    else hipLaunchKernelGGL((k_rows<IO, 64, E4M3, 2>), grid, dim3(NT), 0, st, p);
+    if (d == 128) hipLaunchKernelGGL((k_rows<IO, 128, E4M3>), grid, dim3(NT), 0, st, p);
+    else hipLaunchKernelGGL((k_rows<IO, 64, E4M3>), grid, dim3(NT), 0, st, p);
 }
 
 template <int DH, int IT>

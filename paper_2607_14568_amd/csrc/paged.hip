@@ -79,14 +79,30 @@ struct Turn {
     float eps;
 };
 
-// cos and sin of pos * freq[i]: the angle in float64 (a float32 product is off by 2^-24 of an angle of up to 10^5 radians),
-// in half turns, reduced to within one and rounded (2^-25 half turns, 2^-23.3 radians).  (The sine unit takes turns and is off
-// by 2^-22.9, against 2^-24.3; with it a prompt's rows in an e4m3 cache are 4 % faster, the others the same.)
+// cos and sin of pos * freq[i]: the angle in float64 (a float32 product is off by 2^-24 of an angle of up to 10^5 radians), in
+// turns, reduced to a quadrant n and the rest f in [-1/2, 1/2] quarter turns, whose sine and cosine are polynomials in f^2
+// (fitted for the least largest error at those degrees: 2^-27.6 and 2^-34).  Off by at most 2^-23.6 of 1 and 2^-26 on
+// average, less than sincospif of the rounded half turns (2^-23.1, 2^-25.3), and no slower.  (The sine unit takes turns and
+// is off by 2^-22.9.)
 __device__ __forceinline__ double turns(const Turn& t, int i) { return t.freq[i] * 0.15915494309189535; }   // per position
 __device__ __forceinline__ void angle(double turns, double pos, float& cs, float& sn) {
     double a = pos * turns;
-    a -= rint(a);
-    sincospif((float)(2 * a), &sn, &cs);
+    a = 4. * (a - rint(a));
+    const float n = rintf((float)a), f = (float)(a - (double)n), u = f * f;
+    float s = -0.004602177068591118f, c = 0.0009036316769197583f;
+    s = __builtin_fmaf(s, u, 0.07968022674322128f);
+    s = __builtin_fmaf(s, u, -0.6459634900093079f);
+    s = __builtin_fmaf(s, u, -4.371139e-8f);   // pi / 2 - 1.57079637
+    s = __builtin_fmaf(f, 1.57079637f, f * s);
+    c = __builtin_fmaf(c, u, -0.02086007222533226f);
+    c = __builtin_fmaf(c, u, 0.25366920232772827f);
+    c = __builtin_fmaf(c, u, -1.2337005138397217f);
+    c = __builtin_fmaf(c, u, 1.f);
+    const int k = (int)n;   // -2 .. 2
+    sn = k & 1 ? c : s;
+    cs = k & 1 ? s : c;
+    sn = k & 2 ? -sn : sn;
+    cs = (k + 1) & 2 ? -cs : cs;
 }
 
 // cos and sin of the pairs of a chunk's 8 channels, from tables [rot / 2] of a position; the sign of the sine is that of the
@@ -127,20 +143,22 @@ template <int LPR, typename F> __device__ __forceinline__ float over_row(float x
 
 // x: this lane's 8 channels; w: their weights or null; cs, sn: from angles() (used when t.freq).  y = x w / sqrt(mean(x^2)
 // + eps), then (a, b) -> (a cos - b sin, b cos + a sin) over the pairs: every channel is x cs + partner sn.  (Lanes exchange
-// through DPP; by ds_bpermute a prompt of 4133 tokens took
-// 18.4 us into an e4m3 cache, 17.2 so.)
+// through DPP; by ds_bpermute a prompt of 4133 tokens took 18.4 us into an e4m3 cache, 17.2 so.)
 template <int DH>
-__device__ __forceinline__ void turn_row(const Turn& t, const float* w, const float (&cs)[8], const float (&sn)[8], float (&x)[8]) {
+__device__ __forceinline__ void turn_row(const Turn& t, bool norm, const float* w, const float (&cs)[8], const float (&sn)[8], float (&x)[8]) {
     constexpr int LPR = DH / 8;
     const int lane = threadIdx.x & 63, c = lane % LPR;
-    if (w) {
+    if (norm) {
         float ss = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) ss += x[e] * x[e];
         ss = over_row<LPR>(ss, [](float a, float b) { return a + b; });
-        const float r = 1.f / sqrtf(ss * (1.f / DH) + t.eps);
+        const floatx4 w0 = f4(w + 8 * c), w1 = f4(w + 8 * c + 4);
+        const float var = ss * (1.f / DH) + t.eps;
+        float r = __builtin_amdgcn_rsqf(var);   // (off by 2^-23 at most; 1 / sqrtf takes some 25 instructions)
+        if (__builtin_amdgcn_ballot_w64(var < 0x1p-126f)) r = var < 0x1p-126f ? 1.f / sqrtf(var) : r;   // (it takes those as 0)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] *= r * w[8 * c + e];
+        for (int e = 0; e < 8; ++e) x[e] *= r * (e < 4 ? w0[e] : w1[e - 4]);
     }
     if (t.freq) {
         const int hc = t.rot / 16;   // partners are hc lanes apart
@@ -268,7 +286,11 @@ template <int N> __device__ __forceinline__ void rescale(uint8_t* codes, int pit
 // One wave takes `per` groups of 64 / (DH / 8) rows of one token: its q heads, its k heads and, into a cache, its v heads
 // (those as they are); into an e4m3 cache only where a sequence has one new token, whose rows are then all there is of a
 // page's and head's new values.  Each lane forms one angle of the token's position, the wave's tables of them lie in LDS.
-// Bound by memory: every row is read once and written once.
+// Bound by memory: every row is read once and written once, a lane's 16 bytes (8 channels) an access, so that a head's row
+// lies in 8 or 16 neighbouring lanes and its norm is a sum over them by DPP.  Measured: q and k of 10240 tokens, 24 heads of
+// 128, 28.3 us (4.4 TB/s, a copy reaches 5.2; 25.0 without norm and rotation); q, k and v of 11245 tokens, 32 heads, into a
+// bf16 cache 42 us (4.4 TB/s); one sequence's token 4.2 us.  Rows of two groups are loaded before the first is used; of eight it was slower
+// (30.3 us against 25.9 with the inputs in the last-level cache).
 struct RowsParams {
     const void* q;
     const void* k;
@@ -287,17 +309,25 @@ struct RowsParams {
     Cache c;
 };
 
-struct __attribute__((aligned(16))) AngleTable { float c[64], s[64]; };
+struct __attribute__((aligned(16))) RowTables { float c[64], s[64], qw[128], kw[128]; };   // a wave's angles and weights
 
-template <typename IO, int DH, bool E4M3, int AHEAD, bool QONLY = false>
-__device__ __forceinline__ void token_rows(const RowsParams& p, int wave, AngleTable& tab) {
-    constexpr int LPR = DH / 8, RPG = 64 / LPR;
+template <typename IO, int DH, bool E4M3, bool QONLY = false>
+__device__ __forceinline__ void token_rows(const RowsParams& p, int wave, RowTables& tab) {
+    constexpr int LPR = DH / 8, RPG = 64 / LPR, AHEAD = 2;
     const int token = wave / p.units, unit = wave - token * p.units, lane = threadIdx.x & 63, c = lane % LPR;
     if (token >= p.tokens) return;
     const long tok = token;
     int s = 0, i = 0, n = 0;
     if (!step_seq(p.s, token, s, i, n)) return;
     const int pos = p.pos ? p.pos[tok] : p.s.lens ? max(p.s.lens[s], 0) - n + i : i;
+    // The weights lie in LDS: read for each row through the CU's cache, twice a bf16 row's bytes, they cost 1.1 us more of 28.
+    if (p.qw && 2 * lane < DH)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) tab.qw[2 * lane + e] = p.qw[2 * lane + e];
+    if (!QONLY && p.kw && 2 * lane < DH)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) tab.kw[2 * lane + e] = p.kw[2 * lane + e];
+    __builtin_amdgcn_wave_barrier();
     float cs[8], sn[8];
     if (p.t.freq) {
         if (lane < p.t.rot / 2) angle(turns(p.t, lane), pos, tab.c[lane], tab.s[lane]);
@@ -328,7 +358,7 @@ __device__ __forceinline__ void token_rows(const RowsParams& p, int wave, AngleT
             float x[8];
             in[z].get(x);
             // (a row's lanes share their kind, and the exchanges stay inside a row)
-            if (kind < 2) turn_row<DH>(p.t, kind == 0 ? p.qw : p.kw, cs, sn, x);
+            if (kind < 2) turn_row<DH>(p.t, (kind == 0 ? p.qw : p.kw) != nullptr, kind == 0 ? tab.qw : tab.kw, cs, sn, x);
             if (j >= rows) continue;
             if (kind == 0) {
                 store8((IO*)p.qo + (tok * p.H + h) * DH + 8 * c, x);
@@ -362,11 +392,11 @@ __device__ __forceinline__ void token_rows(const RowsParams& p, int wave, AngleT
     }
 }
 
-template <typename IO, int DH, bool E4M3, int AHEAD>
+template <typename IO, int DH, bool E4M3>
 __global__ __launch_bounds__(NT) void k_rows(RowsParams p) {
-    __shared__ AngleTable tab[NT / 64];
+    __shared__ RowTables tab[NT / 64];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    token_rows<IO, DH, E4M3, AHEAD>(p, (int)blockIdx.x * (NT / 64) + wave, tab[wave]);
+    token_rows<IO, DH, E4M3>(p, (int)blockIdx.x * (NT / 64) + wave, tab[wave]);
 }
 
 // ------------------------------------------------------------------ k_append_e4m3
@@ -409,16 +439,21 @@ __device__ __forceinline__ bool touched_block(const StepSeqs& q, int shift, int 
 // One workgroup per (touched page, head, K or V), `page_wgs` in all, ahead of those of the q rows.  It holds the page's new
 // tokens in registers, finds their largest value, and writes codes and scale.  The angle of slot r = RPP it + i of the page
 // at position a is that of a + RPP it and that of i added up, a product of two table entries: (RPP + IT) rot / 2 sines
-// for RPP IT rows.
+// for RPP IT rows.  A scale needs its page's and head's largest value before the first code is written, so the unit of work
+// is the page: in registers the values are read once and only codes (half the bytes) are written.
+// Bound by the norm's and the angles' arithmetic: 4133 tokens of a prompt, 32 heads of 128, 16.2 us (3.7 TB/s over q, k, v
+// and the codes); without norm and rotation 7.3 us.  With the q rows' workgroups in between the pages' it was 23.6
+// against 18.4 us: the pages, the longer units, have to start first.
 template <int DH, int IT>   // IT: passes of NT / (DH / 8) rows over a page
 __global__ __launch_bounds__(NT) void k_append_e4m3(RowsParams p, int page_wgs, int each) {
     constexpr int LPR = DH / 8, RPP = NT / LPR, NP = DH / 2;
     __shared__ float red[NT / 64];
-    __shared__ __align__(16) float tc[RPP + IT][NP], ts[RPP + IT][NP];   // of i, then of a + RPP it
+    __shared__ __align__(16) float tables[2][RPP + IT][NP], kw[DH];
+    auto &tc = tables[0], &ts = tables[1];   // of i, then of a + RPP it
     const int tid = threadIdx.x, c = tid % LPR, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     if ((int)blockIdx.x >= page_wgs) {
-        static_assert(sizeof(AngleTable) * (NT / 64) <= sizeof tc, "the tables of the q rows' waves");
-        token_rows<bf16_t, DH, false, 2, true>(p, ((int)blockIdx.x - page_wgs) * (NT / 64) + wave, reinterpret_cast<AngleTable*>(tc)[wave]);
+        static_assert(sizeof(RowTables) * (NT / 64) <= sizeof tables, "the tables of the q rows' waves");
+        token_rows<bf16_t, DH, false, true>(p, ((int)blockIdx.x - page_wgs) * (NT / 64) + wave, reinterpret_cast<RowTables*>(tables)[wave]);
         return;
     }
     const int u = (int)blockIdx.x;
@@ -440,6 +475,7 @@ __global__ __launch_bounds__(NT) void k_append_e4m3(RowsParams p, int page_wgs, 
     }
     float x[IT][8], amax = 0.f;
     if (!is_v) {
+        if (p.kw && tid < DH) kw[tid] = p.kw[tid];
         const int np = p.t.rot / 2;
         const int j = tid % NP;
         if (j < np) {
@@ -467,7 +503,7 @@ __global__ __launch_bounds__(NT) void k_append_e4m3(RowsParams p, int page_wgs, 
                     st[e] = sn[e] * ca[e] + cs[e] * sa[e];
                 }
             }
-            turn_row<DH>(p.t, p.kw, ct, st, x[it]);
+            turn_row<DH>(p.t, p.kw != nullptr, kw, ct, st, x[it]);
         }
     } else {
 #pragma unroll
@@ -511,9 +547,10 @@ __global__ __launch_bounds__(NT) void k_append_e4m3(RowsParams p, int page_wgs, 
 // The query rows of a sequence and key/value head, r = i G + g for new token i and the g-th of the head's G query heads, go
 // in blocks of RB.  A block's keys are cut into chunks of c units of UNIT keys, c from the step's lengths, which the host
 // does not know: the least with which all items, (row block, chunk) pairs, are resident at once (`round` of them per
-// key/value head); where that is more than `fine` units and the lengths leave a fifth of them idle, max(fine, N / spare) with
-// N the units of all row blocks, which gives at most N / c + (row blocks) items.  So the long sequences of a batch are cut and the short ones are not.  A block of
-// one chunk writes its output, one of several partial sums, which k_attn_join adds up in order.
+// key/value head); where that is more than `fine` units and the lengths leave a fifth of them idle, max(fine, N / spare)
+// with N the units of all row blocks, which gives at most N / c + (row blocks) items.  So the long sequences of a batch are
+// cut and the short ones are not.  A block of one chunk writes its output, one of several partial sums, which k_attn_join
+// adds up in order.
 constexpr int UNIT = 128;
 
 // x / d for 0 <= x < 2^31 by one product: m = ceil(2^sh / d), sh = 31 + ceil(log2 d); m d - 2^sh < d <= 2^(sh - 31), so that x
@@ -700,7 +737,12 @@ __device__ __forceinline__ float sum_bf16(bf16x8 w, float c) {
 // ------------------------------------------------------------------ k_attn_rows: few rows, many keys
 // Attention of blocks of up to 16 rows; bound by the cache's bytes.  A wave takes 32 keys a step, K and V from memory
 // straight into its registers, 16 KB of steps ahead of their use, without LDS or barriers; the workgroup's waves take the
-// chunk's steps in turn and add up at the end.
+// chunk's steps in turn and add up at the end.  Two workgroups per CU (256 registers a wave) keep 128 KB of loads in
+// flight on a CU; matrix products are nearly free beside them, and a row block of up to 16 rows costs no more than one row.
+// Measured: a token of 64 sequences of 526 to 8138 keys, 695 MB of bf16 cache in 124 us (5.6 TB/s); the same in e4m3 72 us
+// (4.8 TB/s); one sequence of 131072 keys 96 us (5.6 TB/s).  With few items what bounds it is the load path of a CU: 776
+// keys of one sequence, 8 workgroups, 1 us per 128 keys, since a K operand's load touches 64 bytes of 16 rows, a third of
+// that path's rate; eight waves a workgroup there gained nothing.
 //   S^T = K Q^T: the A operand's row 4 a + b of 16-key half t is key 16 t + 4 b + a, so that a lane's results st[t][e] are
 // keys 16 t + 4 e + lg of query l16.
 //   O^T = V^T P^T: with contraction element j of lane group lg standing for key 4 j + lg, the weights are the B operand as
@@ -997,7 +1039,12 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
 // Attention of blocks of 128 rows; bound by the matrix units and the softmax beside them.  Blocks of 64 keys and values
 // lie in a double-buffered LDS ring (16-byte chunks XOR-swizzled as in k_attn_causal, whose products, running softmax and
 // operand orders these are): a bf16 cache is copied there without registers, e4m3 codes are loaded a block ahead, made
-// bf16 with their scale and stored.
+// bf16 with their scale and stored.  A wave has two tiles of 16 rows, so that every K and V operand read from LDS feeds
+// both tiles' products: LDS reads are what a block costs most beside the products (one tile a wave: 175 us against 164).
+// Measured: 2048 new tokens behind 8192, 16 query heads of 128, 157 us and 10 of joining, 155 GFLOP (0.93 PFLOP/s
+// with both; a large product of a library reaches 1.2).  Products and the softmax's vector work of a SIMD's two waves hardly
+// overlap; with the next block's scores formed beside this block's weights in one wave it took 181 us (all 256 registers),
+// and 218 against 196 with the order prescribed to the compiler.
 template <int DH, typename CT>
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2))) void k_attn_tile(PagedParams p) {
     constexpr bool E4M3 = sizeof(CT) == 1;
@@ -1303,8 +1350,8 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2))) void k_
 // The sum of a row's chunks' partial sums, over loads of 4 channels a lane, lanes and waves in a fixed order (so that the
 // result does not depend on which chunk ended first).  (The last workgroup of a block adding up at its end, found by flags
 // stored past the caches, was slower: 64 sequences e4m3 81 us against 78, 16 sequences' 4 tokens 38 against 23.)
-// Blocks of 16 rows may have many chunks: a workgroup a row (blockIdx.y), its waves sharing
-// them.
+// Blocks of 16 rows may have many chunks: a workgroup a row (blockIdx.y), its waves sharing them.  Bound by latency: the
+// launch, the search for the item and one round trip to memory; 5.6 us for 63 chunks.
 template <int DH>
 __global__ __launch_bounds__(NT) void k_attn_join(PagedParams p) {
     constexpr int RB = 16, LPR = DH / 4, SUB = 64 / LPR, NW = NT / 64;   // lanes per row; chunks that a wave's load takes at once

@@ -97,6 +97,24 @@ def test_rotation_stays_in_its_pairs(d, rot, near):
         assert {tuple(x) for x in torch.isnan(got).nonzero().tolist()} == {(0, 1, 1, c) for c in pair}, at
 
 
+@pytest.mark.parametrize("io", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("power", [-66, -63, -60, 0, 60])
+def test_norm_of_small_and_large_rows(io, power):
+    """Rows whose mean square is below the smallest normal float (eps = 0), and large ones.
+
+    A square of 2^-132 is off by 2^-150 at most where it is subnormal, so the mean by 2^-17 of itself (sum and division
+    included: 8 halvings of 2^-150 on a mean of 2^-132 or more), its root by 2^-18, and the output by a rounding more.
+    """
+    g = torch.Generator().manual_seed(4)
+    x = (torch.rand(1, 5, 2, 64, generator=g) + 1) * (torch.randint(0, 2, (1, 5, 2, 64), generator=g) * 2 - 1) * 2.0 ** power
+    x = x.to(io)
+    w = torch.rand(64, generator=g) + 0.5
+    got, _ = gdn.gdn_qk_norm_rope(x.cuda(), x.cuda(), q_weight=w.cuda(), k_weight=w.cuda(), eps=0.0)
+    y = x.double()
+    want = y * w.double() / (y * y).mean(-1, keepdim=True).sqrt()
+    assert ((got.cpu().double() - want).abs() <= want.abs() * (2.0 ** -17 + torch.finfo(io).eps / 2)).all()
+
+
 # ------------------------------------------------------------------ gdn_kv_append
 def _append_case(cache, page, d, H, Hkv, lens, new, cu, rot, near, seed, T=None):
     n, packed = len(lens), cu is not None
