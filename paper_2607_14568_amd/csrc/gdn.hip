@@ -3160,13 +3160,13 @@ void launch_attention(AttnParams a, hipStream_t st) {
         hipLaunchKernelGGL((k_attn_causal<DH, 1>), dim3((unsigned)wgs), dim3(NT_ATT), 0, st, a);
 }
 
-// Row groups per wave of k_rows: one while they do not fill the chip's wave slots (latency), then two or more, up to about
-// 16384 waves, so that a token's angles and place are formed fewer times.  Waves of 2 against 1 group: packed q and k of
-// 60 to 2900 tokens, 20 heads of 64, 11.3 us against 12.0, q of 4133 tokens into an e4m3 cache 18.3 against 20.5; of 3
-// against 6: q and k of 10240 tokens, 24 heads of 128, 30.2 against 32.1.
+// Row groups per wave of k_rows: as many as leave about 6144 waves (24 per CU), so that a token's angles, weights and place
+// are formed fewer times, but no fewer waves, which latency needs.  us with 1, 2, 3 and (or) all of a token's groups a wave: q
+// and k of 2000 tokens, 24 heads of 128 (6 groups) 9.2, 7.7, 8.2 and 9.1; of 4000 15.3, 12.2, 11.2 and 12.0; of 10240 42.8, 30.2,
+// 29.1 and 27.7; packed, of 5809 tokens, 20 heads of 64 (3 groups) 12.1, 10.5 and 9.5.
 void rows_split(RowsParams& p, int rows, int dh) {
     const long groups = (rows + 512 / dh - 1) / (512 / dh), work = p.tokens * groups;   // 64 / (dh / 8) rows a group
-    const long per = work <= 8192 ? 1 : std::min(groups, std::max(2L, work / 16384));
+    const long per = std::min(groups, std::max(1L, (work + 6143) / 6144));
     p.units = (int)((groups + per - 1) / per);
     p.per = (int)((groups + p.units - 1) / p.units);
 }

@@ -288,9 +288,9 @@ template <int N> __device__ __forceinline__ void rescale(uint8_t* codes, int pit
 // page's and head's new values.  Each lane forms one angle of the token's position, the wave's tables of them lie in LDS.
 // Bound by memory: every row is read once and written once, a lane's 16 bytes (8 channels) an access, so that a head's row
 // lies in 8 or 16 neighbouring lanes and its norm is a sum over them by DPP.  Measured: q and k of 10240 tokens, 24 heads of
-// 128, 28.3 us (4.4 TB/s, a copy reaches 5.2; 25.0 without norm and rotation); q, k and v of 11245 tokens, 32 heads, into a
-// bf16 cache 42 us (4.4 TB/s); one sequence's token 4.2 us.  Rows of two groups are loaded before the first is used; of eight it was slower
-// (30.3 us against 25.9 with the inputs in the last-level cache).
+// 128, 27.6 us (4.6 TB/s, a copy reaches 5.2; 25.0 without norm and rotation); q, k and v of 11245 tokens, 32 heads, into a
+// bf16 cache 41 us (4.5 TB/s); one sequence's token 4.2 us.  Rows of two groups are loaded before the first is used; of eight
+// it was slower (30.3 us against 25.9 with the inputs in the last-level cache).
 struct RowsParams {
     const void* q;
     const void* k;
@@ -441,8 +441,8 @@ __device__ __forceinline__ bool touched_block(const StepSeqs& q, int shift, int 
 // at position a is that of a + RPP it and that of i added up, a product of two table entries: (RPP + IT) rot / 2 sines
 // for RPP IT rows.  A scale needs its page's and head's largest value before the first code is written, so the unit of work
 // is the page: in registers the values are read once and only codes (half the bytes) are written.
-// Bound by the norm's and the angles' arithmetic: 4133 tokens of a prompt, 32 heads of 128, 16.2 us (3.7 TB/s over q, k, v
-// and the codes); without norm and rotation 7.3 us.  With the q rows' workgroups in between the pages' it was 23.6
+// Bound by the norm's and the angles' arithmetic: 4133 tokens of a prompt, 32 heads of 128, 15.9 us (3.7 TB/s over q, k, v
+// and the codes); without norm and rotation 11.8 us.  With the q rows' workgroups in between the pages' it was 23.6
 // against 18.4 us: the pages, the longer units, have to start first.
 template <int DH, int IT>   // IT: passes of NT / (DH / 8) rows over a page
 __global__ __launch_bounds__(NT) void k_append_e4m3(RowsParams p, int page_wgs, int each) {
@@ -982,8 +982,8 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
                 *reinterpret_cast<floatx4*>(&lds_o[wave][l16][CW * (4 * lg + e) + n]) = floatx4{acc[n][e], acc[n + 1][e], acc[n + 2][e], acc[n + 3][e]};
     }
     if (k1 - 1 > last0) {
-        // Some rows do not see some of the item's keys, but their weight of 0 does not hide a value that is not finite (0 x NaN):
-        // where that left a sum that is not finite, the rows are done again without the matrix units.
+        // Some rows do not see some of the item's keys, but their weight of 0 does not hide a value that is not finite
+        // (0 x NaN): where that left a sum that is not finite, the rows are done again without the matrix units.
         if (tid == 0) redo = 0;
         __syncthreads();
         float sum = 0.f;
