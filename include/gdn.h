@@ -487,8 +487,10 @@ size_t gdn_attention_paged_workspace_bytes(int B, int T, int H, int H_kv, int d,
  *          (its contents on entry are ignored); NULL and 0 where that is 0.  Calls that may overlap
  *          in time, captured graphs among them, need one each.
  * Slots of the cache behind a sequence's length are not read into results, whatever they hold.
- * Sums are held in fp32, relative to a weight that may lie 2^13 below the largest: they stay finite
- * for values v with |v| * (number of keys) below 2^114.
+ * Scores, weights and sums are formed in fp32, relative to a weight that may lie 2^13 below the largest:
+ * they stay finite for values v with |v| * (number of keys) below 2^114.  In the products with v a weight
+ * is off by 2^-15 of itself at most where the call's rows go in blocks of 16 (decoding, a few tokens a
+ * sequence), and rounded to bf16 (2^-8) where they go in blocks of 128, as in gdn_attention_prefill.
  * Errors as gdn_attention_prefill, and GDN_ERR_WORKSPACE.
  */
 gdn_status gdn_attention_paged(const void* q, const void* k_cache, const void* v_cache,

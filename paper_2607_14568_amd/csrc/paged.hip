@@ -551,9 +551,10 @@ __global__ __launch_bounds__(NT) void k_append_e4m3(RowsParams p, int page_wgs, 
 // with N the units of all row blocks, which gives at most N / c + (row blocks) items.  So the long sequences of a batch are
 // cut and the short ones are not.  A block of one chunk writes its output, one of several partial sums, which k_attn_join
 // adds up in order.
-// Scores, maxima, weight sums and outputs are fp32; only the weights are rounded, to bf16, as the matrix instruction with the
-// values takes them (off by 2^-8 of each at most, up and down over the keys: the outputs' error against 64 bits is 0.0023,
-// that of their own rounding alone 0.0017).
+// Scores, maxima, weight sums and outputs are fp32.  The matrix instruction with the values takes the weights as bf16: two
+// numbers each in k_attn_rows, where its products are nearly free (off by 2^-15; the outputs' error against 64 bits is that of
+// their own rounding, 0.0017), one in k_attn_tile, which such products bound (off by 2^-8 of each at most, up and down over the
+// keys: error 0.0023; with two numbers each 222 us against 168 for the piece below).
 constexpr int UNIT = 128;
 
 // x / d for 0 <= x < 2^31 by one product: m = ceil(2^sh / d), sh = 31 + ceil(log2 d); m d - 2^sh < d <= 2^(sh - 31), so that x
@@ -735,6 +736,21 @@ __device__ __forceinline__ float sum_bf16(bf16x8 w, float c) {
 #pragma unroll
     for (int i = 0; i < 8; i += 2) c = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{w[i], w[i + 1]}, one, c, false);
     return c;
+}
+
+// Eight weights as two bf16 numbers each, hi + lo, off by 2^-15 of them at most: hi the upper half of the float's bits, lo
+// what is left, under 2^-7 of it, rounded.  2^-20 of the weight more keeps lo's sign that of hi where nothing is left, so that an
+// infinite value's products with both add up to that infinity (0 x infinity and a difference of infinities are NaN).
+__device__ __forceinline__ void split_weights(floatx4 a, floatx4 b, bf16x8& hi, bf16x8& lo) {
+    int4v h;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float x = i < 2 ? a[2 * i] : b[2 * i - 4], y = i < 2 ? a[2 * i + 1] : b[2 * i - 3];
+        h[i] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302);
+    }
+    auto rest = [](float w) { return __builtin_fmaf(w, 1.f + 0x1p-20f, -__uint_as_float(__float_as_uint(w) & 0xffff0000u)); };
+    hi = __builtin_bit_cast(bf16x8, h);
+    lo = pack_bf16(floatx4{rest(a[0]), rest(a[1]), rest(a[2]), rest(a[3])}, floatx4{rest(b[0]), rest(b[1]), rest(b[2]), rest(b[3])});
 }
 
 // ------------------------------------------------------------------ k_attn_rows: few rows, many keys
@@ -947,7 +963,8 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
             }
             if constexpr (E4M3) wt[t] *= x.vs[t];
         }
-        const bf16x8 pf = pack_bf16(wt[0], wt[1]);
+        bf16x8 ph, pl;
+        split_weights(wt[0], wt[1], ph, pl);
         int vb[8][CW / 2];   // bf16 pairs of channels
 #pragma unroll
         for (int j = 0; j < 8; ++j)
@@ -959,7 +976,8 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
 #pragma unroll
             for (int jj = 0; jj < 4; ++jj)
                 va[jj] = __builtin_amdgcn_perm(vb[2 * jj + 1][n / 2], vb[2 * jj][n / 2], n % 2 ? 0x07060302 : 0x05040100);
-            acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va), pf, acc[n], 0, 0, 0);
+            acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va), ph, acc[n], 0, 0, 0);
+            acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va), pl, acc[n], 0, 0, 0);
         }
     };
     // DEPTH - 1 steps' loads are in flight while one is used
