@@ -487,6 +487,8 @@ size_t gdn_attention_paged_workspace_bytes(int B, int T, int H, int H_kv, int d,
  *          (its contents on entry are ignored); NULL and 0 where that is 0.  Calls that may overlap
  *          in time, captured graphs among them, need one each.
  * Slots of the cache behind a sequence's length are not read into results, whatever they hold.
+ * A key or value that is not finite acts on the rows that see it and on no other: an infinite value makes
+ * its channel that infinity, two opposite ones NaN; a score of minus infinity is a weight of 0.
  * Scores, weights and sums are formed in fp32, relative to a weight that may lie 2^13 below the largest:
  * they stay finite for values v with |v| * (number of keys) below 2^114.  In the products with v a weight
  * is off by 2^-15 of itself at most where the call's rows go in blocks of 16 (decoding, a few tokens a

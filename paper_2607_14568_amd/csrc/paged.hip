@@ -1204,7 +1204,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2))) void k_
         for (int t = 0; t < NDT; ++t) oacc[u][t] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
     // A weight of 0 does not hide a value that is not finite (0 x NaN).  In the blocks from `part` on, where some rows do not
-    // see a key that others see, such values are taken out, and the rows that see them are made NaN at the end.
+    // see a key that others see, such values are taken out, and added at the end, with their weight, to the rows that see them.
     const int all = base + div_by(it.rb * RB, p.by_g);   // the last key that every row sees
     const int part = all < k0 ? k0 : k0 + (all + 1 - k0) / AKB * AKB;
     if (tid == 0) odd = 0;
@@ -1334,17 +1334,46 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2))) void k_
     for (int key = part < k1 && odd ? part : k1; key < k1; ++key) {   // (rare)
         const int id = __builtin_amdgcn_readfirstlane(page_of(p.c, it.s, key >> p.c.shift));
         if (id < 0) continue;
-        const long at = ((((long)id * p.HKV + hk) << p.c.shift) + (key & (p.c.page - 1))) * DH + 4 * lg;
+        const long at = ((((long)id * p.HKV + hk) << p.c.shift) + (key & (p.c.page - 1))) * DH;
+        float x[NDT][4];   // this lane's channels
+        bool bad = false;
 #pragma unroll
         for (int t = 0; t < NDT; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const CT x = ((const CT*)p.c.v)[at + 16 * t + e];
-                const bool bad = E4M3 ? (x & 0x7f) == 0x7f : (x & 0x7f80) == 0x7f80;
-#pragma unroll
-                for (int u = 0; u < QT; ++u)
-                    if (bad && key <= last[u]) oacc[u][t][e] = __uint_as_float(0x7fc00000u);
+                const CT y = ((const CT*)p.c.v)[at + 16 * t + 4 * lg + e];
+                if constexpr (E4M3) x[t][e] = (y & 0x7f) == 0x7f ? __uint_as_float(0x7fc00000u) : 0.f;
+                else x[t][e] = bf((short)y);
+                bad = bad || !(fabsf(x[t][e]) <= -LOWEST);
             }
+        if (!__builtin_amdgcn_ballot_w64(bad)) continue;
+#pragma unroll
+        for (int u = 0; u < QT; ++u) {
+            float dot = 0.f;   // with this lane's share of the key
+#pragma unroll
+            for (int kb = 0; kb < NKB; ++kb) {
+                const CT* src = (const CT*)p.c.k + at + 32 * kb + 8 * lg;
+                float k[8];
+                if constexpr (E4M3) {
+                    from_e4m3(*(const uint64_t*)src, k);
+                } else {
+                    Chunk8<bf16_t> y;
+                    y.load(src);
+                    y.get(k);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) dot += (float)qf[u][kb][e] * k[e];
+            }
+            if constexpr (E4M3) dot *= p.c.ks[(long)id * p.HKV + hk];
+            dot += __shfl_xor(dot, 16, 64);
+            dot += __shfl_xor(dot, 32, 64);
+            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(dot, sl2, -m[u]));
+#pragma unroll
+            for (int t = 0; t < NDT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (key <= last[u] && !(fabsf(x[t][e]) <= -LOWEST)) oacc[u][t][e] += w * x[t][e];
+        }
     }
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
