@@ -1338,14 +1338,21 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2))) void k_
         float x[NDT][4];   // this lane's channels
         bool bad = false;
 #pragma unroll
-        for (int t = 0; t < NDT; ++t)
+        for (int t = 0; t < NDT; ++t) {
+            const CT* src = (const CT*)p.c.v + at + 16 * t + 4 * lg;
+            short4v y;
+            if constexpr (E4M3) {   // (as staged: a code's product with its scale may be what is not finite)
+                const int4v z = fp8_scaled(*(const int*)src, 0, p.c.vs[(long)id * p.HKV + hk]);
+                y = __builtin_bit_cast(short4v, (uint64_t)(uint32_t)z[0] | (uint64_t)(uint32_t)z[1] << 32);
+            } else {
+                y = *(const short4v*)src;
+            }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const CT y = ((const CT*)p.c.v)[at + 16 * t + 4 * lg + e];
-                if constexpr (E4M3) x[t][e] = (y & 0x7f) == 0x7f ? __uint_as_float(0x7fc00000u) : 0.f;
-                else x[t][e] = bf((short)y);
+                x[t][e] = bf(y[e]);
                 bad = bad || !(fabsf(x[t][e]) <= -LOWEST);
             }
+        }
         if (!__builtin_amdgcn_ballot_w64(bad)) continue;
 #pragma unroll
         for (int u = 0; u < QT; ++u) {

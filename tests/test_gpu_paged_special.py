@@ -57,3 +57,16 @@ def test_infinite_values(new, page, d):
         kc[1][i, h, slot, c] = x
     ref = _check(q, kc, table, lens, "infinite values")
     assert np.isposinf(ref).any() and np.isneginf(ref).any() and np.isnan(ref).any()
+
+
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("new", NEW)
+def test_scales_that_are_no_numbers(new, page):
+    """A NaN as the scale of a page of values, or of keys, under codes that are numbers: rows that see one of the page's keys are
+    NaN in every channel, all others as without it."""
+    print("case: NaN scales", new, page, flush=True)
+    q, kc, table, lens = _case("e4m3", new, page, 128, 30 + page)
+    for s, h, p, i in [(0, 0, lens[0] - 1, 3), (1, 1, lens[1] - new // 2 - 1, 3), (2, 0, lens[2] - 1, 2), (3, 1, 0, 3)]:
+        kc[i][_at(table, page, s, p)[0], h] = float("nan")
+    ref = _check(q, kc, table, lens, "NaN scales")
+    assert np.isnan(ref).any() and np.isfinite(ref).any()
