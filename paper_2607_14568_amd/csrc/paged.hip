@@ -714,11 +714,11 @@ template <bool SCALED> struct PageWalk {
 };
 
 // Eight e4m3 codes times their scale as bf16: exact for a power of two, which is what gdn_kv_append makes a scale (the
-// instruction multiplies by the scale's exponent); any other one's products are rounded to bf16, as keys and values that
-// were cached in bf16 are.
+// instruction multiplies by the scale's exponent alone, so it must be a positive normal number); any other one's products are
+// rounded to bf16, as keys and values that were cached in bf16 are.
 __device__ __forceinline__ int4v fp8_scaled(int a, int b, float scale) {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    if ((__float_as_uint(scale) & 0x7fffff) == 0)
+    if ((__float_as_uint(scale) & 0x7fffff) == 0 && __float_as_uint(scale) - 0x800000u < 0x7f000000u)
         return int4v{__builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false)),
                      __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true)),
                      __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false)),

@@ -70,3 +70,15 @@ def test_scales_that_are_no_numbers(new, page):
         kc[i][_at(table, page, s, p)[0], h] = float("nan")
     ref = _check(q, kc, table, lens, "NaN scales")
     assert np.isnan(ref).any() and np.isfinite(ref).any()
+
+
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("new", NEW)
+def test_negative_scales_and_zero(new, page):
+    """A scale of either sign, powers of two and others, and 0: a code stands for its product with it."""
+    print("case: negative scales", new, page, flush=True)
+    q, kc, table, lens = _case("e4m3", new, page, 128, 40 + page)
+    g = np.random.default_rng(page)
+    for i in (2, 3):
+        kc[i] *= torch.from_numpy(g.choice([1.0, -1.0, -1.25, 0.0], tuple(kc[i].shape))).float()
+    _check(q, kc, table, lens, "negative scales")
