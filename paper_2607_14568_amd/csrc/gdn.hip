@@ -3775,7 +3775,14 @@ extern "C" gdn_status gdn_attention_prefill(const void* q, const void* k, const 
 }
 
 // ------------------------------------------------------------------ the attention layers' serving operators
-// Checks shared by the entry points of paged.hip, in the order of the header's argument lists.
+// Sizes that the entry points of paged.hip are implemented for (each at least 1), and the checks that they share, in the order
+// of the header's argument lists.
+static bool head_size_known(int d) { return d == 64 || d == 128; }
+static bool heads_fit(int H, int d) { return (long)H * d <= (1L << 20); }
+static bool rows_fit(int B, int T, int H) { return (long)B * T * H < (1L << 31) / 2; }
+static bool page_known(int page) { return page == 16 || page == 32 || page == 64 || page == 128; }
+static bool table_fits(int page, int max_pages) { return (long)max_pages * page <= (1L << 30); }
+
 static gdn_status step_sizes(int B, int T, int H, int H_kv, int d, const int32_t* cu_seqlens, int n_seqs) {
     if (B < 1 || T < 0 || H < 1) return fail(GDN_ERR_INVALID_ARG, "B=%d T=%d H=%d out of range", B, T, H);
     if (H_kv < 1 || H_kv > H || H % H_kv != 0)
@@ -3786,9 +3793,9 @@ static gdn_status step_sizes(int B, int T, int H, int H_kv, int d, const int32_t
     if (n_seqs < 0) return fail(GDN_ERR_INVALID_ARG, "n_seqs=%d is negative", n_seqs);
     if (n_seqs > 0 && B != 1) return fail(GDN_ERR_INVALID_ARG, "packed sequences need B == 1 (got %d)", B);
     if (cu_seqlens && !aligned(cu_seqlens, 4)) return fail(GDN_ERR_INVALID_ARG, "cu_seqlens is not 4-byte aligned");
-    if (d != 64 && d != 128) return fail(GDN_ERR_UNSUPPORTED, "d=%d: only 64 and 128 are implemented", d);
-    if ((long)H * d > (1L << 20)) return fail(GDN_ERR_UNSUPPORTED, "H=%d too large", H);
-    if ((long)B * T * H >= (1L << 31) / 2) return fail(GDN_ERR_UNSUPPORTED, "B*T*H=%ld too large", (long)B * T * H);
+    if (!head_size_known(d)) return fail(GDN_ERR_UNSUPPORTED, "d=%d: only 64 and 128 are implemented", d);
+    if (!heads_fit(H, d)) return fail(GDN_ERR_UNSUPPORTED, "H=%d too large", H);
+    if (!rows_fit(B, T, H)) return fail(GDN_ERR_UNSUPPORTED, "B*T*H=%ld too large", (long)B * T * H);
     return GDN_OK;
 }
 
@@ -3812,9 +3819,9 @@ static gdn_status check_cache(const void* k_cache, const void* v_cache, const fl
         return fail(GDN_ERR_INVALID_ARG, "cache_dtype=%d is neither GDN_BF16 nor GDN_E4M3", cache_dtype);
     if (page < 1 || n_pages < 1 || max_pages < 1)
         return fail(GDN_ERR_INVALID_ARG, "page=%d n_pages=%d max_pages=%d must be positive", page, n_pages, max_pages);
-    if (page != 16 && page != 32 && page != 64 && page != 128)
+    if (!page_known(page))
         return fail(GDN_ERR_UNSUPPORTED, "page=%d: only 16, 32, 64 and 128 are implemented", page);
-    if ((long)max_pages * page > (1L << 30)) return fail(GDN_ERR_UNSUPPORTED, "max_pages=%d too large", max_pages);
+    if (!table_fits(page, max_pages)) return fail(GDN_ERR_UNSUPPORTED, "max_pages=%d too large", max_pages);
     if (!k_cache || !v_cache || !block_table || !seq_lens)
         return fail(GDN_ERR_INVALID_ARG, "k_cache, v_cache, block_table and seq_lens must be non-null");
     if (!aligned(k_cache, 16) || !aligned(v_cache, 16)) return fail(GDN_ERR_INVALID_ARG, "a cache is not 16-byte aligned");
@@ -3953,8 +3960,8 @@ extern "C" gdn_status gdn_kv_append(const void* q, const void* k, const void* v,
 }
 
 extern "C" size_t gdn_attention_paged_workspace_bytes(int B, int T, int H, int H_kv, int d, int page, int max_pages, int n_seqs) {
-    if (B < 1 || T < 1 || H < 1 || H_kv < 1 || H % H_kv || (d != 64 && d != 128) || n_seqs < 0 || (n_seqs > 0 && B != 1) ||
-        page < 1 || max_pages < 1)
+    if (B < 1 || T < 1 || H < 1 || H_kv < 1 || H % H_kv || !head_size_known(d) || n_seqs < 0 || (n_seqs > 0 && B != 1) ||
+        !heads_fit(H, d) || !rows_fit(B, T, H) || !page_known(page) || max_pages < 1 || !table_fits(page, max_pages))
         return 0;
     return paged_layout(paged_plan(B, T, H, H_kv, page, max_pages, n_seqs), H_kv, d).total;
 }
