@@ -516,6 +516,8 @@ def _cache_args(dev, k_cache, v_cache, block_table, seq_lens, cu_seqlens, k_scal
     kind = k_cache.dtype
     at = _addresses(dev, (k_cache, v_cache, block_table, seq_lens, cu_seqlens, k_scale, v_scale), _CACHE_NAMES,
                     (kind, kind, _I32, _I32, _I32, _F32, _F32))
+    if None in at[:4]:
+        raise TypeError("%s must be a CUDA (HIP) tensor" % _CACHE_NAMES[at.index(None)])
     shape, table = k_cache.shape, block_table.shape
     n_seqs = 0 if cu_seqlens is None else cu_seqlens.numel() - 1
     n = B if cu_seqlens is None else n_seqs

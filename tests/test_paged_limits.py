@@ -1,5 +1,7 @@
-"""What the workspace query of gdn_attention_paged says for sizes that the call refuses (C ABI, CPU)."""
+"""What the workspace query of gdn_attention_paged says for sizes that the call refuses (C ABI), and what the binding says to a
+cache that is incomplete, CPU."""
 import pytest
+import torch
 
 import paper_2607_14568_amd as gdn
 from test_paged_refusals import A, INVALID, UNSUPPORTED, _attention
@@ -27,3 +29,15 @@ def test_workspace_at_the_limits():
     """The largest sizes that are implemented have one where a sequence may be cut."""
     assert _need() > 0 and _need(page=16) > 0 and _need(page=128, max_pages=1 << 23) > 0 and _need(d=64) > 0
     assert _need(H=1 << 13, Hkv=8) > 0
+
+
+@pytest.mark.parametrize("missing", ["k_cache", "v_cache", "block_table", "seq_lens"])
+@pytest.mark.parametrize("what", [None, 3, [1]])
+def test_a_cache_without_one_of_its_tensors(missing, what):
+    """Named, with a TypeError, whatever stands in its place."""
+    kw = dict(k_cache=torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16), v_cache=torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16),
+              block_table=torch.zeros(1, 3, dtype=torch.int32), seq_lens=torch.zeros(1, dtype=torch.int32), cu_seqlens=None,
+              k_scale=None, v_scale=None)
+    kw[missing] = what
+    with pytest.raises(TypeError, match=missing):
+        gdn._cache_args(-1, *kw.values(), 1, 2, 64)   # (-1: the number that torch gives the CPU)
