@@ -3239,7 +3239,7 @@ PagedLayout paged_layout(const PagedPlan& p, int H_kv, int d) {
 
 template <int DH, typename CT>
 void launch_paged(const PagedParams& p, const PagedPlan& plan, hipStream_t st) {
-    const dim3 grid((unsigned)(p.items * p.HKV));
+    const dim3 grid((unsigned)(plan.items * p.HKV));
     const long blocks = plan.blocks * p.HKV;
     if (plan.rb == AQ) {
         hipLaunchKernelGGL((k_attn_tile<DH, CT>), grid, dim3(NT), 0, st, p);
@@ -3997,7 +3997,7 @@ extern "C" gdn_status gdn_attention_paged(const void* q, const void* k_cache, co
     const PagedPlan plan = paged_plan(B, T, H, H_kv, page, max_pages, n_seqs);
     if (!grid_fits(plan.items * H_kv)) return fail(GDN_ERR_UNSUPPORTED, "B*T*H too large");
     const PagedLayout lay = paged_layout(plan, H_kv, d);
-    p.items = (int)plan.items; p.round = plan.round; p.fine = plan.fine; p.spare = plan.spare;
+    p.round = plan.round; p.fine = plan.fine; p.spare = plan.spare;
     p.pml = reinterpret_cast<float2*>(workspace);
     p.po = reinterpret_cast<float*>(static_cast<char*>(workspace) + lay.po);
     hipStream_t hs = reinterpret_cast<hipStream_t>(stream);

@@ -575,7 +575,6 @@ struct PagedParams {
     int H, HKV, G;
     Div by_hkv, by_g;
     float scale_log2;
-    int items;             // per key/value head (the grid)
     int round, fine, spare; // see above; spare 0: no cuts
     float* po;             // partial sums of item w, head hk: [w HKV + hk][RB][DH], and their largest score and weight sum
     float2* pml;           // ... [w HKV + hk][RB]
@@ -717,7 +716,6 @@ template <bool SCALED> struct PageWalk {
 // instruction multiplies by the scale's exponent alone, so it must be a positive normal number); any other one's products are
 // rounded to bf16, as keys and values that were cached in bf16 are.
 __device__ __forceinline__ int4v fp8_scaled(int a, int b, float scale) {
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
     if ((__float_as_uint(scale) & 0x7fffff) == 0 && __float_as_uint(scale) - 0x800000u < 0x7f000000u)
         return int4v{__builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false)),
                      __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true)),
@@ -1131,8 +1129,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2))) void k_
         rv = rsrc((const char*)p.c.v + at, bytes);
     };
     constexpr int NCW = AKB / RPI / NW;                   // bf16: this wave's 1 KB copies of K, and of V
-    constexpr int PB = AKB * DH / NT < 16 ? 8 : 16;      // e4m3: bytes of a piece, and this thread's pieces of K, and of V
-    constexpr int NCB = AKB * DH / PB / NT;
+    constexpr int PB = 16, NCB = AKB * DH / PB / NT;      // e4m3: bytes of a piece, and this thread's pieces of K, and of V
     static_assert(NCW >= 1 && NCB >= 1, "every thread copies the same share");
     int4v kc[E4M3 ? NCB : 1], vc[E4M3 ? NCB : 1];
     float kscale[E4M3 ? NCB : 1], vscale[E4M3 ? NCB : 1];   // of these pieces' page
@@ -1148,14 +1145,8 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2))) void k_
                 kscale[c] = ks;
                 vscale[c] = vs;
                 const int off = (tid + NT * c) * PB;
-                if constexpr (PB == 16) {
-                    kc[c] = __builtin_bit_cast(int4v, bload16(rk, off));
-                    vc[c] = __builtin_bit_cast(int4v, bload16(rv, off));
-                } else {
-                    const auto k2 = __builtin_amdgcn_raw_buffer_load_b64(rk, off, 0, 0), v2 = __builtin_amdgcn_raw_buffer_load_b64(rv, off, 0, 0);
-                    kc[c] = int4v{(int)k2[0], (int)k2[1], 0, 0};
-                    vc[c] = int4v{(int)v2[0], (int)v2[1], 0, 0};
-                }
+                kc[c] = __builtin_bit_cast(int4v, bload16(rk, off));
+                vc[c] = __builtin_bit_cast(int4v, bload16(rv, off));
             }
         } else {
 #pragma unroll
