@@ -492,7 +492,8 @@ size_t gdn_attention_paged_workspace_bytes(int B, int T, int H, int H_kv, int d,
  * Scores, weights and sums are formed in fp32, relative to a weight that may lie 2^13 below the largest:
  * they stay finite for values v with |v| * (number of keys) below 2^114.  In the products with v a weight
  * is off by 2^-15 of itself at most where the call's rows go in blocks of 16 (decoding, a few tokens a
- * sequence), and rounded to bf16 (2^-8) where they go in blocks of 128, as in gdn_attention_prefill.
+ * sequence), and rounded to bf16 (2^-8) where they go in blocks of 128, as in gdn_attention_prefill; there
+ * a GDN_E4M3 code's product with a scale that is no power of two is rounded to bf16, too.
  * Errors as gdn_attention_prefill, and GDN_ERR_WORKSPACE.
  */
 gdn_status gdn_attention_paged(const void* q, const void* k_cache, const void* v_cache,

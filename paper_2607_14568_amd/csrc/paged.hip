@@ -81,9 +81,9 @@ struct Turn {
 
 // cos and sin of pos * freq[i]: the angle in float64 (a float32 product is off by 2^-24 of an angle of up to 10^5 radians), in
 // turns, reduced to a quadrant n and the rest f in [-1/2, 1/2] quarter turns, whose sine and cosine are polynomials in f^2
-// (fitted for the least largest error at those degrees: 2^-27.6 and 2^-34).  Off by at most 2^-23.6 of 1 and 2^-26 on
-// average, less than sincospif of the rounded half turns (2^-23.1, 2^-25.3), and no slower.  (The sine unit takes turns and
-// is off by 2^-22.9.)
+// (fitted for the least largest error at those degrees and rounded to float: off by 2^-28.1 and 2^-27.1, in float steps by
+// 2^-24.5 and 2^-24.0).  With f rounded to float off by at most 2^-23.6 of 1 and 2^-26 on average, less than sincospif of the
+// rounded half turns (2^-23.1, 2^-25.3), and no slower.  (The sine unit takes turns and is off by 2^-22.9.)
 __device__ __forceinline__ double turns(const Turn& t, int i) { return t.freq[i] * 0.15915494309189535; }   // per position
 __device__ __forceinline__ void angle(double turns, double pos, float& cs, float& sn) {
     double a = pos * turns;
@@ -264,7 +264,8 @@ __device__ __forceinline__ void from_e4m3(uint64_t codes, float (&x)[8]) {
     for (int e = 0; e < 8; ++e) x[e] = y[e / 2][e % 2];
 }
 
-// This lane's 8 codes of rows r0, r0 + step, .. below r1 brought to another scale (N rows' loads at a time).
+// This lane's 8 codes of rows r0, r0 + step, .. below r1 brought to another scale (N rows' loads at a time).  (A single token
+// past its page's scale: 256 sequences, all their pages of 64, K and V of 8 heads, 3.5 us more than a step that keeps them.)
 template <int N> __device__ __forceinline__ void rescale(uint8_t* codes, int pitch, int r0, int r1, int step, float ratio) {
 #pragma unroll 1
     for (int r = r0; r < r1; r += N * step) {
@@ -756,10 +757,10 @@ __device__ __forceinline__ void split_weights(floatx4 a, floatx4 b, bf16x8& hi, 
 // straight into its registers, 16 KB of steps ahead of their use, without LDS or barriers; the workgroup's waves take the
 // chunk's steps in turn and add up at the end.  Two workgroups per CU (256 registers a wave) keep 128 KB of loads in
 // flight on a CU; matrix products are nearly free beside them, and a row block of up to 16 rows costs no more than one row.
-// Measured: a token of 64 sequences of 526 to 8138 keys, 695 MB of bf16 cache in 124 us (5.6 TB/s); the same in e4m3 72 us
-// (4.8 TB/s); one sequence of 131072 keys 96 us (5.6 TB/s).  With few items what bounds it is the load path of a CU: 776
-// keys of one sequence, 8 workgroups, 1 us per 128 keys, since a K operand's load touches 64 bytes of 16 rows, a third of
-// that path's rate; eight waves a workgroup there gained nothing.
+// Measured: a token of 64 sequences of 526 to 8138 keys, 695 MB of bf16 cache in 125 us (5.6 TB/s; reads alone reach 6.4); the
+// same in e4m3 74 us (4.7 TB/s); one sequence of 131072 keys 94 us (5.7 TB/s).  With few items what bounds it is the load path
+// of a CU: 776 keys of one sequence, 8 workgroups, 1 us per 128 keys, since a K operand's load touches 64 bytes of 16 rows, a
+// third of that path's rate; eight waves a workgroup there gained nothing.
 //   S^T = K Q^T: the A operand's row 4 a + b of 16-key half t is key 16 t + 4 b + a, so that a lane's results st[t][e] are
 // keys 16 t + 4 e + lg of query l16.
 //   O^T = V^T P^T: with contraction element j of lane group lg standing for key 4 j + lg, the weights are the B operand as
@@ -1060,8 +1061,9 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
 // operand orders these are): a bf16 cache is copied there without registers, e4m3 codes are loaded a block ahead, made
 // bf16 with their scale and stored.  A wave has two tiles of 16 rows, so that every K and V operand read from LDS feeds
 // both tiles' products: LDS reads are what a block costs most beside the products (one tile a wave: 175 us against 164).
-// Measured: 2048 new tokens behind 8192, 16 query heads of 128, 157 us and 10 of joining, 155 GFLOP (0.93 PFLOP/s
-// with both; a large product of a library reaches 1.2).  Products and the softmax's vector work of a SIMD's two waves hardly
+// Measured: 2048 new tokens behind 8192, 16 query heads of 128, 155 GFLOP in 166 us with joining, calls one after another (0.93
+// PFLOP/s; a large product of a library reaches 1.2); in a trace of ten calls, at a lower clock, 177 us and 11 of joining.  From
+// an e4m3 cache 195 us.  Products and the softmax's vector work of a SIMD's two waves hardly
 // overlap; with the next block's scores formed beside this block's weights in one wave it took 181 us (all 256 registers),
 // and 218 against 196 with the order prescribed to the compiler.
 template <int DH, typename CT>
