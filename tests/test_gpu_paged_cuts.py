@@ -101,3 +101,40 @@ def test_a_table_as_wide_as_the_longest_context(cache, new, lens):
     """Short sequences under a table of 131072 keys: cut and joined, or not, by what they hold."""
     p, _, _ = _run("wide table", cache, 16, 8, 128, 64, [new] * len(lens), lens, width=2048)
     assert p["spare"] > 0
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_pieces_captured_and_on_two_streams(cache):
+    """Blocks of 128 rows, cut and joined: a captured call replays with other lengths and queries, eager calls between, bit by bit as
+    those; two streams at once with a workspace each do too."""
+    H, Hkv, d, page, n, new = 6, 3, 128, 32, 4, 60
+    old = [3000, 40, 1000, 0]
+    lens = [new + x for x in old]
+    print("case: pieces captured", cache, flush=True)
+    table, n_pages = pc.pages_for([x + 300 for x in lens], page, 3)
+    p = rule.plan(n, new, H, Hkv, page, table.shape[1], 0)
+    assert p["rb"] == 128 and p["spare"] > 0 and len(rule.items(p, [new] * n, lens)[0]) > p["blocks"]
+    kc, tab = cuda(*pc.make_cache(n_pages, Hkv, page, d, cache, 4)), torch.from_numpy(table).cuda()
+    qs = [normal(60 + i, n, new, H, d).cuda() for i in range(3)]
+    ats = [torch.tensor([x + 100 * i for x in lens], dtype=torch.int32).cuda() for i in range(3)]
+    need = rule.workspace(p, Hkv, d)
+    ws = [torch.empty(need, dtype=torch.uint8, device="cuda") for _ in range(3)]
+    want = [pc.attend(q, kc, tab, at, workspace=ws[0]) for q, at in zip(qs, ats)]
+    q, at, o = qs[0].clone(), ats[0].clone(), torch.empty_like(qs[0])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        pc.attend(q, kc, tab, at, o=o, workspace=ws[1])
+    for i in (0, 1, 2, 0):
+        q.copy_(qs[i])
+        at.copy_(ats[i])
+        graph.replay()
+        again = pc.attend(qs[i], kc, tab, ats[i], workspace=ws[0])
+        torch.cuda.synchronize()
+        assert torch.equal(o, want[i]) and torch.equal(again, want[i]), i
+    streams, got = [torch.cuda.Stream() for _ in range(3)], []
+    for st, x, y, w in zip(streams, qs, ats, ws):
+        with torch.cuda.stream(st):
+            got.append([pc.attend(x, kc, tab, y, workspace=w) for _ in range(4)])
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, w) for xs, w in zip(got, want) for x in xs)
