@@ -504,6 +504,129 @@ gdn_status gdn_attention_paged(const void* q, const void* k_cache, const void* v
                                int io_dtype, int cache_dtype, float scale,
                                void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * A step's pages and slots, from the lengths of n sequences on the device: the tables that gdn_kv_append and
+ * gdn_attention_paged read, kept against a pool of free pages, so that a captured step needs no host.
+ *
+ * Sequence i needs the pages of its first seq_lens[i] tokens (a negative length counts as 0, positions from
+ * max_pages * page on as none) and has held[i] of them, the entries block_table[i, 0 .. held[i]).
+ * The first shared[i] entries are pages that belong to others (a prefix, see gdn_attention_shared): the
+ * caller writes them and counts them in held; they stay, whatever the length.
+ *   1. Pages that sequences no longer need are put behind the pool's last, free_pages[n_free ..], in
+ *      order of sequence and entry; their entries become -1.
+ *   2. Missing pages, in the same order, are the pool's last ones, in the pool's order: what one call
+ *      takes and the next gives back lies there as before.  Where the pool holds fewer, the first missing
+ *      ones get them, the entries of the others become -1, and missing[0] says how many (else 0).
+ * held and n_free are updated; free_pages from the new n_free on is what the two steps left there.
+ *
+ *   seq_lens    [n] int32; a page that is given back must lie in [0, n_pages) and be held once
+ *   block_table [n, max_pages], held [n], free_pages [n_pages], n_free [1]  int32, updated IN PLACE
+ *               (held and n_free outside [0, max_pages], [0, n_pages] count as the nearest)
+ *   shared      [n] int32, or NULL (none);  missing [1] int32, written, or NULL
+ *   page, n_pages, max_pages  as gdn_kv_append; n * max_pages below 2^31
+ * For the rows of a step (all optional, with the tables as updated):
+ *   rows        tokens of the call, B * T of the layers' entry points
+ *   new_lens    [n] int32: the new tokens of each sequence, packed behind one another (a padded batch:
+ *               rows behind the last sequence); or NULL: rows / n each
+ *   cu_seqlens  [n + 1] int32, written: the new tokens' offsets, clamped to rows; must be given with new_lens
+ *   positions   [rows] int32, written: the i-th of m new tokens of s stands at seq_lens[s] - m + i
+ *               (rows behind the last sequence: 0)
+ *   slots       [rows] int64, written: block_table[s, position / page] * page + position % page, or -1 where
+ *               there is no page, and behind the last sequence
+ * Errors: GDN_ERR_INVALID_ARG, GDN_ERR_UNSUPPORTED (another page, sizes too large).  Needs no workspace.
+ */
+gdn_status gdn_cache_tables(const int32_t* seq_lens, const int32_t* new_lens, const int32_t* shared,
+                            int32_t* block_table, int32_t* held, int32_t* free_pages, int32_t* n_free, int32_t* missing,
+                            int32_t* cu_seqlens, int32_t* positions, int64_t* slots,
+                            int n, int rows, int page, int n_pages, int max_pages, void* stream);
+
+/*
+ * Workspace (device scratch, bytes) of gdn_attention_shared for these sizes (n_seqs = 0: dense).  Pure host
+ * arithmetic; 0 for arguments that it would reject.
+ */
+size_t gdn_attention_shared_workspace_bytes(int B, int T, int H, int H_kv, int d, int page, int max_pages, int n_seqs,
+                                            int n_groups);
+
+/*
+ * gdn_attention_paged for a batch whose sequences share long prefixes: the same result, with a prefix's keys and
+ * values read once for all new tokens of its group instead of once a sequence.
+ *
+ *   prefix_lens [n_groups] int32 DEVICE: tokens at the front of every sequence of the group that lie in the
+ *               same pages; rounded down to whole pages (below 0 as 0)
+ *   cu_groups, n_groups  DEVICE int32 [n_groups + 1]: group g is the sequences cu_groups[g] ..
+ *               cu_groups[g + 1] - 1 (cu_groups[0] = 0; offsets outside the contract are clamped into a
+ *               nondecreasing partition of [0, n]; sequences behind the last group have no prefix); or NULL
+ *               and 1: one group of all.  1 <= n_groups <= n
+ * A sequence whose new tokens do not all stand at or behind the group's prefix (a finished or shorter one) is
+ * attended by itself.  The prefix's pages are those of the group's first sequence that does reach behind it.
+ * Everything else as gdn_attention_paged: causal, pages that are not there, special values, errors, rounding
+ * (the weights of a prefix that many rows share are rounded to bf16); at most 2048 sequences
+ * (GDN_ERR_UNSUPPORTED).  workspace: at least gdn_attention_shared_workspace_bytes(...), 256-byte aligned, its
+ * contents on entry ignored; calls that may overlap in time, captured graphs among them, need one each.
+ */
+gdn_status gdn_attention_shared(const void* q, const void* k_cache, const void* v_cache,
+                                const float* k_scale, const float* v_scale,
+                                const int32_t* block_table, const int32_t* seq_lens,
+                                const int32_t* prefix_lens, const int32_t* cu_groups, int n_groups, void* o,
+                                int B, int T, int H, int H_kv, int d, int page, int n_pages, int max_pages,
+                                const int32_t* cu_seqlens, int n_seqs,
+                                int io_dtype, int cache_dtype, float scale,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * A recurrent layer over a few tokens of each sequence (the token chosen last and drafts behind it), with the state
+ * left at the last token that is kept: gdn_decode_step_ex for several tokens in one pass over the state.  All
+ * tokens' outputs are those of the recurrence; the state becomes the one after the first keep[s] tokens.  So a
+ * step of drafted decoding takes the outputs with keep = 0 (S stays) and, once the drafts are verified, the kept
+ * tokens alone (q and o NULL, keep = the counts of gdn_draft_verify).
+ *
+ *   q, k     [B, T, H_k, dk]   io_dtype;  q NULL: no outputs (then o is NULL, too)
+ *   v, o     [B, T, H, dv]     io_dtype
+ *   g, beta  [B, T, H]         fp32
+ *   S        [n, H, dv, dk]    fp32, read, and updated IN PLACE where a token is kept
+ *   keep     [n] int32 DEVICE (clamped to 0 .. the sequence's tokens), or NULL: all
+ *   cu_seqlens, n_seqs  packed sequences as in gdn_attention_prefill (a padded batch: rows behind the last
+ *            sequence are neither read nor written), or NULL and 0: T tokens for each of B sequences
+ *   flags    0, GDN_QK_L2NORM, GDN_GATE_LOGITS as gdn_chunk_prefill_ex
+ *   dk, dv   64 or 128;  1 <= H_k <= H, H_k divides H;  T >= 0
+ * What a token that is not kept brings (values that are not finite, say) does not reach the state.  A long prompt is
+ * gdn_chunk_prefill's.  Alignment as gdn_decode_step.  Needs no workspace.
+ */
+gdn_status gdn_draft_step(const void* q, const void* k, const void* v, const float* g, const float* beta,
+                          float* S, void* o, const int32_t* keep,
+                          int B, int T, int H, int H_k, int dk, int dv,
+                          const int32_t* cu_seqlens, int n_seqs, int io_dtype, float scale, int flags, void* stream);
+
+/* Workspace (device scratch, bytes) of gdn_draft_verify; 0 for arguments that it would reject. */
+size_t gdn_draft_verify_workspace_bytes(int n, int m, int V);
+
+/*
+ * Which drafted tokens the target's probabilities accept, and the token that follows them, from given random
+ * numbers, so that the tokens are distributed as the target's: of the sequence's drafts x_0 .. x_{len-1},
+ *
+ *     x_j is accepted while  u_j q_j(x_j) < p_j(x_j),
+ *
+ * and the next token is drawn by u_m from max(p_j - q_j, 0) of the first j that is not accepted, or from p_len
+ * behind the last: the lowest v with  w_0 + .. + w_v > u_m W,  W the sum of all w.
+ *
+ *   p          rows of V probabilities (dtype GDN_F32 or GDN_BF16), row s * (m + 1) + j after j drafts of sequence s;
+ *              p_stride elements from one row to the next (V or more)
+ *   q          rows of V that the drafts were drawn from, row s * m + j, q_stride apart; or NULL: every
+ *              draft was certain (1 for it, 0 for any other)
+ *   drafts     [n, m] int32 (one outside [0, V) is not accepted);  draft_lens [n] int32 (clamped to 0 .. m), or NULL: m
+ *   u          [n, m + 1] fp32 in [0, 1): one for each draft, the last for the next token (1 or more: the last
+ *              token that has any probability; below 0 or NaN: as 0)
+ *   tokens     [n, m + 1] int32: the accepted drafts, the next token, then -1
+ *   counts     [n] int32: the tokens gained, accepted drafts and the next token
+ * p and q need not sum to 1 exactly; entries that are not positive and finite count as 0.  Where no
+ * max(p_j - q_j, 0) is positive the token is drawn from p_j; where p_j holds nothing either it is -1.
+ * Comparisons are exact and sums formed in 64 bits, in a fixed order.  m = 0: drafts, draft_lens and q NULL,
+ * one token is drawn from each row.
+ */
+gdn_status gdn_draft_verify(const void* p, const void* q, const int32_t* drafts, const int32_t* draft_lens, const float* u,
+                            int32_t* tokens, int32_t* counts, int n, int m, int V, long long p_stride, long long q_stride,
+                            int dtype, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -23,6 +23,8 @@ __all__ = [
     "gdn_workspace_status", "GDN_ERR_WAIT", "GDN_TEST_WITHHOLD",
     "GDN_E4M3", "GDN_ROPE_INTERLEAVED", "gdn_qk_norm_rope", "gdn_kv_append", "gdn_attention_paged",
     "gdn_attention_paged_workspace_bytes",
+    "gdn_cache_tables", "gdn_attention_shared", "gdn_attention_shared_workspace_bytes", "gdn_draft_step", "gdn_draft_verify",
+    "gdn_draft_verify_workspace_bytes",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -94,6 +96,18 @@ def lib():
         L.gdn_attention_paged_workspace_bytes.restype = S
         L.gdn_attention_paged.argtypes = [P] * 8 + [I] * 8 + [P, I, I, I, F, P, S, P]
         L.gdn_attention_paged.restype = I
+        L.gdn_cache_tables.argtypes = [P] * 11 + [I] * 5 + [P]
+        L.gdn_cache_tables.restype = I
+        L.gdn_attention_shared_workspace_bytes.argtypes = [I] * 9
+        L.gdn_attention_shared_workspace_bytes.restype = S
+        L.gdn_attention_shared.argtypes = [P] * 9 + [I, P] + [I] * 8 + [P, I, I, I, F, P, S, P]
+        L.gdn_attention_shared.restype = I
+        L.gdn_draft_step.argtypes = [P] * 8 + [I] * 6 + [P, I, I, F, I, P]
+        L.gdn_draft_step.restype = I
+        L.gdn_draft_verify_workspace_bytes.argtypes = [I] * 3
+        L.gdn_draft_verify_workspace_bytes.restype = S
+        L.gdn_draft_verify.argtypes = [P] * 7 + [I] * 3 + [LL, LL, I, P, S, P]
+        L.gdn_draft_verify.restype = I
         L.gdn_workspace_status.argtypes = [P, S, P]
         L.gdn_workspace_status.restype = I
         _lib = L
@@ -614,3 +628,173 @@ def gdn_attention_paged(q, k_cache, v_cache, block_table, seq_lens, *, k_scale=N
     _on(dev, lib().gdn_attention_paged, qp, kc, vc, ksc, vsc, table, lens, op, B, T, H, Hkv, d, page, n_pages, max_pages, cu,
         n_seqs, GDN_BF16, ct, d ** -0.5 if scale is None else scale, ws if size else None, size)
     return o
+
+
+_TABLES_NAMES = ("seq_lens", "block_table", "held", "free_pages", "n_free", "shared", "missing", "new_lens", "cu_seqlens",
+                 "positions", "slots")
+
+
+def gdn_cache_tables(seq_lens, block_table, held, free_pages, n_free, page, *, shared=None, missing=None, new_lens=None,
+                     cu_seqlens=None, positions=None, slots=None):
+    """A step's pages from a pool, and its offsets, positions and slots; see ``gdn_cache_tables`` in include/gdn.h.
+
+    ``seq_lens`` [n], ``block_table`` [n,max_pages], ``held`` [n], ``free_pages`` [n_pages] and ``n_free`` [1] int32, all
+    but the first updated in place.  With ``positions`` (int32) or ``slots`` (int64) the call's rows are theirs: [n,T], or
+    packed, [rows], with ``new_lens`` [n] and ``cu_seqlens`` [n+1] int32.  Returns (cu_seqlens, positions, slots).
+    """
+    _dev(seq_lens, "seq_lens", _I32)
+    dev = seq_lens.get_device()
+    at = _addresses(dev, (seq_lens, block_table, held, free_pages, n_free, shared, missing, new_lens, cu_seqlens, positions, slots),
+                    _TABLES_NAMES, (_I32,) * 10 + (torch.int64,))
+    if None in at[:5]:
+        raise TypeError("%s must be a CUDA (HIP) tensor" % _TABLES_NAMES[at.index(None)])
+    n = seq_lens.numel()
+    if seq_lens.dim() != 1 or block_table.dim() != 2 or block_table.shape[0] != n or free_pages.dim() != 1:
+        raise ValueError("seq_lens must be [n], block_table [n, max_pages] and free_pages [n_pages], got %s, %s and %s" % (
+            tuple(seq_lens.shape), tuple(block_table.shape), tuple(free_pages.shape)))
+    for name, t, size in (("held", held, n), ("n_free", n_free, 1), ("shared", shared, n), ("missing", missing, 1),
+                          ("new_lens", new_lens, n), ("cu_seqlens", cu_seqlens, n + 1)):
+        _shaped(t, name, (size,))
+    rows = 0 if positions is None and slots is None else (slots if positions is None else positions).numel()
+    if positions is not None and slots is not None and slots.numel() != rows:
+        raise ValueError("positions and slots must have the same rows, got %s and %s" % (tuple(positions.shape), tuple(slots.shape)))
+    if rows == 0 and cu_seqlens is not None:
+        raise ValueError("cu_seqlens needs the call's rows: positions or slots")
+    lens, table, hp, fp, nf, sh, mp, nl, cu, pos, sl = at
+    _on(dev, lib().gdn_cache_tables, lens, nl, sh, table, hp, fp, nf, mp, cu, pos, sl, n, rows, page, free_pages.numel(),
+        block_table.shape[1])
+    return cu_seqlens, positions, slots
+
+
+def gdn_attention_shared_workspace_bytes(B, T, H, H_kv, d, page, max_pages, n_seqs=0, n_groups=1) -> int:
+    return int(lib().gdn_attention_shared_workspace_bytes(B, T, H, H_kv, d, page, max_pages, n_seqs, n_groups))
+
+
+_SHARED_NAMES = ("q", "prefix_lens", "cu_groups", "o", "workspace")
+
+
+def gdn_attention_shared(q, k_cache, v_cache, block_table, seq_lens, prefix_lens, *, cu_groups=None, k_scale=None, v_scale=None,
+                         scale=None, cu_seqlens=None, o=None, workspace=None):
+    """``gdn_attention_paged`` where groups of sequences share a prefix; see ``gdn_attention_shared`` in include/gdn.h.
+
+    ``prefix_lens`` [n_groups] int32: tokens at the front of each group's sequences that lie in the same pages;
+    ``cu_groups`` [n_groups+1] int32 offsets among the sequences (None: one group of all).  Returns o.
+    """
+    _dev(q, "q", _BF16)
+    if q.dim() != 4:
+        raise ValueError("q must be [B, T, heads, d], got %s" % (tuple(q.shape),))
+    shape = B, T, H, d = q.shape
+    dev = q.get_device()
+    if o is None:
+        o = torch.empty(shape, device=q.device, dtype=_BF16)
+    (kc, vc, table, lens, cu, ksc, vsc), Hkv, page, n_pages, max_pages, n_seqs, ct = _cache_args(
+        dev, k_cache, v_cache, block_table, seq_lens, cu_seqlens, k_scale, v_scale, B, None, d)
+    if not isinstance(prefix_lens, torch.Tensor) or prefix_lens.dim() != 1:
+        raise TypeError("prefix_lens must be a CUDA (HIP) tensor [n_groups]")
+    groups = prefix_lens.numel()
+    if workspace is None:
+        need = lib().gdn_attention_shared_workspace_bytes(B, T, H, Hkv, d, page, max_pages, n_seqs, groups)
+        workspace = torch.empty(need, device=q.device, dtype=torch.uint8) if need else None
+    qp, pre, cg, op, ws = _addresses(dev, (q, prefix_lens, cu_groups, o, workspace), _SHARED_NAMES,
+                                     (_BF16, _I32, _I32, _BF16, torch.uint8))
+    _shaped(o, "o", shape)
+    _shaped(cu_groups, "cu_groups", (groups + 1,))
+    size = 0 if ws is None else workspace.numel()
+    _on(dev, lib().gdn_attention_shared, qp, kc, vc, ksc, vsc, table, lens, pre, cg, groups, op, B, T, H, Hkv, d, page, n_pages,
+        max_pages, cu, n_seqs, GDN_BF16, ct, d ** -0.5 if scale is None else scale, ws if size else None, size)
+    return o
+
+
+_DRAFT_NAMES = ("q", "k", "v", "g", "beta", "S", "keep", "cu_seqlens", "o")
+
+
+def gdn_draft_step(q, k, v, g, beta, S, *, keep=None, flags=0, scale=1.0, cu_seqlens=None, o=None):
+    """A few tokens of each sequence through a recurrent layer, the state left at the last kept one; see
+    ``gdn_draft_step`` in include/gdn.h.
+
+    q (None: no outputs), k [B,T,H_k,dk] and v [B,T,H,dv], fp32 or bf16; g, beta [B,T,H] fp32; ``S`` [n,H,dv,dk] fp32 is
+    updated in place to the state after the first ``keep`` [n] (int32; None: all) tokens.  Packed sequences: B == 1 and
+    ``cu_seqlens`` [n+1] int32.  Returns o (None without q).
+    """
+    if not isinstance(k, torch.Tensor) or k.dtype not in _IO:
+        raise TypeError("k must be float32 or bfloat16")
+    io = k.dtype
+    _dev(k, "k", io)
+    dev = k.get_device()
+    if k.dim() != 4 or not isinstance(v, torch.Tensor) or v.dim() != 4:
+        raise ValueError("k must be [B, T, H_k, dk] and v [B, T, H, dv]")
+    B, T, HK, dk = k.shape
+    H, dv = v.shape[2], v.shape[3]
+    n_seqs = 0 if cu_seqlens is None else cu_seqlens.numel() - 1
+    n = B if cu_seqlens is None else n_seqs
+    if q is None and o is not None:
+        raise ValueError("o without q")
+    if q is not None and o is None:
+        o = torch.empty(v.shape, device=v.device, dtype=io)
+    qp, kp, vp, gp, bp, sp, keepp, cu, op = _addresses(dev, (q, k, v, g, beta, S, keep, cu_seqlens, o), _DRAFT_NAMES,
+                                                       (io, io, io, _F32, _F32, _F32, _I32, _I32, io))
+    for name, t, shape in (("q", q, k.shape), ("v", v, (B, T, H, dv)), ("g", g, (B, T, H)), ("beta", beta, (B, T, H)),
+                           ("S", S, (n, H, dv, dk)), ("keep", keep, (n,)), ("o", o, v.shape)):
+        _shaped(t, name, shape)
+    _on(dev, lib().gdn_draft_step, qp, kp, vp, gp, bp, sp, op, keepp, B, T, H, HK, dk, dv, cu, n_seqs, _IO[io], float(scale),
+        int(flags))
+    return o
+
+
+def gdn_draft_verify_workspace_bytes(n, m, V) -> int:
+    return int(lib().gdn_draft_verify_workspace_bytes(n, m, V))
+
+
+_VERIFY_NAMES = ("drafts", "draft_lens", "u", "tokens", "counts", "workspace")
+
+
+def _probabilities(t, name, shape):
+    """(address, elements between rows, device) of t [n, rows, V]: a row's values contiguous, rows equally far apart."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a CUDA (HIP) tensor" % name)
+    if t.dtype not in _IO:
+        raise TypeError("%s must be float32 or bfloat16, got %s" % (name, t.dtype))
+    if t.dim() != 3 or (shape is not None and t.shape != shape):
+        raise ValueError("%s must be %s, got %s" % (name, "[n, m + 1, V]" if shape is None else tuple(shape), tuple(t.shape)))
+    n, rows, V = t.shape
+    step = V
+    if not t.is_contiguous():
+        sn, sr, sv = t.stride()
+        if (sv != 1 and V > 1) or (n > 1 and rows > 1 and sn != rows * sr):
+            raise ValueError("%s: a row's values must be contiguous and the rows equally far apart" % name)
+        step = sr if rows > 1 else sn if n > 1 else step
+    return t.data_ptr(), step, t.get_device()
+
+
+def gdn_draft_verify(p, u, *, drafts=None, q=None, draft_lens=None, tokens=None, counts=None, workspace=None):
+    """Drafted tokens against the target's probabilities; see ``gdn_draft_verify`` in include/gdn.h.
+
+    p [n,m+1,V] and q [n,m,V] (None: the drafts were certain) fp32 or bf16, parts of wider rows or not; ``u`` [n,m+1]
+    fp32 in [0, 1); ``drafts`` [n,m] int32 (None: m = 0), ``draft_lens`` [n] int32 (None: m each).  Returns
+    (tokens [n,m+1], counts [n]) int32: the accepted drafts and the token behind them, then -1.
+    """
+    pp, ps, dev = _probabilities(p, "p", None)
+    n, m, V = p.shape[0], p.shape[1] - 1, p.shape[2]
+    qp, qs = None, 0
+    if q is not None:
+        qp, qs, qdev = _probabilities(q, "q", (n, m, V))
+        if q.dtype is not p.dtype or qdev != dev:
+            raise ValueError("p and q must have one type and device")
+    if tokens is None:
+        tokens = torch.empty((n, m + 1), device=p.device, dtype=_I32)
+    if counts is None:
+        counts = torch.empty((n,), device=p.device, dtype=_I32)
+    if workspace is None:
+        need = lib().gdn_draft_verify_workspace_bytes(n, m, V)
+        workspace = torch.empty(need, device=p.device, dtype=torch.uint8) if need else None
+    at = _addresses(dev, (drafts, draft_lens, u, tokens, counts, workspace), _VERIFY_NAMES,
+                    (_I32, _I32, _F32, _I32, _I32, torch.uint8))
+    if at[2] is None:
+        raise TypeError("u must be a CUDA (HIP) tensor")
+    for name, t, shape in (("drafts", drafts, (n, m)), ("draft_lens", draft_lens, (n,)), ("u", u, (n, m + 1)),
+                           ("tokens", tokens, (n, m + 1)), ("counts", counts, (n,))):
+        _shaped(t, name, shape)
+    dp, lp, up, tp, cp, ws = at
+    size = 0 if ws is None else workspace.numel()
+    _on(dev, lib().gdn_draft_verify, pp, qp, dp, lp, up, tp, cp, n, m, V, ps, qs, _IO[p.dtype], ws if size else None, size)
+    return tokens, counts

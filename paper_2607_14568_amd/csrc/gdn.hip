@@ -2687,6 +2687,8 @@ __global__ __launch_bounds__(NT_ATT / QT) __attribute__((amdgpu_waves_per_eu(4 /
 #include "wide.hip"
 #include "generic.hip"
 #include "paged.hip"
+#include "shared.hip"
+#include "drafts.hip"
 
 // ------------------------------------------------------------------ host side
 thread_local char g_err[512] = "";
@@ -3242,12 +3244,86 @@ void launch_paged(const PagedParams& p, const PagedPlan& plan, hipStream_t st) {
     const dim3 grid((unsigned)(plan.items * p.HKV));
     const long blocks = plan.blocks * p.HKV;
     if (plan.rb == AQ) {
-        hipLaunchKernelGGL((k_attn_tile<DH, CT>), grid, dim3(NT), 0, st, p);
+        hipLaunchKernelGGL((k_attn_tile<DH, CT, PagedParams>), grid, dim3(NT), 0, st, p);
         if (p.spare > 0) hipLaunchKernelGGL((k_attn_join_tile<DH>), dim3((unsigned)blocks, (unsigned)(plan.rows + 15) / 16), dim3(NT), 0, st, p);
         return;
     }
-    hipLaunchKernelGGL((k_attn_rows<DH, CT>), grid, dim3(NT), 0, st, p);
+    hipLaunchKernelGGL((k_attn_rows<DH, CT, PagedParams>), grid, dim3(NT), 0, st, p);
     if (p.spare > 0) hipLaunchKernelGGL((k_attn_join<DH>), dim3((unsigned)blocks, (unsigned)plan.rows), dim3(NT), 0, st, p);
+}
+
+// How gdn_attention_shared lays out a step (pure host arithmetic): rows per block, row blocks and items per key/value head at
+// most, of the groups' prefixes and of the sequences' own keys (k_shared_setup keeps to these numbers).
+struct SharedPlan {
+    int rbp, rbt, round;
+    long blocks_t, items_p, items_t;
+};
+SharedPlan shared_plan(int B, int T, int H, int H_kv, int page, int max_pages, int n_seqs, int groups) {
+    SharedPlan p;
+    const long G = H / H_kv, n = n_seqs > 0 ? n_seqs : B, tokens = (long)B * T, rows = tokens * G;
+    const long units = ((long)page * max_pages + UNIT - 1) / UNIT;
+    p.round = (int)std::max(1L, 2 * PLAN_CUS / H_kv);   // two workgroups per CU
+    p.rbp = rows <= 32L * groups ? 16 : AQ;
+    p.rbt = rows <= 64 * n ? 16 : AQ;
+    const long blocks_p = rows / p.rbp + std::min<long>(groups, tokens);
+    p.blocks_t = n_seqs > 0 ? rows / p.rbt + std::min<long>(n, tokens) : B * ((T * G + p.rbt - 1) / p.rbt);
+    p.items_p = std::min(blocks_p + p.round, blocks_p * units);
+    p.items_t = std::min(p.blocks_t + p.round, p.blocks_t * units);
+    return p;
+}
+struct SharedLayout { size_t seq, grp, group_of, first_p, first_t, block_t, chunk, ml_p, ml_t, o_p, o_t, total; };
+SharedLayout shared_layout(const SharedPlan& p, long n, int groups, int H_kv, int d) {
+    SharedLayout l;
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t x = at;
+        at += round_up(bytes, 256);
+        return x;
+    };
+    const size_t rows_p = (size_t)p.items_p * H_kv * p.rbp, rows_t = (size_t)p.items_t * H_kv * p.rbt;
+    l.seq = take(n * sizeof(int4));
+    l.grp = take(groups * sizeof(int4));
+    l.group_of = take(n * 4);
+    l.first_p = take((groups + 1L) * 4);
+    l.first_t = take((n + 1) * 4);
+    l.block_t = take((n + 1) * 4);
+    l.chunk = take(8);
+    l.ml_p = take(rows_p * sizeof(float2));
+    l.ml_t = take(rows_t * sizeof(float2));
+    l.o_p = take(rows_p * d * 4);
+    l.o_t = take(rows_t * d * 4);
+    l.total = at;
+    return l;
+}
+
+template <int DH, typename CT>
+void launch_shared(const SharedSetup& setup, const SharedJoin& j, const SharedPlan& plan, hipStream_t st) {
+    hipLaunchKernelGGL(k_shared_setup, dim3(1), dim3(NSU), 0, st, setup);
+    auto attend = [&](const SharedParams& p, int rb, long items) {
+        const dim3 grid((unsigned)(items * p.HKV));
+        if (rb == AQ) hipLaunchKernelGGL((k_attn_tile<DH, CT, SharedParams>), grid, dim3(NT), 0, st, p);
+        else hipLaunchKernelGGL((k_attn_rows<DH, CT, SharedParams>), grid, dim3(NT), 0, st, p);
+    };
+    attend(j.g, plan.rbp, plan.items_p);
+    attend(j.t, plan.rbt, plan.items_t);
+    hipLaunchKernelGGL((k_shared_join<DH>), dim3((unsigned)(plan.blocks_t * j.t.HKV), (unsigned)plan.rbt), dim3(NT), 0, st, j);
+}
+
+template <typename IO, int DK>
+void launch_draft(const DraftParams& p, int n, hipStream_t st) {
+    const long heads = (long)n * p.H;
+    if (heads * p.DV < 512 * 64)
+        hipLaunchKernelGGL((k_draft_step<IO, DK, 1, 4>), dim3((unsigned)(heads * (p.DV / 64))), dim3(256), 0, st, p);
+    else if (p.DV == 128)
+        hipLaunchKernelGGL((k_draft_step<IO, DK, 4, 2>), dim3((unsigned)heads), dim3(128), 0, st, p);
+    else
+        hipLaunchKernelGGL((k_draft_step<IO, DK, 4, 1>), dim3((unsigned)heads), dim3(64), 0, st, p);
+}
+
+template <typename IO>
+void launch_verify(const VerifyParams& p, int n, hipStream_t st) {
+    hipLaunchKernelGGL((k_verify_sums<IO>), dim3((unsigned)((long)n * p.slices)), dim3(NT), 0, st, p);
+    hipLaunchKernelGGL((k_verify_pick<IO>), dim3((unsigned)n), dim3(NT), 0, st, p);
 }
 
 }  // namespace
@@ -4009,5 +4085,207 @@ extern "C" gdn_status gdn_attention_paged(const void* q, const void* k_cache, co
         if (d == 128) launch_paged<128, uint8_t>(p, plan, hs);
         else launch_paged<64, uint8_t>(p, plan, hs);
     }
+    return launched();
+}
+
+extern "C" gdn_status gdn_cache_tables(const int32_t* seq_lens, const int32_t* new_lens, const int32_t* shared, int32_t* block_table,
+                                       int32_t* held, int32_t* free_pages, int32_t* n_free, int32_t* missing, int32_t* cu_seqlens,
+                                       int32_t* positions, int64_t* slots, int n, int rows, int page, int n_pages, int max_pages,
+                                       void* stream) {
+    g_err[0] = '\0';
+    if (n < 1 || rows < 0) return fail(GDN_ERR_INVALID_ARG, "n=%d rows=%d out of range", n, rows);
+    if (page < 1 || n_pages < 1 || max_pages < 1)
+        return fail(GDN_ERR_INVALID_ARG, "page=%d n_pages=%d max_pages=%d must be positive", page, n_pages, max_pages);
+    if (!page_known(page)) return fail(GDN_ERR_UNSUPPORTED, "page=%d: only 16, 32, 64 and 128 are implemented", page);
+    if (!table_fits(page, max_pages)) return fail(GDN_ERR_UNSUPPORTED, "max_pages=%d too large", max_pages);
+    if ((long)n * max_pages >= 1L << 31 || rows >= 1 << 30) return fail(GDN_ERR_UNSUPPORTED, "n*max_pages or rows=%d too large", rows);
+    if (!seq_lens || !block_table || !held || !free_pages || !n_free)
+        return fail(GDN_ERR_INVALID_ARG, "seq_lens, block_table, held, free_pages and n_free must be non-null");
+    if (new_lens && !cu_seqlens) return fail(GDN_ERR_INVALID_ARG, "new_lens needs cu_seqlens");
+    if (!new_lens && (cu_seqlens || positions || slots) && rows % n)
+        return fail(GDN_ERR_INVALID_ARG, "rows=%d is no multiple of n=%d, and no new_lens", rows, n);
+    const void* words[] = {seq_lens, new_lens, shared, block_table, held, free_pages, n_free, missing, cu_seqlens, positions};
+    for (const void* w : words)
+        if (!aligned(w, 4)) return fail(GDN_ERR_INVALID_ARG, "pointer %p is not 4-byte aligned", w);
+    if (!aligned(slots, 8)) return fail(GDN_ERR_INVALID_ARG, "slots is not 8-byte aligned");
+    TablesParams p = {};
+    p.lens = seq_lens; p.new_lens = new_lens; p.shared = shared;
+    p.table = block_table; p.held = held; p.free = free_pages; p.n_free = n_free; p.missing = missing;
+    p.cu = cu_seqlens; p.positions = positions; p.slots = slots;
+    p.n = n; p.rows = rows; p.n_pages = n_pages; p.max_pages = max_pages;
+    p.shift = page == 16 ? 4 : page == 32 ? 5 : page == 64 ? 6 : 7;
+    const bool maps = rows > 0 && (positions || slots), here = maps && n <= NTA && rows <= 8 * NTA;
+    hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+    (void)hipGetLastError();
+    hipLaunchKernelGGL(k_cache_tables, dim3(1), dim3(NTA), 0, hs, p, here ? 1 : 0);
+    if (maps && !here) hipLaunchKernelGGL(k_cache_maps, dim3((unsigned)((rows + NT - 1) / NT)), dim3(NT), 0, hs, p);
+    return launched();
+}
+
+// Sequences that gdn_attention_shared takes in one call.
+static bool batch_fits(int B, int n_seqs) { return (n_seqs > 0 ? n_seqs : B) <= SHARED_SEQS; }
+
+extern "C" size_t gdn_attention_shared_workspace_bytes(int B, int T, int H, int H_kv, int d, int page, int max_pages, int n_seqs,
+                                                       int n_groups) {
+    if (B < 1 || T < 1 || H < 1 || H_kv < 1 || H % H_kv || !head_size_known(d) || n_seqs < 0 || (n_seqs > 0 && B != 1) ||
+        !heads_fit(H, d) || !rows_fit(B, T, H) || !page_known(page) || max_pages < 1 || !table_fits(page, max_pages) ||
+        !batch_fits(B, n_seqs) || n_groups < 1 || n_groups > (n_seqs > 0 ? n_seqs : B))
+        return 0;
+    return shared_layout(shared_plan(B, T, H, H_kv, page, max_pages, n_seqs, n_groups), n_seqs > 0 ? n_seqs : B, n_groups, H_kv, d).total;
+}
+
+extern "C" gdn_status gdn_attention_shared(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
+                                           const float* v_scale, const int32_t* block_table, const int32_t* seq_lens,
+                                           const int32_t* prefix_lens, const int32_t* cu_groups, int n_groups, void* o, int B, int T,
+                                           int H, int H_kv, int d, int page, int n_pages, int max_pages, const int32_t* cu_seqlens,
+                                           int n_seqs, int io_dtype, int cache_dtype, float scale, void* workspace,
+                                           size_t workspace_bytes, void* stream) {
+    g_err[0] = '\0';
+    if (io_dtype != GDN_F32 && io_dtype != GDN_BF16)
+        return fail(GDN_ERR_INVALID_ARG, "io_dtype=%d is neither GDN_F32 nor GDN_BF16", io_dtype);
+    gdn_status st = step_sizes(B, T, H, H_kv, d, cu_seqlens, n_seqs);
+    if (st == GDN_OK)
+        st = check_cache(k_cache, v_cache, k_scale, v_scale, block_table, seq_lens, page, n_pages, max_pages, cache_dtype);
+    if (st != GDN_OK) return st;
+    const int n = n_seqs > 0 ? n_seqs : B;
+    if (n_groups < 1 || n_groups > n) return fail(GDN_ERR_INVALID_ARG, "n_groups=%d must lie in 1..%d, the sequences", n_groups, n);
+    if (n_groups > 1 && !cu_groups) return fail(GDN_ERR_INVALID_ARG, "n_groups=%d needs cu_groups", n_groups);
+    if (!prefix_lens) return fail(GDN_ERR_INVALID_ARG, "prefix_lens must be non-null");
+    if (!aligned(prefix_lens, 4) || !aligned(cu_groups, 4))
+        return fail(GDN_ERR_INVALID_ARG, "prefix_lens or cu_groups is not 4-byte aligned");
+    if (io_dtype != GDN_BF16) return fail(GDN_ERR_UNSUPPORTED, "attention is implemented for bf16 io only");
+    if (!batch_fits(B, n_seqs)) return fail(GDN_ERR_UNSUPPORTED, "%d sequences: at most %d are implemented", n, SHARED_SEQS);
+    if (T == 0) return GDN_OK;
+    if (!q || !o) return fail(GDN_ERR_INVALID_ARG, "q and o must be non-null");
+    if (!aligned(q, 16) || !aligned(o, 16)) return fail(GDN_ERR_INVALID_ARG, "q or o is not 16-byte aligned");
+    const SharedPlan plan = shared_plan(B, T, H, H_kv, page, max_pages, n_seqs, n_groups);
+    const SharedLayout lay = shared_layout(plan, n, n_groups, H_kv, d);
+    if (!workspace || workspace_bytes < lay.total)
+        return fail(GDN_ERR_WORKSPACE, "workspace of %zu bytes given, %zu needed", workspace ? workspace_bytes : (size_t)0, lay.total);
+    if (!aligned(workspace, 256)) return fail(GDN_ERR_INVALID_ARG, "workspace is not 256-byte aligned");
+    if (!grid_fits(plan.items_p * H_kv) || !grid_fits(plan.items_t * H_kv) || !grid_fits(plan.blocks_t * H_kv * plan.rbt))
+        return fail(GDN_ERR_UNSUPPORTED, "B*T*H too large");
+    char* const ws = static_cast<char*>(workspace);
+    auto words = [&](size_t at) { return reinterpret_cast<int32_t*>(ws + at); };
+    SharedSetup u = {};
+    u.s.cu = cu_seqlens; u.s.lens = seq_lens; u.s.n = n; u.s.T = T;
+    u.prefix = prefix_lens; u.cu_groups = cu_groups; u.groups = n_groups;
+    u.G = H / H_kv;
+    u.rbp = plan.rbp; u.rbt = plan.rbt; u.round_p = u.round_t = plan.round;
+    u.least_p = plan.rbp == 16 ? 1 : 4;   // (a tile's chunk of fewer keys is mostly joining)
+    u.least_t = plan.rbt == 16 ? 1 : 4;
+    u.grp = reinterpret_cast<int4*>(ws + lay.grp); u.seq = reinterpret_cast<int4*>(ws + lay.seq);
+    u.group_of = words(lay.group_of); u.first_p = words(lay.first_p); u.first_t = words(lay.first_t);
+    u.block_t = words(lay.block_t); u.chunk = words(lay.chunk);
+    SharedJoin j = {};
+    j.t.q = static_cast<const bf16_t*>(q);
+    j.t.o = static_cast<bf16_t*>(o);
+    j.t.H = H; j.t.HKV = H_kv; j.t.G = u.G;
+    j.t.by_hkv = make_div(H_kv); j.t.by_g = make_div(u.G);
+    j.t.scale_log2 = scale * 1.4426950408889634f;
+    j.t.s = u.s;
+    j.t.c = make_cache(k_cache, v_cache, k_scale, v_scale, block_table, page, n_pages, max_pages);
+    u.shift = j.t.c.shift; u.cap = max_pages << j.t.c.shift;
+    j.g = j.t;
+    j.t.part = u.seq; j.t.first = u.first_t; j.t.chunk = u.chunk + 1; j.t.parts = n; j.t.prefix = false;
+    j.g.part = u.grp; j.g.first = u.first_p; j.g.chunk = u.chunk; j.g.parts = n_groups; j.g.prefix = true;
+    j.t.pml = reinterpret_cast<float2*>(ws + lay.ml_t); j.t.po = reinterpret_cast<float*>(ws + lay.o_t);
+    j.g.pml = reinterpret_cast<float2*>(ws + lay.ml_p); j.g.po = reinterpret_cast<float*>(ws + lay.o_p);
+    j.group_of = u.group_of; j.block_t = u.block_t; j.rbp = plan.rbp; j.rbt = plan.rbt;
+    hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+    (void)hipGetLastError();
+    if (cache_dtype == GDN_BF16) {
+        if (d == 128) launch_shared<128, bf16_t>(u, j, plan, hs);
+        else launch_shared<64, bf16_t>(u, j, plan, hs);
+    } else {
+        if (d == 128) launch_shared<128, uint8_t>(u, j, plan, hs);
+        else launch_shared<64, uint8_t>(u, j, plan, hs);
+    }
+    return launched();
+}
+
+extern "C" gdn_status gdn_draft_step(const void* q, const void* k, const void* v, const float* g, const float* beta, float* S, void* o,
+                                     const int32_t* keep, int B, int T, int H, int H_k, int dk, int dv, const int32_t* cu_seqlens,
+                                     int n_seqs, int io_dtype, float scale, int flags, void* stream) {
+    g_err[0] = '\0';
+    if (flags & ~(PRE_L2 | PRE_GATES)) return fail(GDN_ERR_INVALID_ARG, "flags=%d: unknown bits", flags);
+    if (io_dtype != GDN_F32 && io_dtype != GDN_BF16)
+        return fail(GDN_ERR_INVALID_ARG, "io_dtype=%d is neither GDN_F32 nor GDN_BF16", io_dtype);
+    if (B < 1 || T < 0 || H < 1) return fail(GDN_ERR_INVALID_ARG, "B=%d T=%d H=%d out of range", B, T, H);
+    if (H_k < 1 || H_k > H || H % H_k != 0)
+        return fail(GDN_ERR_INVALID_ARG, "H_k=%d key heads must divide the H=%d value heads", H_k, H);
+    gdn_status st = check_dims(dk, dv);
+    if (st != GDN_OK) return st;
+    if ((cu_seqlens == nullptr) != (n_seqs == 0))
+        return fail(GDN_ERR_INVALID_ARG, "cu_seqlens and n_seqs=%d must be given together", n_seqs);
+    if (n_seqs < 0) return fail(GDN_ERR_INVALID_ARG, "n_seqs=%d is negative", n_seqs);
+    if (n_seqs > 0 && B != 1) return fail(GDN_ERR_INVALID_ARG, "packed sequences need B == 1 (got %d)", B);
+    if ((q == nullptr) != (o == nullptr)) return fail(GDN_ERR_INVALID_ARG, "q and o must be given together");
+    if (T == 0) return GDN_OK;
+    if (!k || !v || !g || !beta || !S) return fail(GDN_ERR_INVALID_ARG, "k, v, g, beta and S must be non-null");
+    if (!aligned(S, 16)) return fail(GDN_ERR_INVALID_ARG, "state pointer %p is not 16-byte aligned", (const void*)S);
+    const size_t esz = io_dtype == GDN_BF16 ? 2 : 4;
+    const void* io_ptrs[] = {q, k, v, o};
+    for (const void* ptr : io_ptrs)
+        if (!aligned(ptr, esz)) return fail(GDN_ERR_INVALID_ARG, "pointer %p is not element-aligned", ptr);
+    if (!aligned(g, 4) || !aligned(beta, 4) || !aligned(keep, 4) || !aligned(cu_seqlens, 4))
+        return fail(GDN_ERR_INVALID_ARG, "g, beta, keep or cu_seqlens is not 4-byte aligned");
+    const int n = n_seqs > 0 ? n_seqs : B;
+    if ((long)n * H > 65535L * 64 || (long)B * T >= 1L << 30) return fail(GDN_ERR_UNSUPPORTED, "%ld states or B*T=%ld too large", (long)n * H, (long)B * T);
+    DraftParams p = {};
+    p.q = q; p.k = k; p.v = v; p.g = g; p.beta = beta; p.S = S; p.o = o; p.keep = keep;
+    p.s.cu = cu_seqlens; p.s.n = n; p.s.T = T;
+    p.H = H; p.HK = H_k; p.G = H / H_k; p.DV = dv;
+    p.scale = scale; p.pre = flags;
+    hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+    (void)hipGetLastError();
+    if (io_dtype == GDN_BF16) {
+        if (dk == 128) launch_draft<bf16_t, 128>(p, n, hs);
+        else launch_draft<bf16_t, 64>(p, n, hs);
+    } else {
+        if (dk == 128) launch_draft<float, 128>(p, n, hs);
+        else launch_draft<float, 64>(p, n, hs);
+    }
+    return launched();
+}
+
+static bool vocabulary_fits(int n, int m, int V) {
+    return n >= 1 && m >= 0 && V >= 1 && m < 1 << 20 && V < 1 << 30 && (long)n * (m + 1) < 1L << 30 && grid_fits((long)n * ((V + VS - 1) / VS));
+}
+
+extern "C" size_t gdn_draft_verify_workspace_bytes(int n, int m, int V) {
+    if (!vocabulary_fits(n, m, V)) return 0;
+    return round_up((size_t)n * ((V + VS - 1) / VS) * sizeof(double2), 256);
+}
+
+extern "C" gdn_status gdn_draft_verify(const void* p, const void* q, const int32_t* drafts, const int32_t* draft_lens, const float* u,
+                                       int32_t* tokens, int32_t* counts, int n, int m, int V, long long p_stride, long long q_stride,
+                                       int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+    g_err[0] = '\0';
+    if (dtype != GDN_F32 && dtype != GDN_BF16) return fail(GDN_ERR_INVALID_ARG, "dtype=%d is neither GDN_F32 nor GDN_BF16", dtype);
+    if (n < 1 || m < 0 || V < 1) return fail(GDN_ERR_INVALID_ARG, "n=%d m=%d V=%d out of range", n, m, V);
+    if (!vocabulary_fits(n, m, V)) return fail(GDN_ERR_UNSUPPORTED, "n=%d m=%d V=%d too large", n, m, V);
+    if (!p || !u || !tokens || !counts) return fail(GDN_ERR_INVALID_ARG, "p, u, tokens and counts must be non-null");
+    if ((m == 0) != (drafts == nullptr)) return fail(GDN_ERR_INVALID_ARG, "drafts belong to m=%d > 0", m);
+    if (m == 0 && (q || draft_lens)) return fail(GDN_ERR_INVALID_ARG, "q and draft_lens belong to m > 0");
+    if (p_stride < V || (q && q_stride < V))
+        return fail(GDN_ERR_INVALID_ARG, "rows (strides %lld, %lld) must be V=%d elements or more apart", p_stride, q_stride, V);
+    const size_t esz = dtype == GDN_BF16 ? 2 : 4;
+    if (!aligned(p, esz) || !aligned(q, esz)) return fail(GDN_ERR_INVALID_ARG, "p or q is not element-aligned");
+    if (!aligned(drafts, 4) || !aligned(draft_lens, 4) || !aligned(u, 4) || !aligned(tokens, 4) || !aligned(counts, 4))
+        return fail(GDN_ERR_INVALID_ARG, "drafts, draft_lens, u, tokens or counts is not 4-byte aligned");
+    const size_t need = gdn_draft_verify_workspace_bytes(n, m, V);
+    if (!workspace || workspace_bytes < need)
+        return fail(GDN_ERR_WORKSPACE, "workspace of %zu bytes given, %zu needed", workspace ? workspace_bytes : (size_t)0, need);
+    if (!aligned(workspace, 256)) return fail(GDN_ERR_INVALID_ARG, "workspace is not 256-byte aligned");
+    VerifyParams a = {};
+    a.p = p; a.q = q; a.drafts = drafts; a.lens = draft_lens; a.u = u; a.tokens = tokens; a.counts = counts;
+    a.part = static_cast<double2*>(workspace);
+    a.ps = (long)p_stride; a.qs = (long)q_stride;
+    a.m = m; a.V = V; a.slices = (V + VS - 1) / VS;
+    hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+    (void)hipGetLastError();
+    if (dtype == GDN_BF16) launch_verify<bf16_t>(a, n, hs);
+    else launch_verify<float>(a, n, hs);
     return launched();
 }

@@ -588,6 +588,8 @@ struct Item {
     int rb, nrb;           // row block, of how many
     int c, chunks, chunk, first;   // keys per chunk, chunks, chunk of the item; the sequence's first item (see item_of)
     int end;               // keys that the row block's last row sees
+    int start;             // the first key that the sequence's items take
+    bool direct;           // the block's only partial sums: the item writes the output itself
 };
 
 // Item of chunk j of the row block: chunk by chunk, even ones from the block with the most keys down, odd ones up, so that
@@ -600,6 +602,17 @@ __device__ __forceinline__ int item_of(const Item& it, int j) {
 template <int RB> __device__ __forceinline__ int block_end(const PagedParams& p, int n, int len, int rb) {
     const int i = min(div_by(rb * RB + RB - 1, p.by_g), n - 1);
     return min(max(len - n + i + 1, 0), p.c.max_pages << p.c.shift);
+}
+
+// An item's `keys` in as many chunks as chunks of c units make, all of one size.
+__device__ __forceinline__ void cut_keys(Item& it, int keys, int c) {
+    it.chunks = 1;
+    it.c = max(keys, 1);
+    if (keys > c * UNIT) {
+        it.chunks = (keys + c * UNIT - 1) / (c * UNIT);
+        it.c = ((keys + it.chunks - 1) / it.chunks + UNIT - 1) / UNIT * UNIT;
+        it.chunks = (keys + it.c - 1) / it.c;
+    }
 }
 
 // Item w of a key/value head (BLOCK: row block w instead, chunk 0).  Called by a whole wave; false past the last.
@@ -671,13 +684,9 @@ template <int RB, bool BLOCK = false> __device__ __forceinline__ bool find_item(
             it.rb = it.chunk % 2 ? z : it.nrb - 1 - z;   // see item_of
             it.first = fi;
             it.end = block_end<RB>(p, it.n, it.len, it.rb);
-            it.chunks = 1;
-            it.c = max(it.end, 1);
-            if (it.end > c * UNIT) {   // as many chunks as chunks of c units make, all of one size
-                it.chunks = (it.end + c * UNIT - 1) / (c * UNIT);
-                it.c = ((it.end + it.chunks - 1) / it.chunks + UNIT - 1) / UNIT * UNIT;
-                it.chunks = (it.end + it.c - 1) / it.c;
-            }
+            cut_keys(it, it.end, c);
+            it.start = 0;
+            it.direct = it.chunks == 1;
             return true;
         }
         items += last_lane(si);
@@ -685,6 +694,10 @@ template <int RB, bool BLOCK = false> __device__ __forceinline__ bool find_item(
     }
     return false;
 }
+
+// The same kernels over other parts of a step's keys (shared.hip): that form's parameters and its item search.
+struct SharedParams;
+template <int RB> __device__ __forceinline__ bool find_item(const SharedParams& p, int w, Item& it);
 
 // Pages of a walk over a sequence's keys: lane i holds entry i of 64 of its table (and, e4m3, its scales), so that a step
 // takes its page without waiting for memory.  Asked for in rising order.
@@ -847,8 +860,8 @@ __device__ __forceinline__ void plain_row(const PagedParams& p, const Item& it, 
     }
 }
 
-template <int DH, typename CT>
-__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_attn_rows(PagedParams p) {
+template <int DH, typename CT, typename P>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_attn_rows(P p) {
     constexpr int NW = NT / 64, RB = 16, CW = DH / 16, ESZ = sizeof(CT), NKB = DH / 32, NK = DH * ESZ / 64, VD = CW * ESZ / 4;
     constexpr bool E4M3 = ESZ == 1;
     __shared__ __align__(16) float lds_o[NW][RB][DH + 4];   // (rows 4 banks apart: 16 rows' 16-byte accesses meet no bank twice)
@@ -859,7 +872,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
     const int w = div_by(blockIdx.x, p.by_hkv), hk = (int)blockIdx.x - w * p.HKV;
     Item it;
     if (!find_item<RB>(p, w, it) || it.chunk >= it.chunks) return;
-    const int k0 = it.chunk * it.c, k1 = min(it.end - k0, it.c) + k0;   // the item's keys
+    const int k0 = it.start + it.chunk * it.c, k1 = min(it.end - k0, it.c) + k0;   // the item's keys
     const int rows = min(it.n * p.G - it.rb * RB, RB);
     const int row = it.rb * RB + l16, qi = div_by(row, p.by_g);
     const int last = it.len - it.n + qi, last0 = it.len - it.n + div_by(it.rb * RB, p.by_g);   // this lane's row, and the block's first
@@ -1041,7 +1054,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
 #pragma unroll
         for (int n = 0; n < CW / 4; ++n) o[n] += a * f4(&lds_o[z][r][c0 + 4 * n]);
     }
-    if (it.chunks == 1) {
+    if (it.direct) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;   // no key: zeros
         const int rr = it.rb * RB + r, i = div_by(rr, p.by_g);
         bf16_t* dst = p.o + ((long)(it.tok + i) * p.H + hk * p.G + rr - i * p.G) * DH + c0;
@@ -1066,8 +1079,8 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
 // an e4m3 cache 195 us.  Products and the softmax's vector work of a SIMD's two waves hardly
 // overlap; with the next block's scores formed beside this block's weights in one wave it took 181 us (all 256 registers),
 // and 218 against 196 with the order prescribed to the compiler.
-template <int DH, typename CT>
-__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2))) void k_attn_tile(PagedParams p) {
+template <int DH, typename CT, typename P>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2))) void k_attn_tile(P p) {
     constexpr bool E4M3 = sizeof(CT) == 1;
     constexpr int RB = AQ, QT = 2, NW = NT / 64, NCH = DH / 8, RPI = 64 / NCH, NKB = DH / 32, NDT = DH / 16, ESZ = sizeof(CT);
     // (a variable per ring slot: the compiler then sees that reads of one do not wait for the copies into the other)
@@ -1078,7 +1091,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2))) void k_
     const int w = div_by(blockIdx.x, p.by_hkv), hk = (int)blockIdx.x - w * p.HKV;
     Item it;
     if (!find_item<RB>(p, w, it) || it.chunk >= it.chunks) return;
-    const int k0 = it.chunk * it.c, k1 = min(it.end - k0, it.c) + k0;
+    const int k0 = it.start + it.chunk * it.c, k1 = min(it.end - k0, it.c) + k0;
     const int rows = it.n * p.G, base = it.len - it.n;   // rows of the sequence; position of its first new token
     const int r0 = it.rb * RB + 16 * QT * wave;          // this wave's first row
     const int wlast = r0 < rows ? base + div_by(min(r0 + 16 * QT - 1, rows - 1), p.by_g) : -1;   // the last key that its rows see
@@ -1381,7 +1394,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2))) void k_
         l[u] += __shfl_xor(l[u], 32, 64);
         const int r = r0 + 16 * u + l16;
         if (r >= rows) continue;
-        if (it.chunks == 1) {
+        if (it.direct) {
             const float inv = l[u] == 0.f ? 0.f : 1.f / l[u];   // no key: zeros
             const int i = div_by(r, p.by_g);
             bf16_t* dst = p.o + ((long)(it.tok + i) * p.H + hk * p.G + r - i * p.G) * DH + 4 * lg;
