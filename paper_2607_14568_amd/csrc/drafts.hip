@@ -39,18 +39,7 @@ __device__ __forceinline__ void map_none(const TablesParams& p, int t) {
     if (p.slots) p.slots[t] = -1;
 }
 
-// The first index i of [0, n) with ends[i] > x (ends nondecreasing), n where there is none.
-__device__ __forceinline__ int first_past(const int32_t* ends, int n, int x) {
-    int lo = 0, hi = n;
-    while (lo < hi) {
-        const int mid = (lo + hi) / 2;
-        if (ends[mid] > x) hi = mid; else lo = mid + 1;
-    }
-    return lo;
-}
-
 constexpr int NTA = 1024;   // threads of k_cache_tables, and sequences that it takes at a time
-static_assert(NTA == NSU, "wg_scan's workgroup");
 
 // maps: the positions and slots too (at most NTA sequences).
 __global__ __launch_bounds__(NTA) void k_cache_tables(TablesParams p, int maps) {
@@ -75,14 +64,14 @@ __global__ __launch_bounds__(NTA) void k_cache_tables(TablesParams p, int maps) 
     for (int base = 0; base < p.n; base += NTA) {
         const int i = base + tid, m = min(p.n - base, NTA);
         load(i);
-        const int give = max(held - target, 0), y = wg_scan(give, sum, red, all);
+        const int give = max(held - target, 0), y = wg_scan<NTA / 64>(give, sum, red, all);
         ends[tid] = y;
         at[tid] = target - (y - give);
         const int total = all;
-        wg_scan(max(target - held, 0), sum, red, all);
+        wg_scan<NTA / 64>(max(target - held, 0), sum, red, all);
         wanted += all;
         if (p.new_lens) {
-            const int e = tokens(token, wg_scan(i < p.n ? min(max(p.new_lens[i], 0), rows) : 0, tokens, red, all));
+            const int e = tokens(token, wg_scan<NTA / 64>(i < p.n ? min(max(p.new_lens[i], 0), rows) : 0, tokens, red, all));
             if (i < p.n) {
                 cu_ends[tid] = e;
                 p.cu[i + 1] = e;
@@ -109,7 +98,7 @@ __global__ __launch_bounds__(NTA) void k_cache_tables(TablesParams p, int maps) 
     for (int base = 0; base < p.n; base += NTA) {
         const int i = base + tid, m = min(p.n - base, NTA);
         if (p.n > NTA) load(i);
-        const int take = max(target - held, 0), y = wg_scan(take, sum, red, all);
+        const int take = max(target - held, 0), y = wg_scan<NTA / 64>(take, sum, red, all);
         ends[tid] = y;
         at[tid] = held - (y - take);
         if (i < p.n) p.held[i] = min(held, target) + min(max(got - taken - (y - take), 0), take);
@@ -166,13 +155,16 @@ __global__ __launch_bounds__(NT) void k_cache_maps(TablesParams p) {
 // written, where any token is kept, once.  In tiles of TT = 8 tokens, with S the state before the tile:
 //   X_t = S k_t,  Y_t = S (scale q_t)                       one product [K; Q] S^T of 16 rows, fp32 matrix instructions
 //   u_t = beta_t (v_t - gamma_t X_t - sum_{i<t} c_i (k_t . k_i)),   c_i = u_i decayed from i to t
-//   o_t = gamma_t Y_t + sum_{i<=t} c_i (q_t . k_i)          row by row of the state, one lane a row
+//   o_t = gamma_t Y_t + sum_{i<=t} c_i (q_t . k_i)          row by row of the state, a row in four lanes alike
 //   S'  = gamma_n S + sum_i c_i k_i^T                       c after the n-th token: the next tile's state, or the kept one
 // Decays multiply as the tokens pass, so that a gate of 0 (log-decay -inf) is one; nothing is divided.
-// A wave holds 16 RT state rows in registers as accumulators of S^T tiles: lane 16 lg + j has row j's channels 16 b + 4 lg .. + 3,
+// A wave holds 16 state rows in registers as accumulators of S^T tiles: lane 16 lg + j has row j's channels 16 b + 4 lg .. + 3,
 // which is the layout of a product's operand and result alike, so S enters and leaves them without a move.
-// Bound by memory (the state once in, and once out where tokens are kept).
-constexpr int TT = 8;
+// Bound by memory (the state once in, and once out where tokens are kept): 64 sequences, 16 heads of 128, 5 tokens of which 0 to 5
+// are kept, 28.9 us (4.5 TB/s; a copy reaches 5.1); the kept ones of 128 sequences' 1 to 9 tokens alone 46.0 us (4.4 TB/s).  What
+// the tokens make among themselves (their products, norms, gates) is done while the state is on its way: asked for ahead of
+// the tokens it took 33.7 and 55.4 us.  32 rows a wave: 30.6 and 47.6 us.  One sequence, 4.9 us: latency.
+constexpr int TT = 8, DROWS = 64;   // tokens of a tile; state rows of a workgroup
 struct DraftParams {
     const void* q;            // or null: no outputs
     const void* k;
@@ -202,46 +194,64 @@ __device__ __forceinline__ void seq_span(const StepSeqs& q, int s, int& beg, int
     end = min(max(tab(q.cu, s + 1), beg), q.T);
 }
 
-template <typename IO, int DK, int RT, int NW>
-__global__ __launch_bounds__(64 * NW) void k_draft_step(DraftParams p) {
-    constexpr int NB = DK / 16, ROWS = 16 * RT * NW, N = 64 * NW, PITCH = DK + 4;
+// 4 neighbouring values (aligned as one is) in floats
+__device__ __forceinline__ floatx4 four(const float* p) {
+    typedef floatx4 any __attribute__((aligned(4)));
+    return *reinterpret_cast<const any*>(p);
+}
+__device__ __forceinline__ floatx4 four(const bf16_t* p) {
+    typedef short4v any __attribute__((aligned(2)));
+    const short4v y = *reinterpret_cast<const any*>(p);
+    return floatx4{bf(y[0]), bf(y[1]), bf(y[2]), bf(y[3])};
+}
+
+template <typename IO, int DK>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void k_draft_step(DraftParams p) {
+    constexpr int NB = DK / 16, NW = NT / 64, PITCH = DK + 4;
     __shared__ __align__(16) float kq[2 * TT][PITCH];       // keys, then queries, of the tile
-    __shared__ __align__(16) float pair[NW][2 * TT][TT];    // a wave's share of k_t . k_i and q_t . k_i
-    __shared__ __align__(16) float xs[NW][2 * TT][16 * RT]; // X and Y by state row, then the c of both updates
+    __shared__ __align__(16) float part[NW][2 * TT][TT];    // a wave's share of k_t . k_i and q_t . k_i
+    __shared__ __align__(16) float pair[2 * TT][TT];        // their sums
+    __shared__ float xs[NW][2 * TT][20];                    // X and Y by state row, then the c of both updates
     __shared__ float gate[2][TT];                           // alpha and beta
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, lg = lane >> 4;
-    const int per = p.DV / ROWS, u = (int)blockIdx.x, sh = u / per;   // sequence * H + head
-    const int s = sh / p.H, h = sh - s * p.H, r0 = (u - sh * per) * ROWS + 16 * RT * wave;
+    const int per = p.DV / DROWS, u = (int)blockIdx.x, sh = u / per;   // sequence * H + head
+    const int s = sh / p.H, h = sh - s * p.H, r0 = (u - sh * per) * DROWS + 16 * wave;
+    float* const rows = p.S + ((long)sh * p.DV + r0 + l16) * DK + 4 * lg;   // this lane's row
     int beg, end;
     seq_span(p.s, s, beg, end);
     const int kept = p.keep ? min(max(tab(p.keep, s), 0), end - beg) : end - beg, todo = p.q ? end - beg : kept;
     if (todo == 0) return;
-    float* const rows = p.S + ((long)sh * p.DV + r0 + l16) * DK + 4 * lg;   // of tile 0: this lane's row
-    floatx4 S[RT][NB];
-#pragma unroll
-    for (int t = 0; t < RT; ++t)
-#pragma unroll
-        for (int b = 0; b < NB; ++b) S[t][b] = f4(rows + (long)16 * t * DK + 16 * b);
-    const int row = r0 + lane % (16 * RT);   // the row that this lane works out
+    const int row = r0 + l16;
     const long hk = h / p.G;
-    for (int t0 = 0; t0 < todo; t0 += TT) {
+    floatx4 S[NB];
+    auto tile = [&](int t0, auto FIRST) {
         const int m = min(todo - t0, TT);
         const long tok = beg + t0;
-        float v[TT];
+        // Everything of the tokens is asked for ahead of the state, so that what they make among themselves is done by the time
+        // it arrives (loads come back in order).
+        constexpr int LPR = DK / 4, NK = 2 * TT * LPR / NT;   // 4 channels a thread, LPR neighbouring threads a row
+        static_assert(2 * TT * LPR % NT == 0, "every thread has its share");
+        floatx4 in[NK];
+#pragma unroll
+        for (int i = 0; i < NK; ++i) {
+            const int r = (tid + NT * i) / LPR, t = r % TT;
+            in[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+            if (t < m && (r < TT || p.q)) in[i] = four((const IO*)(r < TT ? p.k : p.q) + ((tok + t) * p.HK + hk) * DK + 4 * (tid % LPR));
+        }
+        float gt = 0.f, v[TT];
+        if (tid < 2 * TT && tid % TT < m) gt = (tid < TT ? p.g : p.beta)[(tok + tid % TT) * p.H + h];
 #pragma unroll
         for (int t = 0; t < TT; ++t) v[t] = t < m ? to_f(((const IO*)p.v)[((tok + t) * p.H + h) * p.DV + row]) : 0.f;
-        __syncthreads();   // (the tile before no longer reads these)
-        // keys and queries, 4 channels a thread, DK / 4 neighbouring threads a row
-        constexpr int LPR = DK / 4;
+        if constexpr (decltype(FIRST)::value) {
 #pragma unroll
-        for (int i = tid; i < 2 * TT * LPR; i += N) {
-            const int r = i / LPR, c = 4 * (i % LPR), t = r % TT;
-            floatx4 x = {0.f, 0.f, 0.f, 0.f};
-            if (t < m && (r < TT || p.q)) {
-                const IO* src = (const IO*)(r < TT ? p.k : p.q) + ((tok + t) * p.HK + hk) * DK + c;
+            for (int b = 0; b < NB; ++b) S[b] = f4(rows + 16 * b);
+        } else {
+            __syncthreads();   // (the tile before no longer reads the shared arrays)
+        }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = to_f(src[e]);
-            }
+        for (int i = 0; i < NK; ++i) {
+            const int r = (tid + NT * i) / LPR;
+            floatx4 x = in[i];
             if (p.pre & PRE_L2) {
                 float ss = x[0] * x[0] + x[1] * x[1] + x[2] * x[2] + x[3] * x[3];
 #pragma unroll
@@ -249,70 +259,63 @@ __global__ __launch_bounds__(64 * NW) void k_draft_step(DraftParams p) {
                 x *= 1.f / sqrtf(ss + L2_EPS);
             }
             if (r >= TT) x *= p.scale;
-            *reinterpret_cast<floatx4*>(&kq[r][c]) = x;
+            *reinterpret_cast<floatx4*>(&kq[r][4 * (tid % LPR)]) = x;
         }
-        if (tid < 2 * TT) {
-            const int t = tid % TT;
-            const long at = (tok + t) * p.H + h;
-            if (tid < TT)
-                gate[0][t] = t < m ? expf((p.pre & PRE_GATES) ? gate_g(p.g[at]) : p.g[at]) : 1.f;
-            else
-                gate[1][t] = t < m ? ((p.pre & PRE_GATES) ? gate_beta(p.beta[at]) : p.beta[at]) : 0.f;
-        }
-        __syncthreads();
-        floatx4 x[RT], own = {0.f, 0.f, 0.f, 0.f};
+        if (tid < TT) gate[0][tid] = tid < m ? expf((p.pre & PRE_GATES) ? gate_g(gt) : gt) : 1.f;
+        else if (tid < 2 * TT) gate[1][tid - TT] = tid - TT < m ? ((p.pre & PRE_GATES) ? gate_beta(gt) : gt) : 0.f;
+        lds_barrier();
+        floatx4 own = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int t = 0; t < RT; ++t) x[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int b = 0; b < NB; ++b)
+            if (b % NW == wave) {   // (column i of the product with the keys and queries themselves: row i)
+                const floatx4 a = f4(&kq[l16][16 * b + 4 * lg]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) own = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], a[e], own, 0, 0, 0);
+            }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (l16 < TT) part[wave][4 * lg + e][l16] = own[e];
+        lds_barrier();
+        for (int i = tid; i < 2 * TT * TT; i += NT) {
+            float y = 0.f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) y += part[w][i / TT][i % TT];
+            pair[i / TT][i % TT] = y;
+        }
+        floatx4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
             const floatx4 a = f4(&kq[l16][16 * b + 4 * lg]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int t = 0; t < RT; ++t) x[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], S[t][b][e], x[t], 0, 0, 0);
-            if (b % NW == wave)   // (column i of the product with the keys and queries themselves: row i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) own = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], a[e], own, 0, 0, 0);
+            for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], S[b][e], x, 0, 0, 0);
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (l16 < TT) pair[wave][4 * lg + e][l16] = own[e];
-#pragma unroll
-            for (int t = 0; t < RT; ++t) xs[wave][4 * lg + e][16 * t + l16] = x[t][e];
-        }
-        __syncthreads();
+        for (int e = 0; e < 4; ++e) xs[wave][4 * lg + e][l16] = x[e];
+        lds_barrier();
         // the tile's tokens, row by row
         float c[TT], ck[TT], gamma = 1.f, gamma_k = 1.f;
         const int kt = min(max(kept - t0, 0), TT);   // kept ones of the tile
-        const int lr = lane % (16 * RT);
 #pragma unroll
-        for (int t = 0; t < TT; ++t) ck[t] = 0.f;
+        for (int t = 0; t < TT; ++t) c[t] = ck[t] = 0.f;
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
+            if (t >= m) break;
             const float al = gate[0][t];
-            float kk[TT], qk[TT];
-#pragma unroll
-            for (int i = 0; i <= t; ++i) {
-                kk[i] = qk[i] = 0.f;
-#pragma unroll
-                for (int w = 0; w < NW; ++w) {
-                    kk[i] += pair[w][t][i];
-                    qk[i] += pair[w][TT + t][i];
-                }
-            }
+            const floatx4 k0 = f4(&pair[t][0]), k1 = f4(&pair[t][4]);
             gamma *= al;
-            float sk = gamma * xs[wave][t][lr];
+            float sk = gamma * xs[wave][t][l16];
 #pragma unroll
             for (int i = 0; i < t; ++i) {
                 c[i] *= al;
-                sk += c[i] * kk[i];
+                sk += c[i] * (i < 4 ? k0[i] : k1[i - 4]);
             }
             c[t] = gate[1][t] * (v[t] - sk);
-            if (t < m && p.q) {
-                float o = gamma * xs[wave][TT + t][lr];
+            if (p.q) {
+                const floatx4 q0 = f4(&pair[TT + t][0]), q1 = f4(&pair[TT + t][4]);
+                float o = gamma * xs[wave][TT + t][l16];
 #pragma unroll
-                for (int i = 0; i <= t; ++i) o += c[i] * qk[i];
-                if (lane < 16 * RT) ((IO*)p.o)[((tok + t) * p.H + h) * p.DV + row] = from_f<IO>(o);
+                for (int i = 0; i <= t; ++i) o += c[i] * (i < 4 ? q0[i] : q1[i - 4]);
+                if (lane < 16) ((IO*)p.o)[((tok + t) * p.H + h) * p.DV + row] = from_f<IO>(o);
             }
             if (t + 1 == kt) {
                 gamma_k = gamma;
@@ -321,10 +324,10 @@ __global__ __launch_bounds__(64 * NW) void k_draft_step(DraftParams p) {
             }
         }
         const bool more = t0 + TT < todo, store = kt > 0 && t0 + kt == kept;
-        if (!more && !store) continue;
+        if (!more && !store) return;
         // S' = gamma S + sum_i c_i k_i^T: first the kept state, then the next tile's
         __builtin_amdgcn_wave_barrier();
-        if (lane < 16 * RT)
+        if (lane < 16)
 #pragma unroll
             for (int t = 0; t < TT; ++t) {
                 xs[wave][t][lane] = ck[t];
@@ -332,24 +335,25 @@ __global__ __launch_bounds__(64 * NW) void k_draft_step(DraftParams p) {
             }
         __builtin_amdgcn_wave_barrier();
         auto update = [&](int first, float decay, int count, auto put) {
+            float w[TT / 4];
+#pragma unroll
+            for (int z = 0; z < TT / 4; ++z) w[z] = xs[wave][first + 4 * z + lg][l16];
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 float a[TT / 4];
 #pragma unroll
                 for (int z = 0; z < TT / 4; ++z) a[z] = 4 * z + lg < count ? kq[4 * z + lg][16 * b + l16] : 0.f;
+                floatx4 y = S[b] * decay;
 #pragma unroll
-                for (int t = 0; t < RT; ++t) {
-                    floatx4 y = S[t][b] * decay;
-#pragma unroll
-                    for (int z = 0; z < TT / 4; ++z)
-                        y = __builtin_amdgcn_mfma_f32_16x16x4f32(a[z], xs[wave][first + 4 * z + lg][16 * t + l16], y, 0, 0, 0);
-                    put(t, b, y);
-                }
+                for (int z = 0; z < TT / 4; ++z) y = __builtin_amdgcn_mfma_f32_16x16x4f32(a[z], w[z], y, 0, 0, 0);
+                put(b, y);
             }
         };
-        if (store) update(0, gamma_k, kt, [&](int t, int b, floatx4 y) { *reinterpret_cast<floatx4*>(rows + (long)16 * t * DK + 16 * b) = y; });
-        if (more) update(TT, gamma, TT, [&](int t, int b, floatx4 y) { S[t][b] = y; });
-    }
+        if (store) update(0, gamma_k, kt, [&](int b, floatx4 y) { *reinterpret_cast<floatx4*>(rows + 16 * b) = y; });
+        if (more) update(TT, gamma, TT, [&](int b, floatx4 y) { S[b] = y; });
+    };
+    tile(0, Ic<1>{});
+    for (int t0 = TT; t0 < todo; t0 += TT) tile(t0, Ic<0>{});
 }
 
 // ------------------------------------------------------------------ verification of drafts
@@ -358,8 +362,8 @@ __global__ __launch_bounds__(64 * NW) void k_draft_step(DraftParams p) {
 // draft from w = p of the row after it: the lowest v with w_0 + .. + w_v > u W, sums in 64 bits, so that no rounding of
 // theirs is seen but where u W falls within 2^-50 of a border.  w = p, too, where no w is positive.  Entries that are not
 // positive and finite count as 0.
-// k_verify_sums: a workgroup per slice of VS tokens of the row that is left, its sums of w and of p; k_verify_pick: the slice
-// that holds u W, then the token in it.  Bound by the two rows' bytes.
+// k_verify_sums: waves over slices of VS tokens of the row that is left, a sum of w each; k_verify_pick: the slice that holds
+// u W, then the token in it.  Bound by the two rows' bytes.
 struct VerifyParams {
     const void* p;            // [n][m + 1][..], ps elements a row
     const void* q;            // [n][m][..], qs elements a row, or null: 1 for the drafted token
@@ -368,13 +372,13 @@ struct VerifyParams {
     const float* u;           // [n][m + 1]
     int32_t* tokens;          // [n][m + 1]
     int32_t* counts;          // [n]
-    double2* part;            // [n][slices] sums of w and of p
+    double* part;             // [n][slices] sums of w
     long ps, qs;
-    int m, V, slices;
+    int m, V, slices, groups;   // groups: workgroups of k_verify_sums a sequence
 };
-constexpr int VS = 4096;
+constexpr int VS = 1024;
 
-__device__ __forceinline__ float probability(float x) { return x > 0.f && x <= -LOWEST ? x : 0.f; }
+__device__ __forceinline__ float probability(float x) { return __builtin_amdgcn_classf(x, 0x180) ? x : 0.f; }   // (positive, finite)
 
 // The number of accepted drafts of sequence s, and of its drafts, by a whole wave.
 template <typename IO> __device__ __forceinline__ int accepted(const VerifyParams& p, int s, int& len) {
@@ -398,16 +402,11 @@ template <typename IO> __device__ __forceinline__ int accepted(const VerifyParam
     return len;
 }
 
-// w of a row's entries: of row a of the target, less row a of the drafts' where `less`.
+// w of a row's entries: of row a of the target, less row a of the drafts'.
 template <typename IO> struct Rest {
     const IO* p;
-    const IO* q;
-    int certain;   // the token whose draft was certain (q null), or -1
-    __device__ __forceinline__ double w(int v, double pr) const {
-        const double qr = q ? probability(to_f(q[v])) : v == certain ? 1. : 0.;
-        return pr > qr ? pr - qr : 0.;
-    }
-    __device__ __forceinline__ double target(int v) const { return probability(to_f(p[v])); }
+    const IO* q;   // null: nothing, but for
+    int certain;   // the token whose draft was certain, or -1
 };
 template <typename IO> __device__ __forceinline__ Rest<IO> rest_of(const VerifyParams& p, int s, int a, int len) {
     Rest<IO> r;
@@ -417,112 +416,159 @@ template <typename IO> __device__ __forceinline__ Rest<IO> rest_of(const VerifyP
     return r;
 }
 
-__device__ __forceinline__ double wave_sum(double x) {
+// w of tokens v0 + STEP i + e, i < N, e < 4 (0 from `end` on), all loads sent off before the first is used.
+template <typename IO, int N, int STEP> __device__ __forceinline__ void rest(const Rest<IO>& r, int v0, int end, double (&w)[N][4]) {
+    auto load = [&](const IO* src, floatx4 (&x)[N]) {
 #pragma unroll
-    for (int off = 1; off < 64; off <<= 1) x += __shfl_xor(x, off, 64);
+        for (int i = 0; i < N; ++i) {
+            const int v = v0 + STEP * i;
+            x[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+            if (v + 4 <= end) {
+                x[i] = four(src + v);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (v + e < end) x[i][e] = to_f(src[v + e]);
+            }
+        }
+    };
+    floatx4 x[N], y[N];
+    load(r.p, x);
+    if (r.q) {
+        load(r.q, y);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[i][e] = fmax((double)probability(x[i][e]) - (double)probability(y[i][e]), 0.);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[i][e] = probability(x[i][e]);
+    if (__builtin_amdgcn_ballot_w64(r.certain >= v0 && r.certain < v0 + STEP * (N - 1) + 4))
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (v0 + STEP * i + e == r.certain) w[i][e] = fmax(w[i][e] - 1., 0.);
+}
+
+constexpr int VE = VS / 64 / 4;   // groups of 4 tokens of a lane
+
+// Inclusive sums over the wave's lanes, as wave_scan takes them: always in the same order.
+template <int CTRL, int ROWS> __device__ __forceinline__ double dpp64(double x) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, ROWS, 0xf, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, ROWS, 0xf, false);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double scan64(double x) {
+    x += dpp64<0x111, 0xf>(x);
+    x += dpp64<0x112, 0xf>(x);
+    x += dpp64<0x114, 0xf>(x);
+    x += dpp64<0x118, 0xf>(x);
+    x += dpp64<0x142, 0xa>(x);
+    x += dpp64<0x143, 0xc>(x);
     return x;
+}
+__device__ __forceinline__ double lane64(double x, int l) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)u, l), hi = __builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), l);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
+// The sum of w over a slice, by a wave, in every lane.
+template <typename IO> __device__ __forceinline__ double slice_sum(const Rest<IO>& r, int slice, int V) {
+    const int lane = threadIdx.x & 63, first = slice * VS;
+    double w[VE][4], sum = 0.;
+    rest<IO, VE, 256>(r, first + 4 * lane, min(first + VS, V), w);
+#pragma unroll
+    for (int i = 0; i < VE; ++i) sum += (w[i][0] + w[i][1]) + (w[i][2] + w[i][3]);
+    return lane64(scan64(sum), 63);
 }
 
 template <typename IO>
 __global__ __launch_bounds__(NT) void k_verify_sums(VerifyParams p) {
-    __shared__ double2 red[NT / 64];
-    const int s = (int)blockIdx.x / p.slices, slice = (int)blockIdx.x - s * p.slices, tid = threadIdx.x;
+    const int s = (int)blockIdx.x / p.groups, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int w = ((int)blockIdx.x - s * p.groups) * (NT / 64) + wave;
     int len;
     const int a = accepted<IO>(p, s, len);
     const Rest<IO> r = rest_of<IO>(p, s, a, len);
-    double sw = 0., sp = 0.;
-    const int first = slice * VS, end = min(first + VS, p.V);
-    for (int v = first + tid; v < end; v += NT) {
-        const double pr = r.target(v);
-        sp += pr;
-        sw += r.w(v, pr);
+    for (int i = w; i < p.slices; i += p.groups * (NT / 64)) {
+        const double sum = slice_sum(r, i, p.V);
+        if ((threadIdx.x & 63) == 0) p.part[(long)s * p.slices + i] = sum;
     }
-    sw = wave_sum(sw);
-    sp = wave_sum(sp);
-    if ((tid & 63) == 0) red[tid >> 6] = double2{sw, sp};
-    __syncthreads();
-    if (tid != 0) return;
-    double2 y = red[0];
-#pragma unroll
-    for (int w = 1; w < NT / 64; ++w) {
-        y.x += red[w].x;
-        y.y += red[w].y;
-    }
-    p.part[blockIdx.x] = y;
+    if (w == 0 && threadIdx.x == 0) p.counts[s] = a + 1;
 }
 
 template <typename IO>
 __global__ __launch_bounds__(NT) void k_verify_pick(VerifyParams p) {
-    __shared__ double before[NT / 64];
-    __shared__ int found, last;
-    const int s = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    int len;
-    const int a = accepted<IO>(p, s, len);
-    const Rest<IO> r = rest_of<IO>(p, s, a, len);
-    const double2* part = p.part + (long)s * p.slices;
-    double W = 0., P = 0.;   // (every thread the same sums, in order)
-    for (int i = 0; i < p.slices; ++i) {
-        W += part[i].x;
-        P += part[i].y;
+    const int s = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    double* part = p.part + (long)s * p.slices;
+    const int per = (p.slices + 63) / 64;   // slices of a lane
+    double sum, inc;
+    auto load = [&] {
+        sum = 0.;
+        for (int i = lane * per; i < min((lane + 1) * per, p.slices); ++i) sum += part[i];
+        inc = scan64(sum);
+    };
+    load();
+    const int a = tab(p.counts, s) - 1, len = p.lens ? min(max(tab(p.lens, s), 0), p.m) : p.m;
+    const float u = p.u[(long)s * (p.m + 1) + p.m];
+    Rest<IO> r = rest_of<IO>(p, s, a, len);
+    if (!(lane64(inc, 63) > 0.)) {   // no w is positive: p itself
+        r.q = nullptr;
+        r.certain = -1;
+        __syncthreads();   // (every wave has read the sums)
+        for (int i = wave; i < p.slices; i += NT / 64) {
+            const double x = slice_sum(r, i, p.V);
+            if (lane == 0) part[i] = x;
+        }
+        __syncthreads();
+        load();
     }
-    const bool plain = !(W > 0.);
-    const double all = plain ? P : W;
-    const float draw = p.u[(long)s * (p.m + 1) + p.m];
-    const double goal = (draw > 0.f ? (double)draw : 0.) * all;   // (NaN: 0)
-    // the first slice whose running sum passes the goal; else the last one that holds anything
-    int slice = -1;
-    double run = 0., ahead = 0.;
-    for (int i = 0; i < p.slices; ++i) {
-        const double x = plain ? part[i].y : part[i].x;
-        if (!(x > 0.)) continue;
-        slice = i;
-        ahead = run;
-        run += x;
-        if (run > goal) break;
-    }
-    if (tid == 0) {
-        found = 1 << 30;
-        last = -1;
-    }
-    __syncthreads();
+    if (wave != 0) return;
+    const double goal = (u > 0.f ? (double)u : 0.) * lane64(inc, 63);   // (NaN: 0)
+    // the first lane, slice and token whose running sum passes the goal; each time else the last that holds anything
     int token = -1;
-    if (slice >= 0) {
-        constexpr int EACH = VS / NT;
-        const int v0 = slice * VS + tid * EACH;
-        double w[EACH], sum = 0.;
-        int mine = -1;
+    uint64_t any = __builtin_amdgcn_ballot_w64(sum > 0.), past = __builtin_amdgcn_ballot_w64(sum > 0. && inc > goal);
+    if (any) {
+        int l = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(any);
+        double run = lane64(inc - sum, l), ahead = run;
+        int slice = 0;
+        for (int i = l * per; i < min((l + 1) * per, p.slices); ++i) {
+            const double x = part[i];
+            if (!(x > 0.)) continue;
+            slice = i;
+            ahead = run;
+            run += x;
+            if (run > goal) break;
+        }
+        slice = __builtin_amdgcn_readfirstlane(slice);
+        const int first = slice * VS, v0 = first + 4 * VE * lane;
+        double w[VE][4];
+        rest<IO, VE, 4>(r, v0, min(first + VS, p.V), w);
+        sum = 0.;
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) {
-            w[e] = 0.;
-            if (v0 + e < p.V) {
-                const double pr = r.target(v0 + e);
-                w[e] = plain ? pr : r.w(v0 + e, pr);
+        for (int i = 0; i < VE; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum += w[i][e];
+        double c = ahead + (scan64(sum) - sum);
+        int hit = -1, mine = -1;
+#pragma unroll
+        for (int i = 0; i < VE; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                c += w[i][e];
+                if (w[i][e] > 0.) {
+                    mine = v0 + 4 * i + e;
+                    if (hit < 0 && c > goal) hit = mine;
+                }
             }
-            sum += w[e];
-            if (w[e] > 0.) mine = v0 + e;
-        }
-        double inc = sum;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const double y = __shfl_up(inc, off, 64);
-            if (lane >= off) inc += y;
-        }
-        if (lane == 63) before[wave] = inc;
-        __syncthreads();
-        double c = ahead;
-        for (int z = 0; z < wave; ++z) c += before[z];
-        c += inc - sum;
-        int hit = -1;
-#pragma unroll
-        for (int e = 0; e < EACH; ++e) {
-            c += w[e];
-            if (hit < 0 && w[e] > 0. && c > goal) hit = v0 + e;
-        }
-        if (hit >= 0) atomicMin(&found, hit);
-        if (mine >= 0) atomicMax(&last, mine);
-        __syncthreads();
-        token = found < 1 << 30 ? found : last;
+        any = __builtin_amdgcn_ballot_w64(mine >= 0);
+        past = __builtin_amdgcn_ballot_w64(hit >= 0);
+        token = past ? __builtin_amdgcn_readlane(hit, __builtin_ctzll(past)) : any ? __builtin_amdgcn_readlane(mine, 63 - __builtin_clzll(any)) : -1;
     }
-    for (int j = tid; j <= p.m; j += NT) p.tokens[(long)s * (p.m + 1) + j] = j < a ? p.drafts[(long)s * p.m + j] : j == a ? token : -1;
-    if (tid == 0) p.counts[s] = a + 1;
+    for (int j = lane; j <= p.m; j += 64) p.tokens[(long)s * (p.m + 1) + j] = j < a ? p.drafts[(long)s * p.m + j] : j == a ? token : -1;
 }

@@ -3244,11 +3244,11 @@ void launch_paged(const PagedParams& p, const PagedPlan& plan, hipStream_t st) {
     const dim3 grid((unsigned)(plan.items * p.HKV));
     const long blocks = plan.blocks * p.HKV;
     if (plan.rb == AQ) {
-        hipLaunchKernelGGL((k_attn_tile<DH, CT, PagedParams>), grid, dim3(NT), 0, st, p);
+        hipLaunchKernelGGL((k_attn_tile<DH, CT>), grid, dim3(NT), 0, st, p);
         if (p.spare > 0) hipLaunchKernelGGL((k_attn_join_tile<DH>), dim3((unsigned)blocks, (unsigned)(plan.rows + 15) / 16), dim3(NT), 0, st, p);
         return;
     }
-    hipLaunchKernelGGL((k_attn_rows<DH, CT, PagedParams>), grid, dim3(NT), 0, st, p);
+    hipLaunchKernelGGL((k_attn_rows<DH, CT>), grid, dim3(NT), 0, st, p);
     if (p.spare > 0) hipLaunchKernelGGL((k_attn_join<DH>), dim3((unsigned)blocks, (unsigned)plan.rows), dim3(NT), 0, st, p);
 }
 
@@ -3257,6 +3257,7 @@ void launch_paged(const PagedParams& p, const PagedPlan& plan, hipStream_t st) {
 struct SharedPlan {
     int rbp, rbt, round;
     long blocks_t, items_p, items_t;
+    int rows_t;                  // rows that a block of the sequences' own keys can hold
 };
 SharedPlan shared_plan(int B, int T, int H, int H_kv, int page, int max_pages, int n_seqs, int groups) {
     SharedPlan p;
@@ -3267,6 +3268,7 @@ SharedPlan shared_plan(int B, int T, int H, int H_kv, int page, int max_pages, i
     p.rbt = rows <= 64 * n ? 16 : AQ;
     const long blocks_p = rows / p.rbp + std::min<long>(groups, tokens);
     p.blocks_t = n_seqs > 0 ? rows / p.rbt + std::min<long>(n, tokens) : B * ((T * G + p.rbt - 1) / p.rbt);
+    p.rows_t = (int)std::min<long>(T * G, p.rbt);
     p.items_p = std::min(blocks_p + p.round, blocks_p * units);
     p.items_t = std::min(p.blocks_t + p.round, p.blocks_t * units);
     return p;
@@ -3287,7 +3289,7 @@ SharedLayout shared_layout(const SharedPlan& p, long n, int groups, int H_kv, in
     l.first_p = take((groups + 1L) * 4);
     l.first_t = take((n + 1) * 4);
     l.block_t = take((n + 1) * 4);
-    l.chunk = take(8);
+    l.chunk = take(4);
     l.ml_p = take(rows_p * sizeof(float2));
     l.ml_t = take(rows_t * sizeof(float2));
     l.o_p = take(rows_p * d * 4);
@@ -3298,31 +3300,23 @@ SharedLayout shared_layout(const SharedPlan& p, long n, int groups, int H_kv, in
 
 template <int DH, typename CT>
 void launch_shared(const SharedSetup& setup, const SharedJoin& j, const SharedPlan& plan, hipStream_t st) {
-    hipLaunchKernelGGL(k_shared_setup, dim3(1), dim3(NSU), 0, st, setup);
-    auto attend = [&](const SharedParams& p, int rb, long items) {
-        const dim3 grid((unsigned)(items * p.HKV));
-        if (rb == AQ) hipLaunchKernelGGL((k_attn_tile<DH, CT, SharedParams>), grid, dim3(NT), 0, st, p);
-        else hipLaunchKernelGGL((k_attn_rows<DH, CT, SharedParams>), grid, dim3(NT), 0, st, p);
-    };
-    attend(j.g, plan.rbp, plan.items_p);
-    attend(j.t, plan.rbt, plan.items_t);
-    hipLaunchKernelGGL((k_shared_join<DH>), dim3((unsigned)(plan.blocks_t * j.t.HKV), (unsigned)plan.rbt), dim3(NT), 0, st, j);
+    hipLaunchKernelGGL(k_shared_setup, dim3(1), dim3(NT), 0, st, setup);
+    const int prefix_wgs = (int)(plan.items_p * j.t.HKV);
+    const dim3 grid((unsigned)(prefix_wgs + plan.items_t * j.t.HKV));
+    if (plan.rbp == 16) hipLaunchKernelGGL((k_attn_shared<DH, CT, 0>), grid, dim3(NT), 0, st, j.g, j.t, prefix_wgs);
+    else if (plan.rbt == 16) hipLaunchKernelGGL((k_attn_shared<DH, CT, 1>), grid, dim3(NT), 0, st, j.g, j.t, prefix_wgs);
+    else hipLaunchKernelGGL((k_attn_shared<DH, CT, 2>), grid, dim3(NT), 0, st, j.g, j.t, prefix_wgs);
+    hipLaunchKernelGGL((k_shared_join<DH>), dim3((unsigned)(plan.blocks_t * j.t.HKV), (unsigned)plan.rows_t), dim3(NT), 0, st, j);
 }
 
 template <typename IO, int DK>
 void launch_draft(const DraftParams& p, int n, hipStream_t st) {
-    const long heads = (long)n * p.H;
-    if (heads * p.DV < 512 * 64)
-        hipLaunchKernelGGL((k_draft_step<IO, DK, 1, 4>), dim3((unsigned)(heads * (p.DV / 64))), dim3(256), 0, st, p);
-    else if (p.DV == 128)
-        hipLaunchKernelGGL((k_draft_step<IO, DK, 4, 2>), dim3((unsigned)heads), dim3(128), 0, st, p);
-    else
-        hipLaunchKernelGGL((k_draft_step<IO, DK, 4, 1>), dim3((unsigned)heads), dim3(64), 0, st, p);
+    hipLaunchKernelGGL((k_draft_step<IO, DK>), dim3((unsigned)((long)n * p.H * (p.DV / DROWS))), dim3(NT), 0, st, p);
 }
 
 template <typename IO>
 void launch_verify(const VerifyParams& p, int n, hipStream_t st) {
-    hipLaunchKernelGGL((k_verify_sums<IO>), dim3((unsigned)((long)n * p.slices)), dim3(NT), 0, st, p);
+    hipLaunchKernelGGL((k_verify_sums<IO>), dim3((unsigned)((long)n * p.groups)), dim3(NT), 0, st, p);
     hipLaunchKernelGGL((k_verify_pick<IO>), dim3((unsigned)n), dim3(NT), 0, st, p);
 }
 
@@ -4163,7 +4157,7 @@ extern "C" gdn_status gdn_attention_shared(const void* q, const void* k_cache, c
     if (!workspace || workspace_bytes < lay.total)
         return fail(GDN_ERR_WORKSPACE, "workspace of %zu bytes given, %zu needed", workspace ? workspace_bytes : (size_t)0, lay.total);
     if (!aligned(workspace, 256)) return fail(GDN_ERR_INVALID_ARG, "workspace is not 256-byte aligned");
-    if (!grid_fits(plan.items_p * H_kv) || !grid_fits(plan.items_t * H_kv) || !grid_fits(plan.blocks_t * H_kv * plan.rbt))
+    if (!grid_fits((plan.items_p + plan.items_t) * H_kv) || !grid_fits(plan.blocks_t * H_kv * plan.rbt))
         return fail(GDN_ERR_UNSUPPORTED, "B*T*H too large");
     char* const ws = static_cast<char*>(workspace);
     auto words = [&](size_t at) { return reinterpret_cast<int32_t*>(ws + at); };
@@ -4171,9 +4165,8 @@ extern "C" gdn_status gdn_attention_shared(const void* q, const void* k_cache, c
     u.s.cu = cu_seqlens; u.s.lens = seq_lens; u.s.n = n; u.s.T = T;
     u.prefix = prefix_lens; u.cu_groups = cu_groups; u.groups = n_groups;
     u.G = H / H_kv;
-    u.rbp = plan.rbp; u.rbt = plan.rbt; u.round_p = u.round_t = plan.round;
-    u.least_p = plan.rbp == 16 ? 1 : 4;   // (a tile's chunk of fewer keys is mostly joining)
-    u.least_t = plan.rbt == 16 ? 1 : 4;
+    u.rbp = plan.rbp; u.rbt = plan.rbt; u.round = plan.round;
+    u.least = plan.rbp == 16 ? 1 : 2;   // (a tile's chunk of fewer keys is mostly joining)
     u.grp = reinterpret_cast<int4*>(ws + lay.grp); u.seq = reinterpret_cast<int4*>(ws + lay.seq);
     u.group_of = words(lay.group_of); u.first_p = words(lay.first_p); u.first_t = words(lay.first_t);
     u.block_t = words(lay.block_t); u.chunk = words(lay.chunk);
@@ -4187,7 +4180,7 @@ extern "C" gdn_status gdn_attention_shared(const void* q, const void* k_cache, c
     j.t.c = make_cache(k_cache, v_cache, k_scale, v_scale, block_table, page, n_pages, max_pages);
     u.shift = j.t.c.shift; u.cap = max_pages << j.t.c.shift;
     j.g = j.t;
-    j.t.part = u.seq; j.t.first = u.first_t; j.t.chunk = u.chunk + 1; j.t.parts = n; j.t.prefix = false;
+    j.t.part = u.seq; j.t.first = u.first_t; j.t.chunk = u.chunk; j.t.parts = n; j.t.prefix = false;
     j.g.part = u.grp; j.g.first = u.first_p; j.g.chunk = u.chunk; j.g.parts = n_groups; j.g.prefix = true;
     j.t.pml = reinterpret_cast<float2*>(ws + lay.ml_t); j.t.po = reinterpret_cast<float*>(ws + lay.o_t);
     j.g.pml = reinterpret_cast<float2*>(ws + lay.ml_p); j.g.po = reinterpret_cast<float*>(ws + lay.o_p);
@@ -4255,7 +4248,7 @@ static bool vocabulary_fits(int n, int m, int V) {
 
 extern "C" size_t gdn_draft_verify_workspace_bytes(int n, int m, int V) {
     if (!vocabulary_fits(n, m, V)) return 0;
-    return round_up((size_t)n * ((V + VS - 1) / VS) * sizeof(double2), 256);
+    return round_up((size_t)n * ((V + VS - 1) / VS) * sizeof(double), 256);
 }
 
 extern "C" gdn_status gdn_draft_verify(const void* p, const void* q, const int32_t* drafts, const int32_t* draft_lens, const float* u,
@@ -4280,9 +4273,11 @@ extern "C" gdn_status gdn_draft_verify(const void* p, const void* q, const int32
     if (!aligned(workspace, 256)) return fail(GDN_ERR_INVALID_ARG, "workspace is not 256-byte aligned");
     VerifyParams a = {};
     a.p = p; a.q = q; a.drafts = drafts; a.lens = draft_lens; a.u = u; a.tokens = tokens; a.counts = counts;
-    a.part = static_cast<double2*>(workspace);
+    a.part = static_cast<double*>(workspace);
     a.ps = (long)p_stride; a.qs = (long)q_stride;
     a.m = m; a.V = V; a.slices = (V + VS - 1) / VS;
+    const long per = ((long)n * a.slices + 24 * PLAN_CUS - 1) / (24 * PLAN_CUS);   // slices a wave, of 24 waves a CU
+    a.groups = (int)((a.slices + NT / 64 * per - 1) / (NT / 64 * per));
     hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
     (void)hipGetLastError();
     if (dtype == GDN_BF16) launch_verify<bf16_t>(a, n, hs);

@@ -860,16 +860,16 @@ __device__ __forceinline__ void plain_row(const PagedParams& p, const Item& it, 
     }
 }
 
-template <int DH, typename CT, typename P>
-__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_attn_rows(P p) {
+// wg: the workgroup's number among those of p; outs(z): LDS of RB * PITCH floats for the sums of wave z.
+template <int DH> constexpr int ROWS_PITCH = DH + 4;   // (rows 4 banks apart: 16 rows' 16-byte accesses meet no bank twice)
+template <int DH, typename CT, typename P, typename F>
+__device__ __forceinline__ void attn_rows(const P& p, int wg, F outs, float2 (&lds_ml)[NT / 64][16], int& redo) {
     constexpr int NW = NT / 64, RB = 16, CW = DH / 16, ESZ = sizeof(CT), NKB = DH / 32, NK = DH * ESZ / 64, VD = CW * ESZ / 4;
+    constexpr int PITCH = ROWS_PITCH<DH>;
     constexpr bool E4M3 = ESZ == 1;
-    __shared__ __align__(16) float lds_o[NW][RB][DH + 4];   // (rows 4 banks apart: 16 rows' 16-byte accesses meet no bank twice)
-    __shared__ float2 lds_ml[NW][RB];
-    __shared__ int redo;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, lg = lane >> 4;
-    const int w = div_by(blockIdx.x, p.by_hkv), hk = (int)blockIdx.x - w * p.HKV;
+    const int w = div_by(wg, p.by_hkv), hk = wg - w * p.HKV;
     Item it;
     if (!find_item<RB>(p, w, it) || it.chunk >= it.chunks) return;
     const int k0 = it.start + it.chunk * it.c, k1 = min(it.end - k0, it.c) + k0;   // the item's keys
@@ -1012,7 +1012,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
         for (int e = 0; e < 4; ++e)
 #pragma unroll
             for (int n = 0; n < CW; n += 4)
-                *reinterpret_cast<floatx4*>(&lds_o[wave][l16][CW * (4 * lg + e) + n]) = floatx4{acc[n][e], acc[n + 1][e], acc[n + 2][e], acc[n + 3][e]};
+                *reinterpret_cast<floatx4*>(&outs(wave)[l16 * PITCH + CW * (4 * lg + e) + n]) = floatx4{acc[n][e], acc[n + 1][e], acc[n + 2][e], acc[n + 3][e]};
     }
     if (k1 - 1 > last0) {
         // Some rows do not see some of the item's keys, but their weight of 0 does not hide a value that is not finite
@@ -1036,7 +1036,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
 #pragma unroll
                     for (int z = 0; z < NW; ++z)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) lds_o[z][r][8 * lane + e] = z == 0 ? o[e] : 0.f;
+                        for (int e = 0; e < 8; ++e) outs(z)[r * PITCH + 8 * lane + e] = z == 0 ? o[e] : 0.f;
             }
         }
     }
@@ -1052,7 +1052,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
         const float a = __builtin_amdgcn_exp2f(lds_ml[z][r].x - M);
         sum += a * lds_ml[z][r].y;
 #pragma unroll
-        for (int n = 0; n < CW / 4; ++n) o[n] += a * f4(&lds_o[z][r][c0 + 4 * n]);
+        for (int n = 0; n < CW / 4; ++n) o[n] += a * f4(&outs(z)[r * PITCH + c0 + 4 * n]);
     }
     if (it.direct) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;   // no key: zeros
@@ -1061,11 +1061,19 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
 #pragma unroll
         for (int n = 0; n < CW / 4; ++n) *reinterpret_cast<bf16x4*>(dst + 4 * n) = __builtin_convertvector(o[n] * inv, bf16x4);
     } else {
-        const long slot = (long)blockIdx.x * RB + r;
+        const long slot = (long)wg * RB + r;
         if (c0 == 0) p.pml[slot] = float2{M, sum};
 #pragma unroll
         for (int n = 0; n < CW / 4; ++n) *reinterpret_cast<floatx4*>(p.po + slot * DH + c0 + 4 * n) = o[n];
     }
+}
+
+template <int DH, typename CT>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_attn_rows(PagedParams p) {
+    __shared__ __align__(16) float out[NT / 64][16 * ROWS_PITCH<DH>];
+    __shared__ float2 ml[NT / 64][16];
+    __shared__ int redo;
+    attn_rows<DH, CT>(p, blockIdx.x, [&](int z) -> float* { return out[z]; }, ml, redo);
 }
 
 // ------------------------------------------------------------------ k_attn_tile: many rows
@@ -1079,16 +1087,15 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
 // an e4m3 cache 195 us.  Products and the softmax's vector work of a SIMD's two waves hardly
 // overlap; with the next block's scores formed beside this block's weights in one wave it took 181 us (all 256 registers),
 // and 218 against 196 with the order prescribed to the compiler.
+// k_even .. v_odd: LDS of AKB * DH each (a variable per ring slot: the compiler then sees that reads of one do not wait for the
+// copies into the other).
 template <int DH, typename CT, typename P>
-__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2))) void k_attn_tile(P p) {
+__device__ __forceinline__ void attn_tile(const P& p, int wg, bf16_t* k_even, bf16_t* v_even, bf16_t* k_odd, bf16_t* v_odd, int& odd) {
     constexpr bool E4M3 = sizeof(CT) == 1;
     constexpr int RB = AQ, QT = 2, NW = NT / 64, NCH = DH / 8, RPI = 64 / NCH, NKB = DH / 32, NDT = DH / 16, ESZ = sizeof(CT);
-    // (a variable per ring slot: the compiler then sees that reads of one do not wait for the copies into the other)
-    __shared__ __align__(16) bf16_t k_even[AKB * DH], v_even[AKB * DH], k_odd[AKB * DH], v_odd[AKB * DH];
-    __shared__ int odd;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, lg = lane >> 4;
-    const int w = div_by(blockIdx.x, p.by_hkv), hk = (int)blockIdx.x - w * p.HKV;
+    const int w = div_by(wg, p.by_hkv), hk = wg - w * p.HKV;
     Item it;
     if (!find_item<RB>(p, w, it) || it.chunk >= it.chunks) return;
     const int k0 = it.start + it.chunk * it.c, k1 = min(it.end - k0, it.c) + k0;
@@ -1401,12 +1408,19 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2))) void k_
 #pragma unroll
             for (int t = 0; t < NDT; ++t) *reinterpret_cast<bf16x4*>(dst + 16 * t) = __builtin_convertvector(oacc[u][t] * inv, bf16x4);
         } else {
-            const long slot = (long)blockIdx.x * RB + (r - it.rb * RB);
+            const long slot = (long)wg * RB + (r - it.rb * RB);
             if (lg == 0) p.pml[slot] = float2{m[u], l[u]};
 #pragma unroll
             for (int t = 0; t < NDT; ++t) *reinterpret_cast<floatx4*>(p.po + slot * DH + 16 * t + 4 * lg) = oacc[u][t];
         }
     }
+}
+
+template <int DH, typename CT>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2))) void k_attn_tile(PagedParams p) {
+    __shared__ __align__(16) bf16_t k_even[AKB * DH], v_even[AKB * DH], k_odd[AKB * DH], v_odd[AKB * DH];
+    __shared__ int odd;
+    attn_tile<DH, CT>(p, blockIdx.x, k_even, v_even, k_odd, v_odd, odd);
 }
 
 // ------------------------------------------------------------------ k_attn_join

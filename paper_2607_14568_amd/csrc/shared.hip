@@ -6,7 +6,8 @@
 // The rows of all the group's new tokens attend the prefix together (each sees all of it, so no key is masked), which reads
 // it once for the group, and every sequence's rows attend its own keys behind it.  So one call takes
 //   k_shared_setup   the parts: groups and sequences with their keys, chunks and items, from the lengths on the device
-//   k_attn_rows or k_attn_tile, twice: over the groups' prefixes and over the sequences' own keys
+//   k_attn_shared    the items, of the groups' prefixes (first in the grid) and of the sequences' own keys, by the workgroups of
+//                    k_attn_rows and k_attn_tile
 //   k_shared_join    every row's partial sums added up in order
 // A sequence that does not reach behind its group's prefix (a finished one, one that does not belong) takes no part in it and
 // attends all its keys by itself.
@@ -14,7 +15,7 @@
 struct SharedParams : PagedParams {
     const int4* part;         // groups {first token, tokens, P, a sequence that shares}, or sequences {first token, tokens, length, start}
     const int32_t* first;     // [parts + 1] items of one key/value head ahead of each part's
-    const int32_t* chunk;     // units per chunk
+    const int32_t* chunk;     // units per chunk (one word)
     int parts;
     bool prefix;
 };
@@ -63,118 +64,131 @@ template <int RB> __device__ __forceinline__ bool find_item(const SharedParams& 
     return true;
 }
 
+// ------------------------------------------------------------------ k_attn_shared
+// FORM: both parts by blocks of 16 rows; the prefixes by blocks of 128; both by blocks of 128.
+template <int DH, typename CT, int FORM>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_attn_shared(SharedParams g, SharedParams t, int prefix_wgs) {
+    const bool prefix = (int)blockIdx.x < prefix_wgs;
+    const int wg = (int)blockIdx.x - (prefix ? 0 : prefix_wgs);
+    const SharedParams& p = prefix ? g : t;
+    if constexpr (FORM == 0) {
+        __shared__ __align__(16) float out[NT / 64][16 * ROWS_PITCH<DH>];
+        __shared__ float2 ml[NT / 64][16];
+        __shared__ int redo;
+        attn_rows<DH, CT>(p, wg, [&](int z) -> float* { return out[z]; }, ml, redo);
+    } else {
+        __shared__ __align__(16) bf16_t k_even[AKB * DH], v_even[AKB * DH], k_odd[AKB * DH], v_odd[AKB * DH];
+        __shared__ int odd;
+        if (FORM == 2 || prefix) {
+            attn_tile<DH, CT>(p, wg, k_even, v_even, k_odd, v_odd, odd);
+        } else {
+            static_assert(16 * ROWS_PITCH<DH> * sizeof(float) <= sizeof k_even, "a wave's sums in a ring slot");
+            __shared__ float2 ml[NT / 64][16];
+            auto outs = [&](int z) { return reinterpret_cast<float*>(z == 0 ? k_even : z == 1 ? v_even : z == 2 ? k_odd : v_odd); };
+            attn_rows<DH, CT>(p, wg, outs, ml, odd);
+        }
+    }
+}
+
 // ------------------------------------------------------------------ k_shared_setup
-// One workgroup.  A part's keys are cut into chunks of c units so that all items are resident at once where that can be:
+// One workgroup.  All parts' keys are cut into chunks of c units, so that all items are resident at once where that can be:
 // c0 = ceil(all row blocks' units / round) at least, and of the next 31 c that grow by a sixteenth the first with at most
 // `round` items; where none has, c0 itself, with at most round + (row blocks) items (ceil(u / c) < u / c + 1).
-constexpr int SHARED_SEQS = 2048, NSU = 1024;   // sequences of a call; threads
+// Bound by latency.
+constexpr int SHARED_SEQS = 2048;   // sequences of a call
 
 struct SharedSetup {
     StepSeqs s;
     const int32_t* prefix;    // [groups] tokens that a group's sequences share
     const int32_t* cu_groups; // [groups + 1] offsets of the groups among the sequences; null: one group
     int groups, G, shift, cap;
-    int rbp, rbt, round_p, round_t;   // rows per block, and items at once, of the prefixes and of the sequences' own keys
-    int least_p, least_t;             // units of a chunk at least
+    int rbp, rbt;             // rows per block of the prefixes and of the sequences' own keys
+    int round, least;         // items at once (of both); units of a chunk at least
     int4* grp;                // [groups], [n]: the parts
     int4* seq;
     int32_t* group_of;        // [n]: group whose prefix a sequence attends, or -1
     int32_t* first_p;         // [groups + 1], [n + 1]: items
     int32_t* first_t;
     int32_t* block_t;         // [n + 1]: row blocks of the sequences
-    int32_t* chunk;           // of the prefixes, of the own keys
+    int32_t* chunk;
 };
 
-// Inclusive scan over the workgroup of values of 0 or more; `all`: over all threads.
-template <typename F> __device__ __forceinline__ int wg_scan(int x, F f, int* red, int& all) {
+// The first index i of [0, n) with ends[i] > x (ends nondecreasing), n where there is none.
+__device__ __forceinline__ int first_past(const int32_t* ends, int n, int x) {
+    int lo = 0, hi = n;
+    while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (ends[mid] > x) hi = mid; else lo = mid + 1;
+    }
+    return lo;
+}
+
+// Inclusive scans over the workgroup (of NW waves) of values of 0 or more; `all`: over all threads.
+template <int NW, typename F> __device__ __forceinline__ int wg_scan(int x, F f, int* red, int& all) {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     x = wave_scan(x, f);
     __syncthreads();   // (red is free)
     if (lane == 63) red[wave] = x;
     __syncthreads();
-    int y = lane < NSU / 64 ? red[lane] : 0;
+    int y = lane < NW ? red[lane] : 0;
     y = wave_scan(y, f);
-    all = __builtin_amdgcn_readlane(y, NSU / 64 - 1);
+    all = __builtin_amdgcn_readlane(y, NW - 1);
     const int before = __shfl(y, max(wave - 1, 0), 64);
     return wave > 0 ? f(x, before) : x;
 }
 
-// Units per chunk of parts with blocks[i] row blocks of units[i] units each (see above).
-__device__ __forceinline__ int chunk_units(const int* blocks, const int* units, int n, int round, int least, int* red) {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, tid = threadIdx.x;
-    float total = 0.f;
-    for (int i = lane; i < n; i += 64) total += (float)blocks[i] * (float)units[i];
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) total += __shfl_xor(total, off, 64);
-    const int c0 = max((int)min(ceilf(total * (1.f + 0x1p-17f) / (float)round), 0x1p23f), least);   // (sums of 2048 floats: 2^-18 off at most)
-    __syncthreads();
-    for (int k = wave; k < 32; k += NSU / 64) {
-        const int c = c0 + (c0 * k + 15) / 16;
-        const float rc = 1.f / (float)c;
-        int sum = 0;
-        for (int i = lane; i < n; i += 64) sum = (int)min((long)blocks[i] * ceil_div(units[i], c, rc) + sum, 1L << 24);
-        sum = last_lane(scan_add(sum));
-        if (lane == 0) red[k] = sum;
-    }
-    __syncthreads();
-    const uint64_t fits = __builtin_amdgcn_ballot_w64(lane < 32 && red[lane & 31] <= round);
-    const int k = fits ? __builtin_ctzll(fits) : 0;
-    __syncthreads();
-    (void)tid;
-    return c0 + (c0 * k + 15) / 16;
-}
-
-__global__ __launch_bounds__(NSU) void k_shared_setup(SharedSetup p) {
-    __shared__ int tok[SHARED_SEQS + 1], len[SHARED_SEQS], start[SHARED_SEQS], units[SHARED_SEQS], blocks[SHARED_SEQS];
+__global__ __launch_bounds__(NT) void k_shared_setup(SharedSetup p) {
+    constexpr int NW = NT / 64;
+    __shared__ int tok[SHARED_SEQS + 1], len[SHARED_SEQS];
     __shared__ int gend[SHARED_SEQS], gkeys[SHARED_SEQS], gseq[SHARED_SEQS];
+    __shared__ int blocks[2 * SHARED_SEQS], units[2 * SHARED_SEQS];   // of the groups, then of the sequences
     __shared__ int red[32];
-    const int tid = threadIdx.x, n = p.s.n;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = p.s.n, groups = p.groups;
     auto most = [](int a, int b) { return max(a, b); };
     auto sum = [](int a, int b) { return a + b; };
-    // sequences: tokens (offsets outside the contract are clamped as in span64) and lengths
     int carry = 0, all;
     if (tid == 0) tok[0] = 0;
-    for (int base = 0; base < n; base += NSU) {
+    // groups: their sequences end at gend; whole pages of their prefixes (offsets outside the contract are clamped as in span64)
+    for (int base = 0; base < groups; base += NT) {
+        const int g = base + tid;
+        int e = n;
+        if (g < groups) {
+            gkeys[g] = min(max(p.prefix[g], 0), p.cap) >> p.shift << p.shift;
+            gseq[g] = 1 << 30;
+        }
+        if (p.cu_groups) {
+            e = max(wg_scan<NW>(g < groups ? min(max(p.cu_groups[g + 1], 0), n) : 0, most, red, all), carry);
+            carry = max(carry, all);
+        }
+        if (g < groups) gend[g] = e;
+    }
+    // sequences: tokens and lengths
+    carry = 0;
+    for (int base = 0; base < n; base += NT) {
         const int i = base + tid;
         if (i < n) len[i] = max(p.s.lens[i], 0);
         if (p.s.cu) {
-            const int e = max(wg_scan(i < n ? min(max(p.s.cu[i + 1], 0), p.s.T) : 0, most, red, all), carry);
+            const int e = max(wg_scan<NW>(i < n ? min(max(p.s.cu[i + 1], 0), p.s.T) : 0, most, red, all), carry);
             carry = max(carry, all);
             if (i < n) tok[i + 1] = e;
         } else if (i < n) {
             tok[i + 1] = (i + 1) * p.s.T;
         }
     }
-    // groups: their sequences end at gend; whole pages of their prefixes
-    carry = 0;
-    for (int base = 0; base < p.groups; base += NSU) {
-        const int g = base + tid;
-        int e = g < p.groups ? (p.cu_groups ? min(max(p.cu_groups[g + 1], 0), n) : n) : 0;
-        e = max(wg_scan(e, most, red, all), carry);
-        carry = max(carry, all);
-        if (g < p.groups) {
-            gend[g] = e;
-            gkeys[g] = min(max(p.prefix[g], 0), p.cap) >> p.shift << p.shift;
-            gseq[g] = 1 << 30;
-        }
-    }
     __syncthreads();
-    for (int i = tid; i < n; i += NSU) {
-        int lo = 0, hi = p.groups;   // the first group that ends behind i
-        while (lo < hi) {
-            const int mid = (lo + hi) / 2;
-            if (gend[mid] > i) hi = mid; else lo = mid + 1;
-        }
-        const int m = tok[i + 1] - tok[i], P = lo < p.groups ? gkeys[lo] : 0;
+    for (int i = tid; i < n; i += NT) {
+        const int g = first_past(gend, groups, i);
+        const int m = tok[i + 1] - tok[i], P = g < groups ? gkeys[g] : 0;
         const bool shares = P > 0 && m > 0 && len[i] - m >= P;
-        if (shares) atomicMin(&gseq[lo], i);
-        start[i] = shares ? P : 0;
-        p.group_of[i] = shares ? lo : -1;
-        p.seq[i] = int4{tok[i], m, len[i], start[i]};
+        if (shares) atomicMin(&gseq[g], i);
+        const int from = shares ? P : 0;
+        p.group_of[i] = shares ? g : -1;
+        p.seq[i] = int4{tok[i], m, len[i], from};
+        blocks[groups + i] = (m * p.G + p.rbt - 1) / p.rbt;
+        units[groups + i] = max((min(len[i], p.cap) - from + UNIT - 1) / UNIT, 1);
     }
     __syncthreads();
-    // items of the prefixes
-    for (int g = tid; g < p.groups; g += NSU) {
+    for (int g = tid; g < groups; g += NT) {
         const int from = g > 0 ? gend[g - 1] : 0, m = tok[gend[g]] - tok[from];
         const bool any = gseq[g] < n;
         p.grp[g] = int4{tok[from], m, any ? gkeys[g] : 0, any ? gseq[g] : 0};
@@ -182,37 +196,43 @@ __global__ __launch_bounds__(NSU) void k_shared_setup(SharedSetup p) {
         units[g] = (gkeys[g] + UNIT - 1) / UNIT;
     }
     __syncthreads();
-    const int cp = chunk_units(blocks, units, p.groups, p.round_p, p.least_p, red);
-    carry = 0;
-    if (tid == 0) {
-        p.chunk[0] = cp;
-        p.first_p[0] = 0;
+    // units per chunk
+    float total = 0.f;
+    for (int i = lane; i < groups + n; i += 64) total += (float)blocks[i] * (float)units[i];
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) total += __shfl_xor(total, off, 64);
+    const int c0 = max((int)min(ceilf(total * (1.f + 0x1p-17f) / (float)p.round), 0x1p23f), p.least);   // (sums of 64 floats a lane: 2^-18 off at most)
+    for (int k = wave; k < 32; k += NW) {
+        const int c = c0 + (c0 * k + 15) / 16;
+        const float rc = 1.f / (float)c;
+        int x = 0;
+        for (int i = lane; i < groups + n; i += 64) x = (int)min((long)blocks[i] * ceil_div(units[i], c, rc) + x, 1L << 24);
+        x = last_lane(scan_add(x));
+        if (lane == 0) red[k] = x;
     }
-    for (int base = 0; base < p.groups; base += NSU) {
-        const int g = base + tid, x = g < p.groups ? blocks[g] * ((units[g] + cp - 1) / cp) : 0, y = wg_scan(x, sum, red, all);
-        if (g < p.groups) p.first_p[g + 1] = carry + y;
+    __syncthreads();
+    const uint64_t fits = __builtin_amdgcn_ballot_w64(lane < 32 && red[lane & 31] <= p.round);
+    const int c = c0 + (c0 * (fits ? __builtin_ctzll(fits) : 0) + 15) / 16;
+    const float rc = 1.f / (float)c;
+    if (tid == 0) {
+        p.chunk[0] = c;
+        p.first_p[0] = p.first_t[0] = p.block_t[0] = 0;
+    }
+    // items, and row blocks of the sequences
+    carry = 0;
+    for (int base = 0; base < groups; base += NT) {
+        const int g = base + tid, y = wg_scan<NW>(g < groups ? blocks[g] * ceil_div(units[g], c, rc) : 0, sum, red, all);
+        if (g < groups) p.first_p[g + 1] = carry + y;
         carry += all;
     }
-    __syncthreads();
-    // ... and of the sequences' own keys
-    for (int i = tid; i < n; i += NSU) {
-        blocks[i] = ((tok[i + 1] - tok[i]) * p.G + p.rbt - 1) / p.rbt;
-        units[i] = max((min(len[i], p.cap) - start[i] + UNIT - 1) / UNIT, 1);
-    }
-    __syncthreads();
-    const int ct = chunk_units(blocks, units, n, p.round_t, p.least_t, red);
     int carry_b = 0;
     carry = 0;
-    if (tid == 0) {
-        p.chunk[1] = ct;
-        p.first_t[0] = p.block_t[0] = 0;
-    }
-    for (int base = 0; base < n; base += NSU) {
-        const int i = base + tid, b = i < n ? blocks[i] : 0, x = i < n ? b * ((units[i] + ct - 1) / ct) : 0;
-        const int y = wg_scan(x, sum, red, all);
+    for (int base = 0; base < n; base += NT) {
+        const int i = base + tid, b = i < n ? blocks[groups + i] : 0;
+        const int y = wg_scan<NW>(i < n ? b * ceil_div(units[groups + i], c, rc) : 0, sum, red, all);
         if (i < n) p.first_t[i + 1] = carry + y;
         carry += all;
-        const int z = wg_scan(b, sum, red, all);
+        const int z = wg_scan<NW>(b, sum, red, all);
         if (i < n) p.block_t[i + 1] = carry_b + z;
         carry_b += all;
     }
