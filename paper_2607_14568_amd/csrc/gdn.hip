@@ -3273,7 +3273,7 @@ SharedPlan shared_plan(int B, int T, int H, int H_kv, int page, int max_pages, i
     p.items_t = std::min(p.blocks_t + p.round, p.blocks_t * units);
     return p;
 }
-struct SharedLayout { size_t seq, grp, group_of, first_p, first_t, block_t, chunk, ml_p, ml_t, o_p, o_t, total; };
+struct SharedLayout { size_t seq, grp, note, first_p, first_t, block, chunk, ml_p, ml_t, o_p, o_t, total; };
 SharedLayout shared_layout(const SharedPlan& p, long n, int groups, int H_kv, int d) {
     SharedLayout l;
     size_t at = 0;
@@ -3285,10 +3285,10 @@ SharedLayout shared_layout(const SharedPlan& p, long n, int groups, int H_kv, in
     const size_t rows_p = (size_t)p.items_p * H_kv * p.rbp, rows_t = (size_t)p.items_t * H_kv * p.rbt;
     l.seq = take(n * sizeof(int4));
     l.grp = take(groups * sizeof(int4));
-    l.group_of = take(n * 4);
+    l.note = take(n * sizeof(SharedNote));
     l.first_p = take((groups + 1L) * 4);
     l.first_t = take((n + 1) * 4);
-    l.block_t = take((n + 1) * 4);
+    l.block = take((n + 1) * 4);
     l.chunk = take(4);
     l.ml_p = take(rows_p * sizeof(float2));
     l.ml_t = take(rows_t * sizeof(float2));
@@ -3300,13 +3300,16 @@ SharedLayout shared_layout(const SharedPlan& p, long n, int groups, int H_kv, in
 
 template <int DH, typename CT>
 void launch_shared(const SharedSetup& setup, const SharedJoin& j, const SharedPlan& plan, hipStream_t st) {
-    hipLaunchKernelGGL(k_shared_setup, dim3(1), dim3(NT), 0, st, setup);
+    if (setup.p.s.n > 64) hipLaunchKernelGGL(k_shared_setup, dim3(1), dim3(NT), 0, st, setup);
     const int prefix_wgs = (int)(plan.items_p * j.t.HKV);
     const dim3 grid((unsigned)(prefix_wgs + plan.items_t * j.t.HKV));
-    if (plan.rbp == 16) hipLaunchKernelGGL((k_attn_shared<DH, CT, 0>), grid, dim3(NT), 0, st, j.g, j.t, prefix_wgs);
-    else if (plan.rbt == 16) hipLaunchKernelGGL((k_attn_shared<DH, CT, 1>), grid, dim3(NT), 0, st, j.g, j.t, prefix_wgs);
-    else hipLaunchKernelGGL((k_attn_shared<DH, CT, 2>), grid, dim3(NT), 0, st, j.g, j.t, prefix_wgs);
-    hipLaunchKernelGGL((k_shared_join<DH>), dim3((unsigned)(plan.blocks_t * j.t.HKV), (unsigned)plan.rows_t), dim3(NT), 0, st, j);
+    if (plan.rbp == 16) hipLaunchKernelGGL((k_attn_shared<DH, CT, 0>), grid, dim3(NT), 0, st, j.g, j.t, prefix_wgs, j.notes);
+    else if (plan.rbt == 16) hipLaunchKernelGGL((k_attn_shared<DH, CT, 1>), grid, dim3(NT), 0, st, j.g, j.t, prefix_wgs, j.notes);
+    else hipLaunchKernelGGL((k_attn_shared<DH, CT, 2>), grid, dim3(NT), 0, st, j.g, j.t, prefix_wgs, j.notes);
+    // A workgroup a row while they are all resident at once, a wave a row where there are more of them
+    const unsigned blocks = (unsigned)(plan.blocks_t * j.t.HKV), rows = (unsigned)plan.rows_t;
+    if ((long)blocks * rows <= 4 * PLAN_CUS) hipLaunchKernelGGL((k_shared_join<DH, false>), dim3(blocks, rows), dim3(NT), 0, st, j);
+    else hipLaunchKernelGGL((k_shared_join<DH, true>), dim3(blocks, (rows + NT / 64 - 1) / (NT / 64)), dim3(NT), 0, st, j);
 }
 
 template <typename IO, int DK>
@@ -4161,30 +4164,33 @@ extern "C" gdn_status gdn_attention_shared(const void* q, const void* k_cache, c
         return fail(GDN_ERR_UNSUPPORTED, "B*T*H too large");
     char* const ws = static_cast<char*>(workspace);
     auto words = [&](size_t at) { return reinterpret_cast<int32_t*>(ws + at); };
+    SharedParams p = {};
+    p.q = static_cast<const bf16_t*>(q);
+    p.o = static_cast<bf16_t*>(o);
+    p.H = H; p.HKV = H_kv; p.G = H / H_kv;
+    p.by_hkv = make_div(H_kv); p.by_g = make_div(p.G);
+    p.scale_log2 = scale * 1.4426950408889634f;
+    p.s.cu = cu_seqlens; p.s.lens = seq_lens; p.s.n = n; p.s.T = T;
+    p.c = make_cache(k_cache, v_cache, k_scale, v_scale, block_table, page, n_pages, max_pages);
+    p.prefix = prefix_lens; p.cu_groups = cu_groups; p.groups = n_groups;
+    p.rbp = plan.rbp; p.rbt = plan.rbt; p.round = plan.round;
+    p.least = plan.rbp == 16 ? 1 : 2;   // (a tile's chunk of fewer keys is mostly joining)
     SharedSetup u = {};
-    u.s.cu = cu_seqlens; u.s.lens = seq_lens; u.s.n = n; u.s.T = T;
-    u.prefix = prefix_lens; u.cu_groups = cu_groups; u.groups = n_groups;
-    u.G = H / H_kv;
-    u.rbp = plan.rbp; u.rbt = plan.rbt; u.round = plan.round;
-    u.least = plan.rbp == 16 ? 1 : 2;   // (a tile's chunk of fewer keys is mostly joining)
+    u.p = p;
     u.grp = reinterpret_cast<int4*>(ws + lay.grp); u.seq = reinterpret_cast<int4*>(ws + lay.seq);
-    u.group_of = words(lay.group_of); u.first_p = words(lay.first_p); u.first_t = words(lay.first_t);
-    u.block_t = words(lay.block_t); u.chunk = words(lay.chunk);
+    u.first_p = words(lay.first_p); u.first_t = words(lay.first_t); u.chunk = words(lay.chunk);
+    u.notes.note = reinterpret_cast<SharedNote*>(ws + lay.note); u.notes.block = words(lay.block);
     SharedJoin j = {};
-    j.t.q = static_cast<const bf16_t*>(q);
-    j.t.o = static_cast<bf16_t*>(o);
-    j.t.H = H; j.t.HKV = H_kv; j.t.G = u.G;
-    j.t.by_hkv = make_div(H_kv); j.t.by_g = make_div(u.G);
-    j.t.scale_log2 = scale * 1.4426950408889634f;
-    j.t.s = u.s;
-    j.t.c = make_cache(k_cache, v_cache, k_scale, v_scale, block_table, page, n_pages, max_pages);
-    u.shift = j.t.c.shift; u.cap = max_pages << j.t.c.shift;
-    j.g = j.t;
-    j.t.part = u.seq; j.t.first = u.first_t; j.t.chunk = u.chunk; j.t.parts = n; j.t.prefix = false;
-    j.g.part = u.grp; j.g.first = u.first_p; j.g.chunk = u.chunk; j.g.parts = n_groups; j.g.prefix = true;
+    j.t = j.g = p;
+    j.g.of_prefix = true;
+    if (n > 64) {   // (the parts from k_shared_setup)
+        j.t.part = u.seq; j.t.first = u.first_t; j.t.chunk = u.chunk; j.t.parts = n;
+        j.g.part = u.grp; j.g.first = u.first_p; j.g.chunk = u.chunk; j.g.parts = n_groups;
+    }
     j.t.pml = reinterpret_cast<float2*>(ws + lay.ml_t); j.t.po = reinterpret_cast<float*>(ws + lay.o_t);
     j.g.pml = reinterpret_cast<float2*>(ws + lay.ml_p); j.g.po = reinterpret_cast<float*>(ws + lay.o_p);
-    j.group_of = u.group_of; j.block_t = u.block_t; j.rbp = plan.rbp; j.rbt = plan.rbt;
+    j.notes = u.notes;
+    j.each = n_seqs > 0 ? 0 : (int)(((long)T * p.G + plan.rbt - 1) / plan.rbt);
     hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
     (void)hipGetLastError();
     if (cache_dtype == GDN_BF16) {

@@ -5,7 +5,8 @@
 //   m = max(m1, m2),  l = l1 2^(m1 - m) + l2 2^(m2 - m),  o = (o1 2^(m1 - m) + o2 2^(m2 - m)) / l.
 // The rows of all the group's new tokens attend the prefix together (each sees all of it, so no key is masked), which reads
 // it once for the group, and every sequence's rows attend its own keys behind it.  So one call takes
-//   k_shared_setup   the parts: groups and sequences with their keys, chunks and items, from the lengths on the device
+//   k_shared_setup   more than 64 sequences: the parts, groups and sequences with their keys, chunks and items, from the lengths on
+//                    the device (fewer: every wave of the next one does so by itself)
 //   k_attn_shared    the items, of the groups' prefixes (first in the grid) and of the sequences' own keys, by the workgroups of
 //                    k_attn_rows and k_attn_tile
 //   k_shared_join    every row's partial sums added up in order
@@ -13,12 +14,94 @@
 // attends all its keys by itself.
 
 struct SharedParams : PagedParams {
+    const int32_t* prefix;    // [groups] tokens that a group's sequences share
+    const int32_t* cu_groups; // [groups + 1] offsets of the groups among the sequences; null: one group
+    int groups;
+    int rbp, rbt;             // rows per block of the prefixes and of the sequences' own keys
+    int least;                // units of a chunk at least (round: items at once, of both)
+    // The parts as k_shared_setup left them, or null: up to 64 sequences, whose parts every wave works out by itself.
     const int4* part;         // groups {first token, tokens, P, a sequence that shares}, or sequences {first token, tokens, length, start}
     const int32_t* first;     // [parts + 1] items of one key/value head ahead of each part's
     const int32_t* chunk;     // units per chunk (one word)
     int parts;
-    bool prefix;
+    bool of_prefix;           // the groups' prefixes, or the sequences' own keys
 };
+
+// Units per chunk, from all row blocks' units and the number of row blocks; count(c): items with chunks of c units, at most
+// all / c + blocks (ceil(u / c) < u / c + 1).  As many as are resident at once are wanted, `round`: a c that makes them with half
+// a unit lost a block, if it does; else the c that makes at most `round` whatever the lengths, unless its chunks are more
+// than twice as long as those of c0 = ceil(all / round), which makes at most round + blocks.  (No search among more of them: a
+// count takes a wave half a microsecond.)
+template <typename F> __device__ __forceinline__ int chunk_units(double all, int blocks, int round, int least, F count) {
+    auto least_of = [&](double slots) { return max((int)min(ceil(all / slots), 0x1p23), least); };
+    const int c0 = least_of(round);
+    if (blocks >= round) return c0;
+    const int mid = least_of(round - 0.5 * blocks);
+    if (count(mid) <= round) return mid;
+    const int c1 = least_of(round - blocks);
+    return c1 <= 2 * c0 ? c1 : c0;
+}
+
+// What k_shared_join takes of a sequence, and where its row blocks begin (of one key/value head).
+struct SharedNote {
+    int tok, n, len, start;           // first token, tokens, length, first key of its own
+    int first, block, c, gfirst;      // first item; first row block; units per chunk; first item of its group's prefix
+    int gblocks, grow, pad[2];        // row blocks of its group, and the sequence's first row in them
+};
+struct SharedNotes {
+    SharedNote* note;         // [n]
+    int32_t* block;           // [n + 1] row blocks of the sequences ahead of each one's
+};
+
+// The parts of up to 64 sequences and groups: a lane's sequence and a lane's group.
+struct Parts {
+    int tok, n, len, start, group;            // sequence: first token, tokens, length, first key of its own, group
+    int gtok, gn, gkeys, gseq;                // group: first token, tokens, P (0: nobody reaches behind it), a sequence that shares
+    int blocks, units, gblocks, gunits, c;    // row blocks and units of either; units per chunk
+    __device__ __forceinline__ int items() const { return blocks * ceil_div(units, c, 1.f / (float)c); }
+    __device__ __forceinline__ int gitems() const { return gblocks * ceil_div(gunits, c, 1.f / (float)c); }
+};
+__device__ __forceinline__ double scan64(double x);
+__device__ __forceinline__ double lane64(double x, int l);
+__device__ __forceinline__ Parts parts64(const SharedParams& p) {
+    const int lane = threadIdx.x & 63, n = p.s.n, groups = p.groups, cap = p.c.max_pages << p.c.shift;
+    Parts q;
+    q.len = lane < n ? max(p.s.lens[lane], 0) : 0;
+    int P = lane < groups ? p.prefix[lane] : 0, gend = lane < groups && p.cu_groups ? p.cu_groups[lane + 1] : 0;
+    int at = 0, end;
+    span64(p.s, 0, at, q.tok, end);
+    q.n = end - q.tok;
+    gend = p.cu_groups ? scan_max(lane < groups ? min(max(gend, 0), n) : 0) : n;
+    const int gbeg = p.cu_groups ? lane_before(gend, 0) : lane == 0 ? 0 : n;
+    P = min(max(P, 0), cap) >> p.c.shift << p.c.shift;
+    q.group = 0;
+    for (int g = 0; g < groups; ++g) q.group += __builtin_amdgcn_readlane(gend, g) <= lane;
+    const int mine = __shfl(P, min(q.group, groups - 1), 64);
+    const bool shares = q.group < groups && mine > 0 && q.n > 0 && q.len - q.n >= mine;
+    q.start = shares ? mine : 0;
+    q.gseq = -1;
+    for (int g = 0; g < groups; ++g) {
+        const uint64_t any = __builtin_amdgcn_ballot_w64(shares && q.group == g);
+        if (lane == g && any) q.gseq = __builtin_ctzll(any);
+    }
+    const int first = __shfl(end, max(gbeg - 1, 0), 64), last = __shfl(end, max(gend - 1, 0), 64);   // (a sequence's tokens end where the next one's begin)
+    q.gtok = gbeg > 0 ? first : 0;
+    q.gn = gend > 0 ? last - q.gtok : 0;
+    q.gkeys = q.gseq >= 0 ? P : 0;
+    q.blocks = (q.n * p.G + p.rbt - 1) / p.rbt;
+    q.units = max((min(q.len, cap) - q.start + UNIT - 1) / UNIT, 1);
+    q.gblocks = q.gseq >= 0 ? (q.gn * p.G + p.rbp - 1) / p.rbp : 0;
+    q.gunits = (q.gkeys + UNIT - 1) / UNIT;
+    const double all = lane64(scan64((double)q.blocks * q.units + (double)q.gblocks * q.gunits), 63);
+    const int blocks = last_lane(scan_add(min(q.blocks + q.gblocks, 1 << 24)));
+    q.c = chunk_units(all, blocks, p.round, p.least, [&](int c) {
+        const float rc = 1.f / (float)c;
+        const long x = (long)q.blocks * ceil_div(q.units, c, rc) + (long)q.gblocks * ceil_div(q.gunits, c, rc);
+        return last_lane(scan_add((int)min(x, 1L << 24)));
+    });
+    q.c = __builtin_amdgcn_readfirstlane(q.c);
+    return q;
+}
 
 // The last index i of [0, n) with first[i] <= w (`first` nondecreasing, its next entry past w), by a whole wave; -1 where
 // w is past the last.
@@ -36,19 +119,37 @@ __device__ __forceinline__ int part_of(const int32_t* first, int n, int w) {
 }
 
 template <int RB> __device__ __forceinline__ bool find_item(const SharedParams& p, int w, Item& it) {
-    const int s = part_of(p.first, p.parts, w);
-    if (s < 0) return false;
-    const int* x = reinterpret_cast<const int*>(p.part + s);
-    it.tok = tab(x, 0);
-    it.n = tab(x, 1);
-    const int a = tab(x, 2), b = tab(x, 3);
+    int s, a, b, c;
+    if (p.part) {
+        s = part_of(p.first, p.parts, w);
+        if (s < 0) return false;
+        const int* x = reinterpret_cast<const int*>(p.part + s);
+        it.tok = tab(x, 0);
+        it.n = tab(x, 1);
+        a = tab(x, 2);
+        b = tab(x, 3);
+        it.first = tab(p.first, s);
+        c = tab(p.chunk, 0);
+    } else {
+        const Parts q = parts64(p);
+        const int x = p.of_prefix ? q.gitems() : q.items(), y = scan_add(x);
+        const uint64_t past = __builtin_amdgcn_ballot_w64(y > w);
+        if (!past) return false;
+        s = __builtin_ctzll(past);
+        auto of = [s](int x) { return __builtin_amdgcn_readlane(x, s); };
+        it.tok = of(p.of_prefix ? q.gtok : q.tok);
+        it.n = of(p.of_prefix ? q.gn : q.n);
+        a = of(p.of_prefix ? q.gkeys : q.len);
+        b = of(p.of_prefix ? q.gseq : q.start);
+        it.first = of(y - x);
+        c = q.c;
+    }
     it.nrb = (it.n * p.G + RB - 1) / RB;
-    it.first = tab(p.first, s);
     const int r = w - it.first;
     it.chunk = r / it.nrb;
     const int z = r - it.chunk * it.nrb;
     it.rb = it.chunk % 2 ? z : it.nrb - 1 - z;   // see item_of
-    if (p.prefix) {
+    if (p.of_prefix) {
         it.s = b;
         it.len = a + it.n + AKB;   // (every row sees every key, and those of the last block behind them)
         it.start = 0;
@@ -59,15 +160,30 @@ template <int RB> __device__ __forceinline__ bool find_item(const SharedParams& 
         it.start = b;
         it.end = block_end<RB>(p, it.n, a, it.rb);
     }
-    cut_keys(it, it.end - it.start, tab(p.chunk, 0));
-    it.direct = !p.prefix && it.start == 0 && it.chunks == 1;
+    cut_keys(it, it.end - it.start, c);
+    it.direct = !p.of_prefix && it.start == 0 && it.chunks == 1;
     return true;
+}
+
+// The notes of up to 64 sequences, by a wave.
+__device__ __forceinline__ void write_notes(const SharedParams& p, const SharedNotes& to) {
+    const int lane = threadIdx.x & 63;
+    const Parts q = parts64(p);
+    const int b = scan_add(q.blocks), x = q.items(), y = scan_add(x), gx = q.gitems(), gy = scan_add(gx), g = min(q.group, 63);
+    SharedNote r = {q.tok, q.n, q.len, q.start, y - x, b - q.blocks, q.c, __shfl(gy - gx, g, 64), __shfl(q.gblocks, g, 64), 0, {0, 0}};
+    r.grow = (q.tok - __shfl(q.gtok, g, 64)) * p.G;
+    if (lane < p.s.n) {
+        to.note[lane] = r;
+        to.block[lane + 1] = b;
+    }
+    if (lane == 0) to.block[0] = 0;
 }
 
 // ------------------------------------------------------------------ k_attn_shared
 // FORM: both parts by blocks of 16 rows; the prefixes by blocks of 128; both by blocks of 128.
 template <int DH, typename CT, int FORM>
-__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_attn_shared(SharedParams g, SharedParams t, int prefix_wgs) {
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_attn_shared(SharedParams g, SharedParams t, int prefix_wgs, SharedNotes notes) {
+    if (blockIdx.x == 0 && threadIdx.x < 64 && !g.part) write_notes(t, notes);
     const bool prefix = (int)blockIdx.x < prefix_wgs;
     const int wg = (int)blockIdx.x - (prefix ? 0 : prefix_wgs);
     const SharedParams& p = prefix ? g : t;
@@ -91,26 +207,17 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
 }
 
 // ------------------------------------------------------------------ k_shared_setup
-// One workgroup.  All parts' keys are cut into chunks of c units, so that all items are resident at once where that can be:
-// c0 = ceil(all row blocks' units / round) at least, and of the next 31 c that grow by a sixteenth the first with at most
-// `round` items; where none has, c0 itself, with at most round + (row blocks) items (ceil(u / c) < u / c + 1).
-// Bound by latency.
+// One workgroup works out the parts of more than 64 sequences, for all.  Bound by latency.
 constexpr int SHARED_SEQS = 2048;   // sequences of a call
 
 struct SharedSetup {
-    StepSeqs s;
-    const int32_t* prefix;    // [groups] tokens that a group's sequences share
-    const int32_t* cu_groups; // [groups + 1] offsets of the groups among the sequences; null: one group
-    int groups, G, shift, cap;
-    int rbp, rbt;             // rows per block of the prefixes and of the sequences' own keys
-    int round, least;         // items at once (of both); units of a chunk at least
+    SharedParams p;
     int4* grp;                // [groups], [n]: the parts
     int4* seq;
-    int32_t* group_of;        // [n]: group whose prefix a sequence attends, or -1
     int32_t* first_p;         // [groups + 1], [n + 1]: items
     int32_t* first_t;
-    int32_t* block_t;         // [n + 1]: row blocks of the sequences
     int32_t* chunk;
+    SharedNotes notes;
 };
 
 // The first index i of [0, n) with ends[i] > x (ends nondecreasing), n where there is none.
@@ -137,42 +244,44 @@ template <int NW, typename F> __device__ __forceinline__ int wg_scan(int x, F f,
     return wave > 0 ? f(x, before) : x;
 }
 
-__global__ __launch_bounds__(NT) void k_shared_setup(SharedSetup p) {
+__global__ __launch_bounds__(NT) void k_shared_setup(SharedSetup u) {
+    const SharedParams& p = u.p;
     constexpr int NW = NT / 64;
-    __shared__ int tok[SHARED_SEQS + 1], len[SHARED_SEQS];
-    __shared__ int gend[SHARED_SEQS], gkeys[SHARED_SEQS], gseq[SHARED_SEQS];
-    __shared__ int blocks[2 * SHARED_SEQS], units[2 * SHARED_SEQS];   // of the groups, then of the sequences
-    __shared__ int red[32];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = p.s.n, groups = p.groups;
+    __shared__ int tok[SHARED_SEQS + 1], len[SHARED_SEQS], start[SHARED_SEQS], group[SHARED_SEQS];
+    __shared__ int gend[SHARED_SEQS], gkeys[SHARED_SEQS], gseq[SHARED_SEQS], gfirst[SHARED_SEQS];
+    __shared__ int2 work[2 * SHARED_SEQS];   // row blocks and units of the groups, then of the sequences
+    __shared__ int red[NW];
+    const int tid = threadIdx.x, lane = tid & 63, n = p.s.n, groups = p.groups, cap = p.c.max_pages << p.c.shift;
     auto most = [](int a, int b) { return max(a, b); };
     auto sum = [](int a, int b) { return a + b; };
-    int carry = 0, all;
+    // groups: their sequences end at gend; whole pages of their prefixes (offsets outside the contract are clamped as in span64).
+    // Sequences: tokens and lengths.  All of the first NT's values are asked for before any is used.
+    int carry_g = 0, carry = 0, all;
     if (tid == 0) tok[0] = 0;
-    // groups: their sequences end at gend; whole pages of their prefixes (offsets outside the contract are clamped as in span64)
-    for (int base = 0; base < groups; base += NT) {
-        const int g = base + tid;
-        int e = n;
-        if (g < groups) {
-            gkeys[g] = min(max(p.prefix[g], 0), p.cap) >> p.shift << p.shift;
-            gseq[g] = 1 << 30;
-        }
-        if (p.cu_groups) {
-            e = max(wg_scan<NW>(g < groups ? min(max(p.cu_groups[g + 1], 0), n) : 0, most, red, all), carry);
-            carry = max(carry, all);
-        }
-        if (g < groups) gend[g] = e;
-    }
-    // sequences: tokens and lengths
-    carry = 0;
-    for (int base = 0; base < n; base += NT) {
+    for (int base = 0; base < max(n, groups); base += NT) {
         const int i = base + tid;
-        if (i < n) len[i] = max(p.s.lens[i], 0);
+        const int L = i < n ? p.s.lens[i] : 0, P = i < groups ? p.prefix[i] : 0;
+        int e = i < n && p.s.cu ? p.s.cu[i + 1] : 0, g = i < groups && p.cu_groups ? p.cu_groups[i + 1] : 0;
+        if (p.cu_groups) {
+            g = max(wg_scan<NW>(min(max(g, 0), n), most, red, all), carry_g);
+            carry_g = max(carry_g, all);
+        } else {
+            g = n;
+        }
         if (p.s.cu) {
-            const int e = max(wg_scan<NW>(i < n ? min(max(p.s.cu[i + 1], 0), p.s.T) : 0, most, red, all), carry);
+            e = max(wg_scan<NW>(min(max(e, 0), p.s.T), most, red, all), carry);
             carry = max(carry, all);
-            if (i < n) tok[i + 1] = e;
-        } else if (i < n) {
-            tok[i + 1] = (i + 1) * p.s.T;
+        } else {
+            e = (i + 1) * p.s.T;
+        }
+        if (i < groups) {
+            gend[i] = g;
+            gkeys[i] = min(max(P, 0), cap) >> p.c.shift << p.c.shift;
+            gseq[i] = 1 << 30;
+        }
+        if (i < n) {
+            len[i] = max(L, 0);
+            tok[i + 1] = e;
         }
     }
     __syncthreads();
@@ -181,120 +290,120 @@ __global__ __launch_bounds__(NT) void k_shared_setup(SharedSetup p) {
         const int m = tok[i + 1] - tok[i], P = g < groups ? gkeys[g] : 0;
         const bool shares = P > 0 && m > 0 && len[i] - m >= P;
         if (shares) atomicMin(&gseq[g], i);
-        const int from = shares ? P : 0;
-        p.group_of[i] = shares ? g : -1;
-        p.seq[i] = int4{tok[i], m, len[i], from};
-        blocks[groups + i] = (m * p.G + p.rbt - 1) / p.rbt;
-        units[groups + i] = max((min(len[i], p.cap) - from + UNIT - 1) / UNIT, 1);
+        start[i] = shares ? P : 0;
+        group[i] = g;
+        u.seq[i] = int4{tok[i], m, len[i], start[i]};
+        work[groups + i] = int2{(m * p.G + p.rbt - 1) / p.rbt, max((min(len[i], cap) - start[i] + UNIT - 1) / UNIT, 1)};
     }
     __syncthreads();
     for (int g = tid; g < groups; g += NT) {
         const int from = g > 0 ? gend[g - 1] : 0, m = tok[gend[g]] - tok[from];
         const bool any = gseq[g] < n;
-        p.grp[g] = int4{tok[from], m, any ? gkeys[g] : 0, any ? gseq[g] : 0};
-        blocks[g] = any ? (m * p.G + p.rbp - 1) / p.rbp : 0;
-        units[g] = (gkeys[g] + UNIT - 1) / UNIT;
+        u.grp[g] = int4{tok[from], m, any ? gkeys[g] : 0, any ? gseq[g] : 0};
+        work[g] = int2{any ? (m * p.G + p.rbp - 1) / p.rbp : 0, (gkeys[g] + UNIT - 1) / UNIT};
     }
     __syncthreads();
-    // units per chunk
-    float total = 0.f;
-    for (int i = lane; i < groups + n; i += 64) total += (float)blocks[i] * (float)units[i];
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) total += __shfl_xor(total, off, 64);
-    const int c0 = max((int)min(ceilf(total * (1.f + 0x1p-17f) / (float)p.round), 0x1p23f), p.least);   // (sums of 64 floats a lane: 2^-18 off at most)
-    for (int k = wave; k < 32; k += NW) {
-        const int c = c0 + (c0 * k + 15) / 16;
+    // units per chunk (sums of up to 64 parts a lane, in every wave)
+    double total = 0.;
+    int nb = 0;
+    for (int i = lane; i < groups + n; i += 64) {
+        total += (double)work[i].x * work[i].y;
+        nb = min(nb + work[i].x, 1 << 24);
+    }
+    const int c = chunk_units(lane64(scan64(total), 63), last_lane(scan_add(nb)), p.round, p.least, [&](int c) {
         const float rc = 1.f / (float)c;
         int x = 0;
-        for (int i = lane; i < groups + n; i += 64) x = (int)min((long)blocks[i] * ceil_div(units[i], c, rc) + x, 1L << 24);
-        x = last_lane(scan_add(x));
-        if (lane == 0) red[k] = x;
-    }
-    __syncthreads();
-    const uint64_t fits = __builtin_amdgcn_ballot_w64(lane < 32 && red[lane & 31] <= p.round);
-    const int c = c0 + (c0 * (fits ? __builtin_ctzll(fits) : 0) + 15) / 16;
+        for (int i = lane; i < groups + n; i += 64) x = (int)min((long)work[i].x * ceil_div(work[i].y, c, rc) + x, 1L << 24);
+        return last_lane(scan_add(x));
+    });
     const float rc = 1.f / (float)c;
     if (tid == 0) {
-        p.chunk[0] = c;
-        p.first_p[0] = p.first_t[0] = p.block_t[0] = 0;
+        u.chunk[0] = c;
+        u.first_p[0] = u.first_t[0] = u.notes.block[0] = 0;
     }
     // items, and row blocks of the sequences
     carry = 0;
     for (int base = 0; base < groups; base += NT) {
-        const int g = base + tid, y = wg_scan<NW>(g < groups ? blocks[g] * ceil_div(units[g], c, rc) : 0, sum, red, all);
-        if (g < groups) p.first_p[g + 1] = carry + y;
-        carry += all;
+        const int g = base + tid, x = g < groups ? work[g].x * ceil_div(work[g].y, c, rc) : 0;
+        const int y = groups > 1 ? wg_scan<NW>(x, sum, red, all) : x;
+        if (g < groups) {
+            gfirst[g] = carry + y - x;
+            u.first_p[g + 1] = carry + y;
+        }
+        if (groups > 1) carry += all;
     }
+    __syncthreads();
     int carry_b = 0;
     carry = 0;
     for (int base = 0; base < n; base += NT) {
-        const int i = base + tid, b = i < n ? blocks[groups + i] : 0;
-        const int y = wg_scan<NW>(i < n ? b * ceil_div(units[groups + i], c, rc) : 0, sum, red, all);
-        if (i < n) p.first_t[i + 1] = carry + y;
+        const int i = base + tid, b = i < n ? work[groups + i].x : 0, x = i < n ? b * ceil_div(work[groups + i].y, c, rc) : 0;
+        const int y = carry + wg_scan<NW>(x, sum, red, all);
         carry += all;
-        const int z = wg_scan<NW>(b, sum, red, all);
-        if (i < n) p.block_t[i + 1] = carry_b + z;
-        carry_b += all;
+        int z = (i + 1) * b;   // (a dense step's sequences have as many row blocks each)
+        if (p.s.cu) {
+            z = carry_b + wg_scan<NW>(b, sum, red, all);
+            carry_b += all;
+        }
+        if (i < n) {
+            u.first_t[i + 1] = y;
+            u.notes.block[i + 1] = z;
+            const int g = start[i] > 0 ? group[i] : -1;
+            u.notes.note[i] = {tok[i], tok[i + 1] - tok[i], len[i], start[i], y - x, z - b, c, g >= 0 ? gfirst[g] : 0,
+                               g >= 0 ? work[g].x : 0, g >= 0 ? (tok[i] - tok[g > 0 ? gend[g - 1] : 0]) * p.G : 0, {0, 0}};
+        }
     }
 }
 
 // ------------------------------------------------------------------ k_shared_join
-// One workgroup per row (blockIdx.y) of a row block of the sequences' own keys and key/value head: the block's chunks, then
-// those of the prefix, as k_attn_join adds them up.
+// One workgroup per row (or, WAVE, one wave: blockIdx.y holds NT / 64 of them) of a row block of the sequences' own keys and
+// key/value head: the block's chunks, then those of the prefix, as k_attn_join adds them up.  Bound by latency: the block's
+// sequence, its numbers, the partial sums.
 struct SharedJoin {
     SharedParams t;           // the sequences' own keys, and their partial sums
     SharedParams g;           // the groups' prefixes
-    const int32_t* group_of;
-    const int32_t* block_t;
-    int rbp, rbt;
+    SharedNotes notes;
+    int each;                 // row blocks of a dense step's sequence, or 0
 };
 
-template <int DH>
+template <int DH, bool WAVE>
 __global__ __launch_bounds__(NT) void k_shared_join(SharedJoin p) {
-    constexpr int LPR = DH / 4, SUB = 64 / LPR, NW = NT / 64;   // lanes per row; chunks that a wave's load takes at once
+    constexpr int LPR = DH / 4, SUB = 64 / LPR, NW = WAVE ? 1 : NT / 64;   // lanes per row; chunks that a wave's load takes at once; waves a row
     __shared__ __align__(16) float red[NW][DH];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, at = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = WAVE ? 0 : at;
     const int b = div_by(blockIdx.x, p.t.by_hkv), hk = (int)blockIdx.x - b * p.t.HKV, c4 = 4 * (lane % LPR), HKV = p.t.HKV, G = p.t.G;
-    const int s = part_of(p.block_t, p.t.parts, b);
+    const int s = p.each ? b / p.each : part_of(p.notes.block, p.t.s.n, b);
     if (s < 0) return;
-    const int* x = reinterpret_cast<const int*>(p.t.part + s);
-    Item it;
+    const int* x = reinterpret_cast<const int*>(p.notes.note + s);
+    Item it, gr;
     it.tok = tab(x, 0);
     it.n = tab(x, 1);
     it.len = tab(x, 2);
     it.start = tab(x, 3);
-    it.nrb = (it.n * G + p.rbt - 1) / p.rbt;
-    it.first = tab(p.t.first, s);
-    it.rb = b - tab(p.block_t, s);
-    it.end = p.rbt == 16 ? block_end<16>(p.t, it.n, it.len, it.rb) : block_end<AQ>(p.t, it.n, it.len, it.rb);
-    cut_keys(it, it.end - it.start, tab(p.t.chunk, 0));
+    it.first = tab(x, 4);
+    it.rb = b - tab(x, 5);
+    const int c = tab(x, 6), row0 = tab(x, 9);
+    gr.first = tab(x, 7);
+    gr.nrb = tab(x, 8);
+    it.nrb = (it.n * G + p.t.rbt - 1) / p.t.rbt;
+    it.end = p.t.rbt == 16 ? block_end<16>(p.t, it.n, it.len, it.rb) : block_end<AQ>(p.t, it.n, it.len, it.rb);
+    cut_keys(it, it.end - it.start, c);
     if (it.start == 0 && it.chunks == 1) return;
-    const int r = blockIdx.y, rr = it.rb * p.rbt + r;
-    if (r >= p.rbt || rr >= it.n * G) return;
-    Item gr;
+    const int r = WAVE ? (int)blockIdx.y * (NT / 64) + at : (int)blockIdx.y, rr = it.rb * p.t.rbt + r;
+    if (r >= p.t.rbt || rr >= it.n * G) return;
     gr.chunks = 0;
-    int rg = 0;   // the row in its block of the group
-    if (it.start > 0) {
-        const int g = tab(p.group_of, s);
-        const int* y = reinterpret_cast<const int*>(p.g.part + g);
-        const int row = (it.tok - tab(y, 0)) * G + rr;
-        gr.n = tab(y, 1);
-        gr.end = tab(y, 2);
-        gr.nrb = (gr.n * G + p.rbp - 1) / p.rbp;
-        gr.rb = row / p.rbp;
-        rg = row - gr.rb * p.rbp;
-        gr.first = tab(p.g.first, g);
-        cut_keys(gr, gr.end, tab(p.g.chunk, 0));
-    }
+    const int row = row0 + rr;   // of the group
+    gr.rb = row / p.t.rbp;
+    const int rg = row - gr.rb * p.t.rbp;
+    if (it.start > 0) cut_keys(gr, it.start, c);
     const int own = it.chunks, chunks = own + gr.chunks;
     auto slot = [&](int j) {   // in the group's partial sums from `own` on
-        return j < own ? ((long)item_of(it, j) * HKV + hk) * p.rbt + r : ((long)item_of(gr, j - own) * HKV + hk) * p.rbp + rg;
+        return j < own ? ((long)item_of(it, j) * HKV + hk) * p.t.rbt + r : ((long)item_of(gr, j - own) * HKV + hk) * p.t.rbp + rg;
     };
-    constexpr int EACH = 64 / (NW * SUB);   // loads of a wave for 64 chunks, all sent off before the first is used
+    constexpr int STEP = WAVE ? 8 * SUB : 64, EACH = STEP / (NW * SUB);   // chunks at a time, and their loads of a wave, all sent off first
     const int mine = wave * SUB + lane / LPR;
     float M = LOWEST, sum = 0.f;
     floatx4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int j0 = 0; j0 < chunks; j0 += 64) {
+    for (int j0 = 0; j0 < chunks; j0 += STEP) {
         floatx4 y[EACH];
 #pragma unroll
         for (int k = 0; k < EACH; ++k) {
@@ -303,7 +412,7 @@ __global__ __launch_bounds__(NT) void k_shared_join(SharedJoin p) {
             if (j < chunks) y[k] = f4((j < own ? p.t.po : p.g.po) + slot(j) * DH + c4);
         }
         float2 ml = {LOWEST, 0.f};   // of chunk j0 + lane
-        if (j0 + lane < chunks) ml = (j0 + lane < own ? p.t.pml : p.g.pml)[slot(j0 + lane)];
+        if (lane < STEP && j0 + lane < chunks) ml = (j0 + lane < own ? p.t.pml : p.g.pml)[slot(j0 + lane)];
         float top = fmaxf(M, ml.x);
 #pragma unroll
         for (int off = 1; off < 64; off <<= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
@@ -323,12 +432,14 @@ __global__ __launch_bounds__(NT) void k_shared_join(SharedJoin p) {
     for (int off = LPR; off < 64; off <<= 1)
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], off, 64);
-    if (lane < LPR) *reinterpret_cast<floatx4*>(&red[wave][c4]) = o;
-    __syncthreads();
-    if (wave != 0 || lane >= LPR) return;
-    o = f4(&red[0][c4]);
+    if constexpr (!WAVE) {
+        if (lane < LPR) *reinterpret_cast<floatx4*>(&red[wave][c4]) = o;
+        __syncthreads();
+        o = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int z = 1; z < NW; ++z) o += f4(&red[z][c4]);
+        for (int z = 0; z < NW; ++z) o += f4(&red[z][c4]);
+    }
+    if (wave != 0 || lane >= LPR) return;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     const int i = div_by(rr, p.t.by_g);
     bf16_t* dst = p.t.o + ((long)(it.tok + i) * p.t.H + hk * G + rr - i * G) * DH + c4;
