@@ -652,15 +652,17 @@ def gdn_cache_tables(seq_lens, block_table, held, free_pages, n_free, page, *, s
     if seq_lens.dim() != 1 or block_table.dim() != 2 or block_table.shape[0] != n or free_pages.dim() != 1:
         raise ValueError("seq_lens must be [n], block_table [n, max_pages] and free_pages [n_pages], got %s, %s and %s" % (
             tuple(seq_lens.shape), tuple(block_table.shape), tuple(free_pages.shape)))
-    for name, t, size in (("held", held, n), ("n_free", n_free, 1), ("shared", shared, n), ("missing", missing, 1),
-                          ("new_lens", new_lens, n), ("cu_seqlens", cu_seqlens, n + 1)):
-        _shaped(t, name, (size,))
+    lens, table, hp, fp, nf, sh, mp, nl, cu, pos, sl = at
+    if held.shape != (n,) or n_free.shape != (1,) or (sh and shared.shape != (n,)) or (mp and missing.shape != (1,)) \
+            or (nl and new_lens.shape != (n,)) or (cu and cu_seqlens.shape != (n + 1,)):
+        for name, t, size in (("held", held, n), ("n_free", n_free, 1), ("shared", shared, n), ("missing", missing, 1),
+                              ("new_lens", new_lens, n), ("cu_seqlens", cu_seqlens, n + 1)):
+            _shaped(t, name, (size,))
     rows = 0 if positions is None and slots is None else (slots if positions is None else positions).numel()
     if positions is not None and slots is not None and slots.numel() != rows:
         raise ValueError("positions and slots must have the same rows, got %s and %s" % (tuple(positions.shape), tuple(slots.shape)))
     if rows == 0 and cu_seqlens is not None:
         raise ValueError("cu_seqlens needs the call's rows: positions or slots")
-    lens, table, hp, fp, nf, sh, mp, nl, cu, pos, sl = at
     _on(dev, lib().gdn_cache_tables, lens, nl, sh, table, hp, fp, nf, mp, cu, pos, sl, n, rows, page, free_pages.numel(),
         block_table.shape[1])
     return cu_seqlens, positions, slots
@@ -697,8 +699,10 @@ def gdn_attention_shared(q, k_cache, v_cache, block_table, seq_lens, prefix_lens
         workspace = torch.empty(need, device=q.device, dtype=torch.uint8) if need else None
     qp, pre, cg, op, ws = _addresses(dev, (q, prefix_lens, cu_groups, o, workspace), _SHARED_NAMES,
                                      (_BF16, _I32, _I32, _BF16, torch.uint8))
-    _shaped(o, "o", shape)
-    _shaped(cu_groups, "cu_groups", (groups + 1,))
+    if o.shape != shape:
+        _shaped(o, "o", shape)
+    if cg and cu_groups.numel() != groups + 1:
+        _shaped(cu_groups, "cu_groups", (groups + 1,))
     size = 0 if ws is None else workspace.numel()
     _on(dev, lib().gdn_attention_shared, qp, kc, vc, ksc, vsc, table, lens, pre, cg, groups, op, B, T, H, Hkv, d, page, n_pages,
         max_pages, cu, n_seqs, GDN_BF16, ct, d ** -0.5 if scale is None else scale, ws if size else None, size)
@@ -733,9 +737,11 @@ def gdn_draft_step(q, k, v, g, beta, S, *, keep=None, flags=0, scale=1.0, cu_seq
         o = torch.empty(v.shape, device=v.device, dtype=io)
     qp, kp, vp, gp, bp, sp, keepp, cu, op = _addresses(dev, (q, k, v, g, beta, S, keep, cu_seqlens, o), _DRAFT_NAMES,
                                                        (io, io, io, _F32, _F32, _F32, _I32, _I32, io))
-    for name, t, shape in (("q", q, k.shape), ("v", v, (B, T, H, dv)), ("g", g, (B, T, H)), ("beta", beta, (B, T, H)),
-                           ("S", S, (n, H, dv, dk)), ("keep", keep, (n,)), ("o", o, v.shape)):
-        _shaped(t, name, shape)
+    if (qp and q.shape != k.shape) or v.shape != (B, T, H, dv) or g.shape != (B, T, H) or beta.shape != g.shape \
+            or S.shape != (n, H, dv, dk) or (keepp and keep.shape != (n,)) or (op and o.shape != v.shape):
+        for name, t, shape in (("q", q, k.shape), ("v", v, (B, T, H, dv)), ("g", g, (B, T, H)), ("beta", beta, (B, T, H)),
+                               ("S", S, (n, H, dv, dk)), ("keep", keep, (n,)), ("o", o, v.shape)):
+            _shaped(t, name, shape)
     _on(dev, lib().gdn_draft_step, qp, kp, vp, gp, bp, sp, op, keepp, B, T, H, HK, dk, dv, cu, n_seqs, _IO[io], float(scale),
         int(flags))
     return o
@@ -791,10 +797,12 @@ def gdn_draft_verify(p, u, *, drafts=None, q=None, draft_lens=None, tokens=None,
                     (_I32, _I32, _F32, _I32, _I32, torch.uint8))
     if at[2] is None:
         raise TypeError("u must be a CUDA (HIP) tensor")
-    for name, t, shape in (("drafts", drafts, (n, m)), ("draft_lens", draft_lens, (n,)), ("u", u, (n, m + 1)),
-                           ("tokens", tokens, (n, m + 1)), ("counts", counts, (n,))):
-        _shaped(t, name, shape)
     dp, lp, up, tp, cp, ws = at
+    if u.shape != (n, m + 1) or tokens.shape != u.shape or counts.shape != (n,) or (dp and drafts.shape != (n, m)) \
+            or (lp and draft_lens.shape != (n,)):
+        for name, t, shape in (("drafts", drafts, (n, m)), ("draft_lens", draft_lens, (n,)), ("u", u, (n, m + 1)),
+                               ("tokens", tokens, (n, m + 1)), ("counts", counts, (n,))):
+            _shaped(t, name, shape)
     size = 0 if ws is None else workspace.numel()
     _on(dev, lib().gdn_draft_verify, pp, qp, dp, lp, up, tp, cp, n, m, V, ps, qs, _IO[p.dtype], ws if size else None, size)
     return tokens, counts

@@ -25,9 +25,9 @@ struct TablesParams {
     int n, rows, shift, n_pages, max_pages;
 };
 
-// Position, and slot or -1, of a token that is the i-th of m new ones of sequence s.
-__device__ __forceinline__ void map_token(const TablesParams& p, int t, int s, int i, int m) {
-    const int pos = max(p.lens[s], 0) - m + i;
+// Position, and slot or -1, of a token that is the i-th of m new ones of sequence s, of L tokens.
+__device__ __forceinline__ void map_token(const TablesParams& p, int t, int s, int i, int m, int L) {
+    const int pos = L - m + i;
     if (p.positions) p.positions[t] = pos;
     if (!p.slots) return;
     int id = -1;
@@ -41,55 +41,78 @@ __device__ __forceinline__ void map_none(const TablesParams& p, int t) {
 
 constexpr int NTA = 1024;   // threads of k_cache_tables, and sequences that it takes at a time
 
+// Inclusive scans over the workgroup of pages given, pages taken and new tokens (running sums held to `rows` < 2^30), in one go.
+__device__ __forceinline__ void scan_three(int (&x)[3], int rows, int (*red)[NTA / 64], int (&all)[3]) {
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    auto sum = [](int a, int b) { return a + b; };
+    auto tokens = [rows](int a, int b) { return min(a + b, rows); };
+    x[0] = wave_scan(x[0], sum);
+    x[1] = wave_scan(x[1], sum);
+    x[2] = wave_scan(x[2], tokens);
+    __syncthreads();   // (red is free)
+    if (lane == 63)
+#pragma unroll
+        for (int k = 0; k < 3; ++k) red[k][wave] = x[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        int y = lane < NTA / 64 ? red[k][lane] : 0;
+        y = k < 2 ? wave_scan(y, sum) : wave_scan(y, tokens);
+        all[k] = __builtin_amdgcn_readlane(y, NTA / 64 - 1);
+        const int before = __builtin_amdgcn_readlane(y, max(__builtin_amdgcn_readfirstlane(wave) - 1, 0));
+        if (wave > 0) x[k] = k < 2 ? sum(x[k], before) : tokens(x[k], before);
+    }
+}
+
 // maps: the positions and slots too (at most NTA sequences).
 __global__ __launch_bounds__(NTA) void k_cache_tables(TablesParams p, int maps) {
-    __shared__ int ends[NTA], at[NTA], cu_ends[NTA];   // running sums of pages moved, where they stand in a sequence's row; token offsets
-    __shared__ int red[NTA / 64];
-    const int tid = threadIdx.x, page = 1 << p.shift;
-    auto sum = [](int a, int b) { return a + b; };
-    const int rows = p.rows;
-    auto tokens = [rows](int a, int b) { return min(a + b, rows); };   // (rows < 2^30)
+    __shared__ int ends[NTA], at[NTA];   // running sums of pages moved, and where they stand in a sequence's row
+    __shared__ int cu_ends[NTA], lens[NTA];   // maps: token offsets and lengths
+    __shared__ int red[3][NTA / 64];
+    const int tid = threadIdx.x, page = 1 << p.shift, rows = p.rows;
     const int have = min(max(p.n_free[0], 0), p.n_pages);
-    int held, target;   // of sequence base + tid
-    auto load = [&](int i) {
+    int held, target, give_end, take_end;   // of sequence base + tid; running sums of its pages given and taken
+    // Sums over the sequences [base, base + NTA) (they stay below 2^31: n max_pages does), offsets of their tokens from `token` on.
+    int sums[3], token = 0;
+    auto load = [&](int base, bool tokens) {
+        const int i = base + tid;
         held = target = 0;
-        if (i >= p.n) return;
-        held = min(max(p.held[i], 0), p.max_pages);
-        const int len = max(p.lens[i], 0);
-        target = min((int)(((long)len + page - 1) >> p.shift), p.max_pages);
-        if (p.shared) target = max(target, min(p.shared[i], held));
+        int fresh = 0;
+        if (i < p.n) {
+            held = min(max(p.held[i], 0), p.max_pages);
+            const int len = max(p.lens[i], 0);
+            if (p.new_lens && tokens) fresh = min(max(p.new_lens[i], 0), rows);
+            target = min((int)(((long)len + page - 1) >> p.shift), p.max_pages);
+            if (p.shared) target = max(target, min(p.shared[i], held));
+            lens[tid] = len;
+        }
+        int x[3] = {max(held - target, 0), max(target - held, 0), fresh};
+        scan_three(x, rows, red, sums);
+        give_end = x[0];
+        take_end = x[1];
+        if (tokens && i < p.n && p.cu) p.cu[i + 1] = cu_ends[tid] = p.new_lens ? min(token + x[2], rows) : (i + 1) * (rows / p.n);
+        token = min(token + sums[2], rows);
     };
-    // pages given back (their sums stay below 2^31: n max_pages does)
-    int given = 0, wanted = 0, token = 0, all;
+    // pages given back
+    int given = 0, wanted = 0;
     for (int base = 0; base < p.n; base += NTA) {
-        const int i = base + tid, m = min(p.n - base, NTA);
-        load(i);
-        const int give = max(held - target, 0), y = wg_scan<NTA / 64>(give, sum, red, all);
-        ends[tid] = y;
-        at[tid] = target - (y - give);
-        const int total = all;
-        wg_scan<NTA / 64>(max(target - held, 0), sum, red, all);
-        wanted += all;
-        if (p.new_lens) {
-            const int e = tokens(token, wg_scan<NTA / 64>(i < p.n ? min(max(p.new_lens[i], 0), rows) : 0, tokens, red, all));
-            if (i < p.n) {
-                cu_ends[tid] = e;
-                p.cu[i + 1] = e;
+        const int m = min(p.n - base, NTA);
+        load(base, true);
+        wanted += sums[1];
+        if (sums[0] > 0) {
+            ends[tid] = give_end;
+            at[tid] = target - (give_end - max(held - target, 0));
+            __syncthreads();
+            for (int x = tid; x < sums[0]; x += NTA) {
+                const int s = first_past(ends, m, x);
+                int32_t* entry = p.table + (long)(base + s) * p.max_pages + at[s] + x;
+                const int to = have + given + x;
+                if (to < p.n_pages) p.free[to] = *entry;
+                *entry = -1;
             }
-            token = tokens(token, all);
-        } else if (i < p.n && p.cu) {
-            p.cu[i + 1] = (i + 1) * (rows / p.n);
+            given += sums[0];
+            __syncthreads();
         }
-        __syncthreads();
-        for (int x = tid; x < total; x += NTA) {
-            const int s = first_past(ends, m, x);
-            int32_t* entry = p.table + (long)(base + s) * p.max_pages + at[s] + x;
-            const int to = have + given + x;
-            if (to < p.n_pages) p.free[to] = *entry;
-            *entry = -1;
-        }
-        given += total;
-        __syncthreads();
     }
     if (tid == 0 && p.cu) p.cu[0] = 0;
     const int pool = min(have + given, p.n_pages), got = min(wanted, pool);
@@ -97,29 +120,31 @@ __global__ __launch_bounds__(NTA) void k_cache_tables(TablesParams p, int maps) 
     int taken = 0;
     for (int base = 0; base < p.n; base += NTA) {
         const int i = base + tid, m = min(p.n - base, NTA);
-        if (p.n > NTA) load(i);
-        const int take = max(target - held, 0), y = wg_scan<NTA / 64>(take, sum, red, all);
-        ends[tid] = y;
-        at[tid] = held - (y - take);
-        if (i < p.n) p.held[i] = min(held, target) + min(max(got - taken - (y - take), 0), take);
-        const int total = all;
-        __syncthreads();
-        for (int x = tid; x < total; x += NTA) {
-            const int s = first_past(ends, m, x);
-            p.table[(long)(base + s) * p.max_pages + at[s] + x] = taken + x < got ? p.free[pool - got + taken + x] : -1;
+        if (p.n > NTA) load(base, false);
+        const int take = max(target - held, 0);
+        if (i < p.n) p.held[i] = min(held, target) + min(max(got - taken - (take_end - take), 0), take);
+        if (sums[1] > 0) {
+            ends[tid] = take_end;
+            at[tid] = held - (take_end - take);
+            __syncthreads();
+            for (int x = tid; x < sums[1]; x += NTA) {
+                const int s = first_past(ends, m, x);
+                p.table[(long)(base + s) * p.max_pages + at[s] + x] = taken + x < got ? p.free[pool - got + taken + x] : -1;
+            }
+            taken += sums[1];
+            __syncthreads();
         }
-        taken += total;
-        __syncthreads();
     }
     if (tid == 0) {
         p.n_free[0] = pool - got;
         if (p.missing) p.missing[0] = wanted - got;
     }
     if (!maps) return;
+    __syncthreads();
     const int T = rows / p.n;
     for (int t = tid; t < rows; t += NTA) {
         if (!p.new_lens) {
-            map_token(p, t, t / T, t % T, T);
+            map_token(p, t, t / T, t % T, T, lens[t / T]);
             continue;
         }
         const int s = first_past(cu_ends, p.n, t);
@@ -127,7 +152,7 @@ __global__ __launch_bounds__(NTA) void k_cache_tables(TablesParams p, int maps) 
             map_none(p, t);
         } else {
             const int beg = s > 0 ? cu_ends[s - 1] : 0;
-            map_token(p, t, s, t - beg, cu_ends[s] - beg);
+            map_token(p, t, s, t - beg, cu_ends[s] - beg, lens[s]);
         }
     }
 }
@@ -138,7 +163,7 @@ __global__ __launch_bounds__(NT) void k_cache_maps(TablesParams p) {
     if (t >= p.rows) return;
     if (!p.new_lens) {
         const int T = p.rows / p.n;
-        map_token(p, t, t / T, t % T, T);
+        map_token(p, t, t / T, t % T, T, max(p.lens[t / T], 0));
         return;
     }
     const int s = first_past(p.cu + 1, p.n, t);
@@ -147,7 +172,7 @@ __global__ __launch_bounds__(NT) void k_cache_maps(TablesParams p) {
         return;
     }
     const int beg = p.cu[s];
-    map_token(p, t, s, t - beg, p.cu[s + 1] - beg);
+    map_token(p, t, s, t - beg, p.cu[s + 1] - beg, max(p.lens[s], 0));
 }
 
 // ------------------------------------------------------------------ k_draft_step
