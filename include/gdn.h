@@ -523,7 +523,7 @@ gdn_status gdn_attention_paged(const void* q, const void* k_cache, const void* v
  *   block_table [n, max_pages], held [n], free_pages [n_pages], n_free [1]  int32, updated IN PLACE
  *               (held and n_free outside [0, max_pages], [0, n_pages] count as the nearest)
  *   shared      [n] int32, or NULL (none);  missing [1] int32, written, or NULL
- *   page, n_pages, max_pages  as gdn_kv_append; n * max_pages below 2^31
+ *   page, n_pages, max_pages  as gdn_kv_append; n_pages and n * max_pages below 2^30
  * For the rows of a step (all optional, with the tables as updated):
  *   rows        tokens of the call, B * T of the layers' entry points
  *   new_lens    [n] int32: the new tokens of each sequence, packed behind one another (a padded batch:

@@ -405,14 +405,17 @@ constexpr int VS = 1024;
 
 __device__ __forceinline__ float probability(float x) { return __builtin_amdgcn_classf(x, 0x180) ? x : 0.f; }   // (positive, finite)
 
-// The number of accepted drafts of sequence s, and of its drafts, by a whole wave.
+// The number of accepted drafts of sequence s, and of its drafts, by a whole wave.  (All m are looked up, so that their number
+// comes with them and not before.)
 template <typename IO> __device__ __forceinline__ int accepted(const VerifyParams& p, int s, int& len) {
     const int lane = threadIdx.x & 63;
-    len = p.lens ? min(max(tab(p.lens, s), 0), p.m) : p.m;
-    for (int base = 0; base < len; base += 64) {
+    len = p.m;
+    if (p.lens) len = p.lens[s];
+    int first = p.m;
+    for (int base = 0; base < p.m && first == p.m; base += 64) {
         const int j = base + lane;
         bool ok = true;
-        if (j < len) {
+        if (j < p.m) {
             const int x = p.drafts[(long)s * p.m + j];
             ok = false;
             if (x >= 0 && x < p.V) {
@@ -422,9 +425,10 @@ template <typename IO> __device__ __forceinline__ int accepted(const VerifyParam
             }
         }
         const uint64_t no = __builtin_amdgcn_ballot_w64(!ok);
-        if (no) return base + __builtin_ctzll(no);
+        if (no) first = base + __builtin_ctzll(no);
     }
-    return len;
+    len = __builtin_amdgcn_readfirstlane(min(max(len, 0), p.m));
+    return min(first, len);
 }
 
 // w of a row's entries: of row a of the target, less row a of the drafts'.
@@ -480,28 +484,6 @@ template <typename IO, int N, int STEP> __device__ __forceinline__ void rest(con
 }
 
 constexpr int VE = VS / 64 / 4;   // groups of 4 tokens of a lane
-
-// Inclusive sums over the wave's lanes, as wave_scan takes them: always in the same order.
-template <int CTRL, int ROWS> __device__ __forceinline__ double dpp64(double x) {
-    const uint64_t u = __builtin_bit_cast(uint64_t, x);
-    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, ROWS, 0xf, false);
-    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, ROWS, 0xf, false);
-    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-}
-__device__ __forceinline__ double scan64(double x) {
-    x += dpp64<0x111, 0xf>(x);
-    x += dpp64<0x112, 0xf>(x);
-    x += dpp64<0x114, 0xf>(x);
-    x += dpp64<0x118, 0xf>(x);
-    x += dpp64<0x142, 0xa>(x);
-    x += dpp64<0x143, 0xc>(x);
-    return x;
-}
-__device__ __forceinline__ double lane64(double x, int l) {
-    const uint64_t u = __builtin_bit_cast(uint64_t, x);
-    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)u, l), hi = __builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), l);
-    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-}
 
 // The sum of w over a slice, by a wave, in every lane.
 template <typename IO> __device__ __forceinline__ double slice_sum(const Rest<IO>& r, int slice, int V) {

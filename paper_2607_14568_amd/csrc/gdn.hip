@@ -3264,6 +3264,8 @@ SharedPlan shared_plan(int B, int T, int H, int H_kv, int page, int max_pages, i
     const long G = H / H_kv, n = n_seqs > 0 ? n_seqs : B, tokens = (long)B * T, rows = tokens * G;
     const long units = ((long)page * max_pages + UNIT - 1) / UNIT;
     p.round = (int)std::max(1L, 2 * PLAN_CUS / H_kv);   // two workgroups per CU
+    // Blocks of 16 rows where a group, and a sequence, has few on average (see paged_plan); a sequence's rows are in a block of
+    // 128 only where its group's are.
     p.rbp = rows <= 32L * groups ? 16 : AQ;
     p.rbt = rows <= 64 * n ? 16 : AQ;
     const long blocks_p = rows / p.rbp + std::min<long>(groups, tokens);
@@ -4095,7 +4097,8 @@ extern "C" gdn_status gdn_cache_tables(const int32_t* seq_lens, const int32_t* n
         return fail(GDN_ERR_INVALID_ARG, "page=%d n_pages=%d max_pages=%d must be positive", page, n_pages, max_pages);
     if (!page_known(page)) return fail(GDN_ERR_UNSUPPORTED, "page=%d: only 16, 32, 64 and 128 are implemented", page);
     if (!table_fits(page, max_pages)) return fail(GDN_ERR_UNSUPPORTED, "max_pages=%d too large", max_pages);
-    if ((long)n * max_pages >= 1L << 31 || rows >= 1 << 30) return fail(GDN_ERR_UNSUPPORTED, "n*max_pages or rows=%d too large", rows);
+    if ((long)n * max_pages >= 1L << 30 || n_pages >= 1 << 30 || rows >= 1 << 30)   // (sums of two stay below 2^31)
+        return fail(GDN_ERR_UNSUPPORTED, "n*max_pages=%ld, n_pages=%d or rows=%d too large", (long)n * max_pages, n_pages, rows);
     if (!seq_lens || !block_table || !held || !free_pages || !n_free)
         return fail(GDN_ERR_INVALID_ARG, "seq_lens, block_table, held, free_pages and n_free must be non-null");
     if (new_lens && !cu_seqlens) return fail(GDN_ERR_INVALID_ARG, "new_lens needs cu_seqlens");
@@ -4119,14 +4122,14 @@ extern "C" gdn_status gdn_cache_tables(const int32_t* seq_lens, const int32_t* n
     return launched();
 }
 
-// Sequences that gdn_attention_shared takes in one call.
-static bool batch_fits(int B, int n_seqs) { return (n_seqs > 0 ? n_seqs : B) <= SHARED_SEQS; }
+// Sequences and tokens that gdn_attention_shared takes in one call (a prefix's keys, up to 2^30, and tokens stay below 2^31).
+static bool batch_fits(int B, int T, int n_seqs) { return (n_seqs > 0 ? n_seqs : B) <= SHARED_SEQS && (long)B * T < 1L << 29; }
 
 extern "C" size_t gdn_attention_shared_workspace_bytes(int B, int T, int H, int H_kv, int d, int page, int max_pages, int n_seqs,
                                                        int n_groups) {
     if (B < 1 || T < 1 || H < 1 || H_kv < 1 || H % H_kv || !head_size_known(d) || n_seqs < 0 || (n_seqs > 0 && B != 1) ||
         !heads_fit(H, d) || !rows_fit(B, T, H) || !page_known(page) || max_pages < 1 || !table_fits(page, max_pages) ||
-        !batch_fits(B, n_seqs) || n_groups < 1 || n_groups > (n_seqs > 0 ? n_seqs : B))
+        !batch_fits(B, T, n_seqs) || n_groups < 1 || n_groups > (n_seqs > 0 ? n_seqs : B))
         return 0;
     return shared_layout(shared_plan(B, T, H, H_kv, page, max_pages, n_seqs, n_groups), n_seqs > 0 ? n_seqs : B, n_groups, H_kv, d).total;
 }
@@ -4151,7 +4154,8 @@ extern "C" gdn_status gdn_attention_shared(const void* q, const void* k_cache, c
     if (!aligned(prefix_lens, 4) || !aligned(cu_groups, 4))
         return fail(GDN_ERR_INVALID_ARG, "prefix_lens or cu_groups is not 4-byte aligned");
     if (io_dtype != GDN_BF16) return fail(GDN_ERR_UNSUPPORTED, "attention is implemented for bf16 io only");
-    if (!batch_fits(B, n_seqs)) return fail(GDN_ERR_UNSUPPORTED, "%d sequences: at most %d are implemented", n, SHARED_SEQS);
+    if (!batch_fits(B, T, n_seqs))
+        return fail(GDN_ERR_UNSUPPORTED, "%d sequences (at most %d are implemented) or B*T=%ld too large", n, SHARED_SEQS, (long)B * T);
     if (T == 0) return GDN_OK;
     if (!q || !o) return fail(GDN_ERR_INVALID_ARG, "q and o must be non-null");
     if (!aligned(q, 16) || !aligned(o, 16)) return fail(GDN_ERR_INVALID_ARG, "q or o is not 16-byte aligned");

@@ -13,6 +13,28 @@
 // A sequence that does not reach behind its group's prefix (a finished one, one that does not belong) takes no part in it and
 // attends all its keys by itself.
 
+// Inclusive sums over the wave's lanes, as wave_scan takes them: always in the same order.
+template <int CTRL, int ROWS> __device__ __forceinline__ double dpp64(double x) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, ROWS, 0xf, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, ROWS, 0xf, false);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double scan64(double x) {
+    x += dpp64<0x111, 0xf>(x);
+    x += dpp64<0x112, 0xf>(x);
+    x += dpp64<0x114, 0xf>(x);
+    x += dpp64<0x118, 0xf>(x);
+    x += dpp64<0x142, 0xa>(x);
+    x += dpp64<0x143, 0xc>(x);
+    return x;
+}
+__device__ __forceinline__ double lane64(double x, int l) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)u, l), hi = __builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), l);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
 struct SharedParams : PagedParams {
     const int32_t* prefix;    // [groups] tokens that a group's sequences share
     const int32_t* cu_groups; // [groups + 1] offsets of the groups among the sequences; null: one group
@@ -53,8 +75,6 @@ struct Parts {
     __device__ __forceinline__ int items() const { return blocks * ceil_div(units, c, 1.f / (float)c); }
     __device__ __forceinline__ int gitems() const { return gblocks * ceil_div(gunits, c, 1.f / (float)c); }
 };
-__device__ __forceinline__ double scan64(double x);
-__device__ __forceinline__ double lane64(double x, int l);
 __device__ __forceinline__ Parts parts64(const SharedParams& p) {
     const int lane = threadIdx.x & 63, n = p.s.n, groups = p.groups, cap = p.c.max_pages << p.c.shift;
     Parts q;
@@ -167,6 +187,12 @@ __device__ __forceinline__ void write_notes(const SharedParams& p, const SharedN
 
 // ------------------------------------------------------------------ k_attn_shared
 // FORM: both parts by blocks of 16 rows; the prefixes by blocks of 128; both by blocks of 128.
+// One launch, so that the sequences' keys, which memory bounds, are read beside the prefixes' products: two launches one after the
+// other took 21.5 and 35.4 us, this one 45, for 64 sequences behind 8192 tokens with 64 to 2000 of their own (179 MB, 4.0 TB/s;
+// 16 heads over 8, as below).  A prefix is bound by the tile's steps, not by memory: 65536 tokens in e4m3 under 48 sequences, 151 MB,
+// 61 us; 2.85 us for two workgroups' blocks of 64 keys on a CU, of which products, exponentials, loads and conversions are 1.3 to 8
+// of the 61 us each when left out.  Tried there without gain: blocks of 32 keys with loads three and four ahead (70 against 64),
+// tiles shared out over the waves, all of a block's LDS reads ahead of its products (spills), an item's head tied to an XCD.
 template <int DH, typename CT, int FORM>
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_attn_shared(SharedParams g, SharedParams t, int prefix_wgs, SharedNotes notes) {
     if (blockIdx.x == 0 && threadIdx.x < 64 && !g.part) write_notes(t, notes);

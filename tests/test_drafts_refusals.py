@@ -20,7 +20,7 @@ def _tables(**kw):
 
 @pytest.mark.parametrize("kw,code", [
     (dict(n=0), INVALID), (dict(rows=-1), INVALID), (dict(page=0), INVALID), (dict(page=48), UNSUPPORTED), (dict(n_pages=0), INVALID),
-    (dict(max_pages=0), INVALID), (dict(max_pages=1 << 27), UNSUPPORTED), (dict(n=1 << 20, max_pages=1 << 11), UNSUPPORTED),
+    (dict(max_pages=0), INVALID), (dict(max_pages=1 << 27), UNSUPPORTED), (dict(n=1 << 20, max_pages=1 << 10), UNSUPPORTED), (dict(n_pages=1 << 30), UNSUPPORTED),
     (dict(rows=1 << 30), UNSUPPORTED), (dict(lens=None), INVALID), (dict(table=None), INVALID), (dict(held=None), INVALID),
     (dict(free=None), INVALID), (dict(n_free=None), INVALID), (dict(cu=None), INVALID), (dict(new=None), INVALID),
     (dict(new=None, cu=None, pos=None), INVALID), (dict(lens=A + 2), INVALID), (dict(shared=A + 1), INVALID),
@@ -41,7 +41,7 @@ def _shared(**kw):
 @pytest.mark.parametrize("kw,code", SIZES + CACHE + [
     (dict(q=None), INVALID), (dict(qo=None), INVALID), (dict(qo=A + 8), INVALID), (dict(pre=None), INVALID), (dict(pre=A + 2), INVALID),
     (dict(groups=0), INVALID), (dict(groups=3, cg=A), INVALID), (dict(groups=2), INVALID), (dict(cg=A + 2), INVALID),
-    (dict(B=2049), UNSUPPORTED), (dict(cu=A, n=2049, B=1, T=4000), UNSUPPORTED), (dict(ws=None), WORKSPACE), (dict(ws_bytes=100), WORKSPACE),
+    (dict(B=2049), UNSUPPORTED), (dict(T=1 << 28, H=1, Hkv=1), UNSUPPORTED), (dict(cu=A, n=2049, B=1, T=4000), UNSUPPORTED), (dict(ws=None), WORKSPACE), (dict(ws_bytes=100), WORKSPACE),
     (dict(ws=A + 16), INVALID)])
 def test_shared_refuses(kw, code):
     assert _shared(**kw) == code
