@@ -176,10 +176,12 @@ __device__ __forceinline__ void write_notes(const SharedParams& p, const SharedN
     const int lane = threadIdx.x & 63;
     const Parts q = parts64(p);
     const int b = scan_add(q.blocks), x = q.items(), y = scan_add(x), gx = q.gitems(), gy = scan_add(gx), g = min(q.group, 63);
-    SharedNote r = {q.tok, q.n, q.len, q.start, y - x, b - q.blocks, q.c, __shfl(gy - gx, g, 64), __shfl(q.gblocks, g, 64), 0, {0, 0}};
-    r.grow = (q.tok - __shfl(q.gtok, g, 64)) * p.G;
-    if (lane < p.s.n) {
-        to.note[lane] = r;
+    const int gfirst = __shfl(gy - gx, g, 64), gblocks = __shfl(q.gblocks, g, 64), gtok = __shfl(q.gtok, g, 64);
+    if (lane < p.s.n) {   // (three vectors: as one struct it went through scratch memory)
+        int4* at = reinterpret_cast<int4*>(to.note + lane);
+        at[0] = int4{q.tok, q.n, q.len, q.start};
+        at[1] = int4{y - x, b - q.blocks, q.c, gfirst};
+        at[2] = int4{gblocks, (q.tok - gtok) * p.G, 0, 0};
         to.block[lane + 1] = b;
     }
     if (lane == 0) to.block[0] = 0;
@@ -198,7 +200,15 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
     if (blockIdx.x == 0 && threadIdx.x < 64 && !g.part) write_notes(t, notes);
     const bool prefix = (int)blockIdx.x < prefix_wgs;
     const int wg = (int)blockIdx.x - (prefix ? 0 : prefix_wgs);
-    const SharedParams& p = prefix ? g : t;
+    SharedParams p = t;   // (field by field: a choice between the two went through scratch memory)
+    if (prefix) {
+        p.of_prefix = true;
+        p.part = g.part;
+        p.first = g.first;
+        p.parts = g.parts;
+        p.pml = g.pml;
+        p.po = g.po;
+    }
     if constexpr (FORM == 0) {
         __shared__ __align__(16) float out[NT / 64][16 * ROWS_PITCH<DH>];
         __shared__ float2 ml[NT / 64][16];
