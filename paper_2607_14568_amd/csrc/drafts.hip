@@ -9,7 +9,7 @@
 // that what one step took and the next gives back lies in the pool as before).
 // One workgroup: the sums over the sequences and the pool's end hold everything together, and a step moves a few pages a
 // sequence.  Bound by latency: the lengths, the pages given, the pages taken and the slots that need them are loads that
-// wait for one another.
+// wait for one another: 3.5 us for 256 sequences' 5 tokens each, with their maps.
 struct TablesParams {
     const int32_t* lens;
     const int32_t* new_lens;   // null: rows / n each
@@ -157,7 +157,9 @@ __global__ __launch_bounds__(NTA) void k_cache_tables(TablesParams p, int maps) 
     }
 }
 
-// The positions and slots of many tokens, from the tables and offsets that k_cache_tables left.
+// The positions and slots of many tokens, from the tables and offsets that k_cache_tables left: a thread each, bound by latency.
+// Up to 4096 tokens that kernel's workgroup makes them itself, a launch less: 512 of 64 sequences 7.8 us (here 10.1), 2048 of 128
+// 9.0 (10.4), 4096 of 8 9.1 (9.1) or of 256 11.2 (10.9), but 8192 of 8 11.5 (9.1) and 32768 25.8 (9.2).
 __global__ __launch_bounds__(NT) void k_cache_maps(TablesParams p) {
     const int t = (int)blockIdx.x * NT + threadIdx.x;
     if (t >= p.rows) return;
@@ -387,8 +389,13 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void k_
 // draft from w = p of the row after it: the lowest v with w_0 + .. + w_v > u W, sums in 64 bits, so that no rounding of
 // theirs is seen but where u W falls within 2^-50 of a border.  w = p, too, where no w is positive.  Entries that are not
 // positive and finite count as 0.
-// k_verify_sums: waves over slices of VS tokens of the row that is left, a sum of w each; k_verify_pick: the slice that holds
-// u W, then the token in it.  Bound by the two rows' bytes.
+// k_verify_sums: a wave for each slice of VS tokens of the row that is left, their sum of w; k_verify_pick: the slice that holds
+// u W, then the token in it.  Bound by the two rows' bytes: 64 sequences, rows of 131072 floats (67 MB), 12.0 and 4.0 us (5.6 TB/s);
+// small calls by latency (drafts, their probabilities, the rows, the sums wait for one another): 3.7 and 2.8 for one of 50000.
+// Waves that take several slices of a sequence, one after another, so that 24 (12) a CU are all there are, look the drafts up
+// less often but wait longer: 96 rows of 100003 floats 16.8 (17.5) us a call against 16.4 of one each, 64 of 131072 in bf16 15.3 (17.7)
+// against 13.2.  Slices of 512: 12.7 us for 96 rows of 100003 in bf16 (11.3 of 1024), 16.8 (16.3) of two in floats, but 5.8 (6.2) for
+// one sequence; of 2048, 16.4 against 12.8 before the last step.
 struct VerifyParams {
     const void* p;            // [n][m + 1][..], ps elements a row
     const void* q;            // [n][m][..], qs elements a row, or null: 1 for the drafted token
@@ -405,8 +412,8 @@ constexpr int VS = 1024;
 
 __device__ __forceinline__ float probability(float x) { return __builtin_amdgcn_classf(x, 0x180) ? x : 0.f; }   // (positive, finite)
 
-// The number of accepted drafts of sequence s, and of its drafts, by a whole wave.  (All m are looked up, so that their number
-// comes with them and not before.)
+// The number of accepted drafts of sequence s, and of its drafts, by a whole wave.  (All m are looked up, also those past the sequence's number of
+// drafts, so that it is loaded along with them and not ahead of them.)
 template <typename IO> __device__ __forceinline__ int accepted(const VerifyParams& p, int s, int& len) {
     const int lane = threadIdx.x & 63;
     len = p.m;
@@ -445,36 +452,42 @@ template <typename IO> __device__ __forceinline__ Rest<IO> rest_of(const VerifyP
     return r;
 }
 
-// w of tokens v0 + STEP i + e, i < N, e < 4 (0 from `end` on), all loads sent off before the first is used.
-template <typename IO, int N, int STEP> __device__ __forceinline__ void rest(const Rest<IO>& r, int v0, int end, double (&w)[N][4]) {
-    auto load = [&](const IO* src, floatx4 (&x)[N]) {
+// w of tokens v0 + STEP i + e, i < N, e < 4 (0 from `end` on; whole: the wave has none there), all loads sent off before the first
+// is used: without a branch between them, whose end would wait for what it has to convert (96 rows of 100003 in bf16 11.3 us a call,
+// with a branch at every group of 4 12.8; less a second row 13.6 and 16.6).
+template <typename IO, int N, int STEP> __device__ __forceinline__ void rest(const Rest<IO>& r, int v0, int end, bool whole, double (&w)[N][4]) {
+    auto all = [&](auto WHOLE, auto LESS) {
+        floatx4 x[N], y[N];
+        auto load = [&](const IO* src, floatx4 (&z)[N]) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int v = v0 + STEP * i;
-            x[i] = floatx4{0.f, 0.f, 0.f, 0.f};
-            if (v + 4 <= end) {
-                x[i] = four(src + v);
-            } else {
+            for (int i = 0; i < N; ++i) {
+                const int v = v0 + STEP * i;
+                if constexpr (decltype(WHOLE)::value) {
+                    z[i] = four(src + v);
+                } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (v + e < end) x[i][e] = to_f(src[v + e]);
+                    for (int e = 0; e < 4; ++e) {
+                        const float one = to_f(src[min(v + e, end - 1)]);
+                        z[i][e] = v + e < end ? one : 0.f;
+                    }
+                }
             }
-        }
-    };
-    floatx4 x[N], y[N];
-    load(r.p, x);
-    if (r.q) {
-        load(r.q, y);
+        };
+        load(r.p, x);
+        if constexpr (decltype(LESS)::value) load(r.q, y);
 #pragma unroll
         for (int i = 0; i < N; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[i][e] = fmax((double)probability(x[i][e]) - (double)probability(y[i][e]), 0.);
+            for (int e = 0; e < 4; ++e) {
+                w[i][e] = probability(x[i][e]);
+                if constexpr (decltype(LESS)::value) w[i][e] = fmax(w[i][e] - (double)probability(y[i][e]), 0.);
+            }
+    };
+    if (r.q) {
+        if (whole) all(Ic<1>{}, Ic<1>{}); else all(Ic<0>{}, Ic<1>{});
         return;
     }
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[i][e] = probability(x[i][e]);
+    if (whole) all(Ic<1>{}, Ic<0>{}); else all(Ic<0>{}, Ic<0>{});
     if (__builtin_amdgcn_ballot_w64(r.certain >= v0 && r.certain < v0 + STEP * (N - 1) + 4))
 #pragma unroll
         for (int i = 0; i < N; ++i)
@@ -489,7 +502,7 @@ constexpr int VE = VS / 64 / 4;   // groups of 4 tokens of a lane
 template <typename IO> __device__ __forceinline__ double slice_sum(const Rest<IO>& r, int slice, int V) {
     const int lane = threadIdx.x & 63, first = slice * VS;
     double w[VE][4], sum = 0.;
-    rest<IO, VE, 256>(r, first + 4 * lane, min(first + VS, V), w);
+    rest<IO, VE, 256>(r, first + 4 * lane, V, first + VS <= V, w);
 #pragma unroll
     for (int i = 0; i < VE; ++i) sum += (w[i][0] + w[i][1]) + (w[i][2] + w[i][3]);
     return lane64(scan64(sum), 63);
@@ -502,9 +515,9 @@ __global__ __launch_bounds__(NT) void k_verify_sums(VerifyParams p) {
     int len;
     const int a = accepted<IO>(p, s, len);
     const Rest<IO> r = rest_of<IO>(p, s, a, len);
-    for (int i = w; i < p.slices; i += p.groups * (NT / 64)) {
-        const double sum = slice_sum(r, i, p.V);
-        if ((threadIdx.x & 63) == 0) p.part[(long)s * p.slices + i] = sum;
+    if (w < p.slices) {
+        const double sum = slice_sum(r, w, p.V);
+        if ((threadIdx.x & 63) == 0) p.part[(long)s * p.slices + w] = sum;
     }
     if (w == 0 && threadIdx.x == 0) p.counts[s] = a + 1;
 }
@@ -555,7 +568,7 @@ __global__ __launch_bounds__(NT) void k_verify_pick(VerifyParams p) {
         slice = __builtin_amdgcn_readfirstlane(slice);
         const int first = slice * VS, v0 = first + 4 * VE * lane;
         double w[VE][4];
-        rest<IO, VE, 4>(r, v0, min(first + VS, p.V), w);
+        rest<IO, VE, 4>(r, v0, p.V, first + VS <= p.V, w);
         sum = 0.;
 #pragma unroll
         for (int i = 0; i < VE; ++i)

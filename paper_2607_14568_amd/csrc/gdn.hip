@@ -3264,8 +3264,10 @@ SharedPlan shared_plan(int B, int T, int H, int H_kv, int page, int max_pages, i
     const long G = H / H_kv, n = n_seqs > 0 ? n_seqs : B, tokens = (long)B * T, rows = tokens * G;
     const long units = ((long)page * max_pages + UNIT - 1) / UNIT;
     p.round = (int)std::max(1L, 2 * PLAN_CUS / H_kv);   // two workgroups per CU
-    // Blocks of 16 rows where a group, and a sequence, has few on average (see paged_plan); a sequence's rows are in a block of
-    // 128 only where its group's are.
+    // Blocks of 16 rows where a group, and a sequence, has few on average; a sequence's rows are in a block of 128 only where its
+    // group's are.  Measured by 16 and by 128 (16 heads over 8, bf16): prefixes, 32 rows behind 1000 tokens 13.2 and 16.3 us a
+    // call, behind 8192 19.2 and 18.7, in 4 groups 53.6 and 46.5; 64 rows 16.7 and 19.3, 26.0 and 21.5, 79.3 and 56.5.  Own keys,
+    // 500 to 2000 of 8 sequences: 64 rows 36.6 and 45.0 us, 128 rows 59.1 and 57.2; of 32: 110 and 106, 185 and 153.
     p.rbp = rows <= 32L * groups ? 16 : AQ;
     p.rbt = rows <= 64 * n ? 16 : AQ;
     const long blocks_p = rows / p.rbp + std::min<long>(groups, tokens);
@@ -3308,7 +3310,7 @@ void launch_shared(const SharedSetup& setup, const SharedJoin& j, const SharedPl
     if (plan.rbp == 16) hipLaunchKernelGGL((k_attn_shared<DH, CT, 0>), grid, dim3(NT), 0, st, j.g, j.t, prefix_wgs, j.notes);
     else if (plan.rbt == 16) hipLaunchKernelGGL((k_attn_shared<DH, CT, 1>), grid, dim3(NT), 0, st, j.g, j.t, prefix_wgs, j.notes);
     else hipLaunchKernelGGL((k_attn_shared<DH, CT, 2>), grid, dim3(NT), 0, st, j.g, j.t, prefix_wgs, j.notes);
-    // A workgroup a row while they are all resident at once, a wave a row where there are more of them
+    // A workgroup a row while they are all resident at once, a wave a row where there are more of them (measured at k_shared_join)
     const unsigned blocks = (unsigned)(plan.blocks_t * j.t.HKV), rows = (unsigned)plan.rows_t;
     if ((long)blocks * rows <= 4 * PLAN_CUS) hipLaunchKernelGGL((k_shared_join<DH, false>), dim3(blocks, rows), dim3(NT), 0, st, j);
     else hipLaunchKernelGGL((k_shared_join<DH, true>), dim3(blocks, (rows + NT / 64 - 1) / (NT / 64)), dim3(NT), 0, st, j);
@@ -4114,7 +4116,7 @@ extern "C" gdn_status gdn_cache_tables(const int32_t* seq_lens, const int32_t* n
     p.cu = cu_seqlens; p.positions = positions; p.slots = slots;
     p.n = n; p.rows = rows; p.n_pages = n_pages; p.max_pages = max_pages;
     p.shift = page == 16 ? 4 : page == 32 ? 5 : page == 64 ? 6 : 7;
-    const bool maps = rows > 0 && (positions || slots), here = maps && n <= NTA && rows <= 8 * NTA;
+    const bool maps = rows > 0 && (positions || slots), here = maps && n <= NTA && rows <= 4 * NTA;   // (measured at k_cache_maps)
     hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
     (void)hipGetLastError();
     hipLaunchKernelGGL(k_cache_tables, dim3(1), dim3(NTA), 0, hs, p, here ? 1 : 0);
@@ -4178,7 +4180,6 @@ extern "C" gdn_status gdn_attention_shared(const void* q, const void* k_cache, c
     p.c = make_cache(k_cache, v_cache, k_scale, v_scale, block_table, page, n_pages, max_pages);
     p.prefix = prefix_lens; p.cu_groups = cu_groups; p.groups = n_groups;
     p.rbp = plan.rbp; p.rbt = plan.rbt; p.round = plan.round;
-    p.least = plan.rbp == 16 ? 1 : 2;   // (a tile's chunk of fewer keys is mostly joining)
     SharedSetup u = {};
     u.p = p;
     u.grp = reinterpret_cast<int4*>(ws + lay.grp); u.seq = reinterpret_cast<int4*>(ws + lay.seq);
@@ -4286,8 +4287,7 @@ extern "C" gdn_status gdn_draft_verify(const void* p, const void* q, const int32
     a.part = static_cast<double*>(workspace);
     a.ps = (long)p_stride; a.qs = (long)q_stride;
     a.m = m; a.V = V; a.slices = (V + VS - 1) / VS;
-    const long per = ((long)n * a.slices + 24 * PLAN_CUS - 1) / (24 * PLAN_CUS);   // slices a wave, of 24 waves a CU
-    a.groups = (int)((a.slices + NT / 64 * per - 1) / (NT / 64 * per));
+    a.groups = (a.slices + NT / 64 - 1) / (NT / 64);
     hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
     (void)hipGetLastError();
     if (dtype == GDN_BF16) launch_verify<bf16_t>(a, n, hs);

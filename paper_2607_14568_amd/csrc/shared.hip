@@ -6,7 +6,8 @@
 // The rows of all the group's new tokens attend the prefix together (each sees all of it, so no key is masked), which reads
 // it once for the group, and every sequence's rows attend its own keys behind it.  So one call takes
 //   k_shared_setup   more than 64 sequences: the parts, groups and sequences with their keys, chunks and items, from the lengths on
-//                    the device (fewer: every wave of the next one does so by itself)
+//                    the device (up to 64, a lane each, every wave of the next one does so by itself: 8, 32 and 64 sequences
+//                    take 19.0, 34.3 and 52.5 us so, 21.9, 37.0 and 55.5 with this kernel)
 //   k_attn_shared    the items, of the groups' prefixes (first in the grid) and of the sequences' own keys, by the workgroups of
 //                    k_attn_rows and k_attn_tile
 //   k_shared_join    every row's partial sums added up in order
@@ -39,8 +40,7 @@ struct SharedParams : PagedParams {
     const int32_t* prefix;    // [groups] tokens that a group's sequences share
     const int32_t* cu_groups; // [groups + 1] offsets of the groups among the sequences; null: one group
     int groups;
-    int rbp, rbt;             // rows per block of the prefixes and of the sequences' own keys
-    int least;                // units of a chunk at least (round: items at once, of both)
+    int rbp, rbt;             // rows per block of the prefixes and of the sequences' own keys (round: items at once, of both)
     // The parts as k_shared_setup left them, or null: up to 64 sequences, whose parts every wave works out by itself.
     const int4* part;         // groups {first token, tokens, P, a sequence that shares}, or sequences {first token, tokens, length, start}
     const int32_t* first;     // [parts + 1] items of one key/value head ahead of each part's
@@ -54,7 +54,7 @@ struct SharedParams : PagedParams {
 // sequences, start as others end.  (A c that makes at most `round` items leaves too few of the long ones where there are many
 // short: 32 sequences behind 65536 tokens, e4m3, 76.8 us against 57.7.  A prefix's unit counted as two of a sequence's,
 // since its 128 rows take longer: 55 against 52.4 for 64 sequences behind 8192.)
-__device__ __forceinline__ int chunk_units(double all, int round, int least) { return max((int)min(ceil(all / round), 0x1p23), least); }
+__device__ __forceinline__ int chunk_units(double all, int round) { return max((int)min(ceil(all / round), 0x1p23), 1); }
 
 // What k_shared_join takes of a sequence, and where its row blocks begin (of one key/value head).
 struct SharedNote {
@@ -105,7 +105,7 @@ __device__ __forceinline__ Parts parts64(const SharedParams& p) {
     q.gblocks = q.gseq >= 0 ? (q.gn * p.G + p.rbp - 1) / p.rbp : 0;
     q.gunits = (q.gkeys + UNIT - 1) / UNIT;
     const double all = lane64(scan64((double)q.blocks * q.units + (double)q.gblocks * q.gunits), 63);
-    q.c = __builtin_amdgcn_readfirstlane(chunk_units(all, p.round, p.least));
+    q.c = __builtin_amdgcn_readfirstlane(chunk_units(all, p.round));
     return q;
 }
 
@@ -229,7 +229,8 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
 }
 
 // ------------------------------------------------------------------ k_shared_setup
-// One workgroup works out the parts of more than 64 sequences, for all.  Bound by latency.
+// One workgroup works out the parts of more than 64 sequences, for all.  Bound by latency: 3 us more a call (see above), since the
+// lengths come from the device and every later wave waits for them.
 constexpr int SHARED_SEQS = 2048;   // sequences of a call
 
 struct SharedSetup {
@@ -327,7 +328,7 @@ __global__ __launch_bounds__(NT) void k_shared_setup(SharedSetup u) {
     __syncthreads();
     double total = 0.;
     for (int i = lane; i < groups + n; i += 64) total += (double)work[i].x * work[i].y;
-    const int c = chunk_units(lane64(scan64(total), 63), p.round, p.least);
+    const int c = chunk_units(lane64(scan64(total), 63), p.round);
     const float rc = 1.f / (float)c;
     if (tid == 0) {
         u.chunk[0] = c;
@@ -369,7 +370,10 @@ __global__ __launch_bounds__(NT) void k_shared_setup(SharedSetup u) {
 // ------------------------------------------------------------------ k_shared_join
 // One workgroup per row (or, WAVE, one wave: blockIdx.y holds NT / 64 of them) of a row block of the sequences' own keys and
 // key/value head: the block's chunks, then those of the prefix, as k_attn_join adds them up.  Bound by latency: the block's
-// sequence, its numbers, the partial sums.
+// sequence, its numbers, the partial sums.  Rows that a workgroup each has resident at once are best split over its waves where
+// a long prefix left each many partial sums (32, 64 and 128 rows behind 30000 tokens: 21.1, 21.9 and 21.3 us a call against 38.9,
+// 31.2 and 30.8 with a wave a row; behind 1000 alike); more rows are best a wave each (4608 rows: 7.5 us, with a workgroup 12.2).
+// With twice the loads of a wave at once, 16 a lane, those take 8.6.
 struct SharedJoin {
     SharedParams t;           // the sequences' own keys, and their partial sums
     SharedParams g;           // the groups' prefixes

@@ -77,7 +77,7 @@ def test_tables_take_and_give_back_restores_the_pool():
     assert after[3] == state[3] and (after[2][:after[3]] == state[2][:state[3]]).all()
 
 
-@pytest.mark.parametrize("n,rows", [(3, 9000), (1100, 3000), (2500, 20000), (4, 8192), (4, 8193)])
+@pytest.mark.parametrize("n,rows", [(3, 9000), (1100, 3000), (2500, 20000), (4, 8192), (4, 8193), (4, 4096), (4, 4097)])
 def test_tables_many(n, rows):
     """Sequences past one round of the workgroup's threads, rows past the launch that takes both."""
     print("case: tables many", n, rows, flush=True)

@@ -46,7 +46,7 @@ def items(p, groups, seqs, cap):
     """Numbers of the groups' items and of the sequences' that have work."""
     rb = [(up(r, p["rbp"]), up(P, UNIT)) for r, P in groups]
     rt = [(up(r, p["rbt"]), max(up(min(L, cap) - a, UNIT), 1)) for r, L, a in seqs]
-    c = max(min(up(sum(b * u for b, u in rb + rt), p["round"]), 1 << 23), 1 if p["rbp"] == 16 else 2)
+    c = max(min(up(sum(b * u for b, u in rb + rt), p["round"]), 1 << 23), 1)
 
     def numbers(blocks, keys_of):
         out, first = [], 0
