@@ -188,9 +188,9 @@ __global__ __launch_bounds__(NT) void k_cache_maps(TablesParams p) {
 // A wave holds 16 state rows in registers as accumulators of S^T tiles: lane 16 lg + j has row j's channels 16 b + 4 lg .. + 3,
 // which is the layout of a product's operand and result alike, so S enters and leaves them without a move.
 // Bound by memory (the state once in, and once out where tokens are kept): 64 sequences, 16 heads of 128, 5 tokens of which 0 to 5
-// are kept, 28.9 us (4.5 TB/s; a copy reaches 5.1); the kept ones of 128 sequences' 1 to 9 tokens alone 46.0 us (4.4 TB/s).  What
+// are kept, 28.5 us (4.6 TB/s; a copy reaches 5.1); the kept ones of 128 sequences' 1 to 9 tokens alone 46.7 us (4.3 TB/s).  What
 // the tokens make among themselves (their products, norms, gates) is done while the state is on its way: asked for ahead of
-// the tokens it took 33.7 and 55.4 us.  32 rows a wave: 30.6 and 47.6 us.  One sequence, 4.9 us: latency.
+// the tokens it took 33.7 and 55.4 us.  32 rows a wave: 30.6 and 47.6 us.  One sequence, 5.3 us: latency.
 constexpr int TT = 8, DROWS = 64;   // tokens of a tile; state rows of a workgroup
 struct DraftParams {
     const void* q;            // or null: no outputs
