@@ -555,7 +555,8 @@ __global__ __launch_bounds__(NT) void k_append_e4m3(RowsParams p, int page_wgs, 
 // Scores, maxima, weight sums and outputs are fp32.  The matrix instruction with the values takes the weights as bf16: two
 // numbers each in k_attn_rows, where its products are nearly free (off by 2^-15; the outputs' error against 64 bits is that of
 // their own rounding, 0.0017), one in k_attn_tile, which such products bound (off by 2^-8 of each at most, up and down over the
-// keys: error 0.0023; with two numbers each 222 us against 168 for the piece below).
+// keys: error 0.0023; with two numbers each 222 us against 168 for the piece below).  gdn_attention_shared, where a decoding
+// batch's rows meet in such blocks, takes two there as well, so that a row is as exact as by itself.
 constexpr int UNIT = 128;
 
 // x / d for 0 <= x < 2^31 by one product: m = ceil(2^sh / d), sh = 31 + ceil(log2 d); m d - 2^sh < d <= 2^(sh - 31), so that x
@@ -1089,7 +1090,9 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
 // and 218 against 196 with the order prescribed to the compiler.
 // k_even .. v_odd: LDS of AKB * DH each (a variable per ring slot: the compiler then sees that reads of one do not wait for the
 // copies into the other).
-template <int DH, typename CT, typename P>
+// SPLIT: as in k_attn_rows, weights in two bf16 numbers each (the values' products twice: 48 sequences behind 65536
+// tokens of an e4m3 cache 65 -> 74 us a call).
+template <int DH, typename CT, bool SPLIT, typename P>
 __device__ __forceinline__ void attn_tile(const P& p, int wg, bf16_t* k_even, bf16_t* v_even, bf16_t* k_odd, bf16_t* v_odd, int& odd) {
     constexpr bool E4M3 = sizeof(CT) == 1;
     constexpr int RB = AQ, QT = 2, NW = NT / 64, NCH = DH / 8, RPI = 64 / NCH, NKB = DH / 32, NDT = DH / 16, ESZ = sizeof(CT);
@@ -1267,7 +1270,7 @@ __device__ __forceinline__ void attn_tile(const P& p, int wg, bf16_t* k_even, bf
                 }
             const bool whole = kb + AKB <= k1 && there == 15;
             float fs[QT], sum[QT];   // the weights are 2^(fs x - m); a lane's sum of them
-            bf16x8 pf[QT][2];
+            bf16x8 pf[QT][2], pl[QT][2];   // the weights (SPLIT: and what is left of them)
             auto weigh = [&](int u) {
                 sum[u] = 0.f;
 #pragma unroll
@@ -1277,8 +1280,14 @@ __device__ __forceinline__ void attn_tile(const P& p, int wg, bf16_t* k_even, bf
                     for (int y = 0; y < 2; ++y)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) w[y][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[u][2 * kk + y][e], fs[u], -m[u]));
-                    pf[u][kk] = pack_bf16(w[0], w[1]);
-                    sum[u] = sum_bf16(pf[u][kk], sum[u]);   // the rounded weights, which the products take
+                    if constexpr (SPLIT) {
+                        split_weights(w[0], w[1], pf[u][kk], pl[u][kk]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sum[u] += w[0][e] + w[1][e];
+                    } else {
+                        pf[u][kk] = pack_bf16(w[0], w[1]);
+                        sum[u] = sum_bf16(pf[u][kk], sum[u]);   // the rounded weights, which the products take
+                    }
                 }
             };
             bool up = false;
@@ -1329,6 +1338,9 @@ __device__ __forceinline__ void attn_tile(const P& p, int wg, bf16_t* k_even, bf
                     const bf16x8 va = join4(lds_tr8(&sv[kq(r, c)]), lds_tr8(&sv[kq(r + 16, c)]));
 #pragma unroll
                     for (int u = 0; u < QT; ++u) oacc[u][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pf[u][kk], oacc[u][t], 0, 0, 0);
+                    if constexpr (SPLIT)
+#pragma unroll
+                        for (int u = 0; u < QT; ++u) oacc[u][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pl[u][kk], oacc[u][t], 0, 0, 0);
                 }
         }
         if (kb + AKB < k1) stage(Ic<1 - SL>{});
@@ -1420,7 +1432,7 @@ template <int DH, typename CT>
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2))) void k_attn_tile(PagedParams p) {
     __shared__ __align__(16) bf16_t k_even[AKB * DH], v_even[AKB * DH], k_odd[AKB * DH], v_odd[AKB * DH];
     __shared__ int odd;
-    attn_tile<DH, CT>(p, blockIdx.x, k_even, v_even, k_odd, v_odd, odd);
+    attn_tile<DH, CT, false>(p, blockIdx.x, k_even, v_even, k_odd, v_odd, odd);
 }
 
 // ------------------------------------------------------------------ k_attn_join

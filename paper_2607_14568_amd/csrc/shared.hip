@@ -218,7 +218,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
         __shared__ __align__(16) bf16_t k_even[AKB * DH], v_even[AKB * DH], k_odd[AKB * DH], v_odd[AKB * DH];
         __shared__ int odd;
         if (FORM == 2 || prefix) {
-            attn_tile<DH, CT>(p, wg, k_even, v_even, k_odd, v_odd, odd);
+            attn_tile<DH, CT, true>(p, wg, k_even, v_even, k_odd, v_odd, odd);
         } else {
             static_assert(16 * ROWS_PITCH<DH> * sizeof(float) <= sizeof k_even, "a wave's sums in a ring slot");
             __shared__ float2 ml[NT / 64][16];
