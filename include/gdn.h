@@ -560,7 +560,8 @@ size_t gdn_attention_shared_workspace_bytes(int B, int T, int H, int H_kv, int d
  * A sequence whose new tokens do not all stand at or behind the group's prefix (a finished or shorter one) is
  * attended by itself.  The prefix's pages are those of the group's first sequence that does reach behind it.
  * Everything else as gdn_attention_paged: causal, pages that are not there, special values, errors; in the
- * products with v a weight is off by 2^-15 of itself at most for every row; at most 2048 sequences
+ * products with v a weight is off by 2^-15 of itself at most for every row (a GDN_E4M3 code's product with
+ * a scale that is no power of two is rounded to bf16 where many rows meet); at most 2048 sequences
  * (GDN_ERR_UNSUPPORTED).  workspace: at least gdn_attention_shared_workspace_bytes(...), 256-byte aligned, its
  * contents on entry ignored; calls that may overlap in time, captured graphs among them, need one each.
  */
