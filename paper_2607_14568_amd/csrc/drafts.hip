@@ -549,7 +549,8 @@ __global__ __launch_bounds__(NT) void k_verify_pick(VerifyParams p) {
         load();
     }
     if (wave != 0) return;
-    const double goal = (u > 0.f ? (double)u : 0.) * lane64(inc, 63);   // (NaN: 0)
+    // 1 or more: past every running sum (which, added up in another order than W, may round past it ahead of the last token).  NaN: 0.
+    const double goal = u >= 1.f ? (double)INFINITY : (u > 0.f ? (double)u : 0.) * lane64(inc, 63);
     // the first lane, slice and token whose running sum passes the goal; each time else the last that holds anything
     int token = -1;
     uint64_t any = __builtin_amdgcn_ballot_w64(sum > 0.), past = __builtin_amdgcn_ballot_w64(sum > 0. && inc > goal);

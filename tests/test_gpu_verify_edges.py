@@ -1,0 +1,41 @@
+"""gdn_draft_verify at the ends of its ranges over rows of many slices: whole numbers, equal to what the definition gives."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2607_14568_amd as gdn
+from paged_cases import f64
+
+pytestmark = pytest.mark.gpu
+IO = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def rows(seed, n, V, io, spread=12.0):
+    """Probabilities [n, V] of a wide spread, in double and rounded to ``io``."""
+    x = spread * np.random.default_rng(seed).standard_normal((n, V))
+    x = np.exp(x - x.max(-1, keepdims=True))
+    return torch.from_numpy(x / x.sum(-1, keepdims=True)).to(IO[io])
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [900, 5000, 9001, 70001])
+@pytest.mark.parametrize("u", [1.0, 1.5, float("inf")])
+def test_one_or_more_draws_the_last_token(u, V, io):
+    """The last token that has any probability, however little, and whatever the order of the sums rounds to."""
+    n = 40
+    p = rows(V, n, V, io)
+    ends = V - 1 - np.arange(n) % 7
+    for s in range(n):
+        p[s, ends[s]:] = 0
+        p[s, ends[s]] = 1e-25
+    t, c = gdn.gdn_draft_verify(p[:, None].contiguous().cuda(), torch.full((n, 1), u).cuda())
+    assert (c == 1).all() and t[:, 0].tolist() == ends.tolist()
+    # behind a draft that is refused, from what is left of p: the same token, which the draft's own row lacks
+    q = rows(V + 1, n, V, io)[:, None].contiguous()
+    x = q[:, 0].argmax(-1, keepdim=True).int()
+    for s in range(n):
+        p[s, x[s, 0]] = 0
+        q[s, 0, ends[s]:] = 0
+    us = torch.tensor([[0.5, u]]).repeat(n, 1)
+    t, c = gdn.gdn_draft_verify(torch.stack([p, p], 1).cuda(), us.cuda(), drafts=x.cuda(), q=q.cuda())
+    assert (c == 1).all() and t[:, 0].tolist() == ends.tolist() and (t[:, 1] == -1).all()
