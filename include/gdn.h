@@ -621,7 +621,8 @@ size_t gdn_draft_verify_workspace_bytes(int n, int m, int V);
  *   counts     [n] int32: the tokens gained, accepted drafts and the next token
  * p and q need not sum to 1 exactly; entries that are not positive and finite count as 0.  Where no
  * max(p_j - q_j, 0) is positive the token is drawn from p_j; where p_j holds nothing either it is -1.
- * Comparisons are exact and sums formed in 64 bits, in a fixed order.  m = 0: drafts, draft_lens and q NULL,
+ * Drafts are compared exactly; sums are formed in 64 bits, in a fixed order, so that a draw within 2^-46 of a
+ * border between two tokens (V up to 2^20) may go to either.  m = 0: drafts, draft_lens and q NULL,
  * one token is drawn from each row.
  */
 gdn_status gdn_draft_verify(const void* p, const void* q, const int32_t* drafts, const int32_t* draft_lens, const float* u,

@@ -386,9 +386,10 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void k_
 // ------------------------------------------------------------------ verification of drafts
 // Token j of a sequence's drafts x_j is accepted while u_j q_j(x_j) < p_j(x_j), both sides exact in 64 bits (a product of two
 // floats has 48).  Where the first is not, the next token is drawn from w = max(p_j - q_j, 0) of that row, behind the last
-// draft from w = p of the row after it: the lowest v with w_0 + .. + w_v > u W, sums in 64 bits, so that no rounding of
-// theirs is seen but where u W falls within 2^-50 of a border.  w = p, too, where no w is positive.  Entries that are not
-// positive and finite count as 0.
+// draft from w = p of the row after it: the lowest v with w_0 + .. + w_v > u W, sums in 64 bits.  Their roundings are
+// seen where u W falls as near to a border as they reach: a running sum passes 59 + 2 c additions on its way at most and W with
+// its product by u 19 + c, c = V / 65536 rounded up (a lane's slices), so (78 + 3 c) 2^-53 of W, 2^-46 of it for a million tokens.
+// w = p, too, where no w is positive.  Entries that are not positive and finite count as 0.
 // k_verify_sums: a wave for each slice of VS tokens of the row that is left, their sum of w; k_verify_pick: the slice that holds
 // u W, then the token in it.  Bound by the two rows' bytes: 64 sequences, rows of 131072 floats (67 MB), 12.0 and 4.0 us (5.6 TB/s);
 // small calls by latency (drafts, their probabilities, the rows, the sums wait for one another): 3.7 and 2.8 for one of 50000.
