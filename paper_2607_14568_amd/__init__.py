@@ -776,8 +776,9 @@ def gdn_draft_verify(p, u, *, drafts=None, q=None, draft_lens=None, tokens=None,
     """Drafted tokens against the target's probabilities; see ``gdn_draft_verify`` in include/gdn.h.
 
     p [n,m+1,V] and q [n,m,V] (None: the drafts were certain) fp32 or bf16, parts of wider rows or not; ``u`` [n,m+1]
-    fp32 in [0, 1); ``drafts`` [n,m] int32 (None: m = 0), ``draft_lens`` [n] int32 (None: m each).  Returns
-    (tokens [n,m+1], counts [n]) int32: the accepted drafts and the token behind them, then -1.
+    fp32 in [0, 1); ``drafts`` [n,m] int32, ``draft_lens`` [n] int32 (None: m each).  m = 0 draws a token from each row: the
+    drafts, their rows and lengths may then be given (empty, the lengths all count as 0) or not.  Returns (tokens
+    [n,m+1], counts [n]) int32: the accepted drafts and the token behind them, then -1.
     """
     pp, ps, dev = _probabilities(p, "p", None)
     n, m, V = p.shape[0], p.shape[1] - 1, p.shape[2]
@@ -798,11 +799,13 @@ def gdn_draft_verify(p, u, *, drafts=None, q=None, draft_lens=None, tokens=None,
     if at[2] is None:
         raise TypeError("u must be a CUDA (HIP) tensor")
     dp, lp, up, tp, cp, ws = at
-    if u.shape != (n, m + 1) or tokens.shape != u.shape or counts.shape != (n,) or (dp and drafts.shape != (n, m)) \
-            or (lp and draft_lens.shape != (n,)):
+    if u.shape != (n, m + 1) or tokens.shape != u.shape or counts.shape != (n,) or (drafts is not None and drafts.shape != (n, m)) \
+            or (draft_lens is not None and draft_lens.shape != (n,)):
         for name, t, shape in (("drafts", drafts, (n, m)), ("draft_lens", draft_lens, (n,)), ("u", u, (n, m + 1)),
                                ("tokens", tokens, (n, m + 1)), ("counts", counts, (n,))):
             _shaped(t, name, shape)
+    if m == 0:   # (nothing of a serving program's buffers is read)
+        qp, qs, dp, lp = None, 0, None, None
     size = 0 if ws is None else workspace.numel()
     _on(dev, lib().gdn_draft_verify, pp, qp, dp, lp, up, tp, cp, n, m, V, ps, qs, _IO[p.dtype], ws if size else None, size)
     return tokens, counts

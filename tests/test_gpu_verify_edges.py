@@ -39,3 +39,23 @@ def test_one_or_more_draws_the_last_token(u, V, io):
     us = torch.tensor([[0.5, u]]).repeat(n, 1)
     t, c = gdn.gdn_draft_verify(torch.stack([p, p], 1).cuda(), us.cuda(), drafts=x.cuda(), q=q.cuda())
     assert (c == 1).all() and t[:, 0].tolist() == ends.tolist() and (t[:, 1] == -1).all()
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("n,V", [(1, 1000), (37, 20001)])
+def test_a_step_without_drafts(n, V, io):
+    """m = 0 with a serving loop's buffers: lengths, whatever they hold, drafts and their rows of no token."""
+    p, u = rows(V, n, V, io, 2.0)[:, None].contiguous(), torch.rand(n, 1, generator=torch.Generator().manual_seed(n))
+    sums = np.cumsum(f64(p)[:, 0].astype(np.longdouble), -1)
+    goal = f64(u)[:, 0].astype(np.longdouble) * sums[:, -1]
+    assert (np.abs(sums - goal[:, None]).min(-1) > 2.0 ** -40).all()   # (no draw on a border)
+    want = [int(np.searchsorted(a, b, side="right")) for a, b in zip(sums, goal)]
+    p, u = p.cuda(), u.cuda()
+    none, lens = torch.empty(n, 0, dtype=torch.int32, device="cuda"), torch.arange(n, dtype=torch.int32, device="cuda") - 3
+    empty = torch.empty(n, 0, V, dtype=IO[io], device="cuda")
+    for kw in ({}, dict(draft_lens=lens), dict(drafts=none), dict(drafts=none, q=empty, draft_lens=lens)):
+        t, c = gdn.gdn_draft_verify(p, u, **kw)
+        assert t[:, 0].tolist() == want and (c == 1).all()
+    for kw in (dict(draft_lens=lens[:0]), dict(drafts=lens[:, None]), dict(q=p), dict(draft_lens=lens.long())):
+        with pytest.raises((ValueError, TypeError)):
+            gdn.gdn_draft_verify(p, u, **kw)
