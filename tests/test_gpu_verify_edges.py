@@ -59,3 +59,29 @@ def test_a_step_without_drafts(n, V, io):
     for kw in (dict(draft_lens=lens[:0]), dict(drafts=lens[:, None]), dict(q=p), dict(draft_lens=lens.long())):
         with pytest.raises((ValueError, TypeError)):
             gdn.gdn_draft_verify(p, u, **kw)
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [300, 5001, 70001, 200003])
+def test_nothing_left_of_the_target(V, io):
+    """q equal to p and a draft that u = 1 refuses: no max(p - q, 0) is positive, and the token is drawn from p by all its slices; the
+    same for a certain draft on a row that holds nothing else."""
+    n = 5
+    p = rows(V, n, V, io, 2.0)
+    u = torch.rand(n, 2, generator=torch.Generator().manual_seed(V))
+    u[:, 0] = 1.0
+    sums = np.cumsum(f64(p).astype(np.longdouble), -1)
+    goal = f64(u)[:, 1].astype(np.longdouble) * sums[:, -1]
+    assert (np.abs(sums - goal[:, None]).min(-1) > 2.0 ** -40).all()   # (no draw on a border)
+    want = [int(np.searchsorted(a, b, side="right")) for a, b in zip(sums, goal)]
+    x = p.argmax(-1, keepdim=True).int()
+    both = torch.stack([p, p.flip(-1)], 1).cuda()
+    for _ in range(3):
+        t, c = gdn.gdn_draft_verify(both, u.cuda(), drafts=x.cuda(), q=both[:, :1].contiguous())
+        assert t[:, 0].tolist() == want and (c == 1).all() and (t[:, 1] == -1).all()
+    one = torch.zeros(n, 2, V, dtype=IO[io])
+    at = [0, V - 1, V // 2, 299, 7]
+    for s in range(n):
+        one[s, 0, at[s]] = 1.0
+    t, c = gdn.gdn_draft_verify(one.cuda(), u.cuda(), drafts=torch.tensor(at, dtype=torch.int32)[:, None].cuda())
+    assert t[:, 0].tolist() == at and (c == 1).all()
