@@ -3265,9 +3265,11 @@ SharedPlan shared_plan(int B, int T, int H, int H_kv, int page, int max_pages, i
     const long units = ((long)page * max_pages + UNIT - 1) / UNIT;
     p.round = (int)std::max(1L, 2 * PLAN_CUS / H_kv);   // two workgroups per CU
     // Blocks of 16 rows where a group, and a sequence, has few on average; a sequence's rows are in a block of 128 only where its
-    // group's are.  Measured by 16 and by 128 (16 heads over 8, bf16): prefixes, 32 rows behind 1000 tokens 13.2 and 16.3 us a
-    // call, behind 8192 19.2 and 18.7, in 4 groups 53.6 and 46.5; 64 rows 16.7 and 19.3, 26.0 and 21.5, 79.3 and 56.5.  Own keys,
-    // 500 to 2000 of 8 sequences: 64 rows 36.6 and 45.0 us, 128 rows 59.1 and 57.2; of 32: 110 and 106, 185 and 153.
+    // group's are.  The rule goes by rows alone: which side wins depends on the lengths, too, which the host does not know.  us a call
+    // by 16 and by 128 (16 heads over 8, bf16), behind 1000 and 8192 tokens: prefixes, one group of 32 rows 12.9 and 14.1, 19.1 and
+    // 19.6, four 25.4 and 22.9, 52.7 and 45.0 (e4m3 23.6 and 22.0, 38.3 and 41.0); one of 64 rows 16.1 and 17.0, 24.6 and 21.4, four
+    // 34.4 and 32.5, 78.3 and 57.7.  Own keys, 500 to 2000 a sequence, 8 of 64 rows 30.9 and 29.8, 48.7 and 52.0, of 128 rows 49.1
+    // and 38.3, 80.5 and 85.0; 32 of 64 rows 93.9 and 80.9, 152 and 164, of 128 rows 156 and 114, 278 and 259.
     p.rbp = rows <= 32L * groups ? 16 : AQ;
     p.rbt = rows <= 64 * n ? 16 : AQ;
     const long blocks_p = rows / p.rbp + std::min<long>(groups, tokens);
