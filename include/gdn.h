@@ -532,7 +532,8 @@ gdn_status gdn_attention_paged(const void* q, const void* k_cache, const void* v
  *   positions   [rows] int32, written: the i-th of m new tokens of s stands at seq_lens[s] - m + i
  *               (rows behind the last sequence: 0)
  *   slots       [rows] int64, written: block_table[s, position / page] * page + position % page, or -1 where
- *               there is no page, and behind the last sequence
+ *               there is no page, and behind the last sequence (where gdn_kv_append, which finds it by itself,
+ *               writes the token: for rows that a caller keeps beside the cache)
  * Errors: GDN_ERR_INVALID_ARG, GDN_ERR_UNSUPPORTED (another page, sizes too large).  Needs no workspace.
  */
 gdn_status gdn_cache_tables(const int32_t* seq_lens, const int32_t* new_lens, const int32_t* shared,
@@ -554,9 +555,9 @@ size_t gdn_attention_shared_workspace_bytes(int B, int T, int H, int H_kv, int d
  *   prefix_lens [n_groups] int32 DEVICE: tokens at the front of every sequence of the group that lie in the
  *               same pages; rounded down to whole pages (below 0 as 0)
  *   cu_groups, n_groups  DEVICE int32 [n_groups + 1]: group g is the sequences cu_groups[g] ..
- *               cu_groups[g + 1] - 1 (cu_groups[0] = 0; offsets outside the contract are clamped into a
- *               nondecreasing partition of [0, n]; sequences behind the last group have no prefix); or NULL
- *               and 1: one group of all.  1 <= n_groups <= n
+ *               cu_groups[g + 1] - 1 (cu_groups[0] is 0 and not read; the others, where outside the contract,
+ *               are clamped into a nondecreasing partition of [0, n]; sequences behind the last group have no
+ *               prefix); or NULL and 1: one group of all.  1 <= n_groups <= n
  * A sequence whose new tokens do not all stand at or behind the group's prefix (a finished or shorter one) is
  * attended by itself.  The prefix's pages are those of the group's first sequence that does reach behind it.
  * Everything else as gdn_attention_paged: causal, pages that are not there, special values, errors; in the

@@ -680,7 +680,7 @@ def gdn_attention_shared(q, k_cache, v_cache, block_table, seq_lens, prefix_lens
     """``gdn_attention_paged`` where groups of sequences share a prefix; see ``gdn_attention_shared`` in include/gdn.h.
 
     ``prefix_lens`` [n_groups] int32: tokens at the front of each group's sequences that lie in the same pages;
-    ``cu_groups`` [n_groups+1] int32 offsets among the sequences (None: one group of all).  Returns o.
+    ``cu_groups`` [n_groups+1] int32 offsets among the sequences, at most 2048 (None: one group of all).  Returns o.
     """
     _dev(q, "q", _BF16)
     if q.dim() != 4:
@@ -775,7 +775,8 @@ def _probabilities(t, name, shape):
 def gdn_draft_verify(p, u, *, drafts=None, q=None, draft_lens=None, tokens=None, counts=None, workspace=None):
     """Drafted tokens against the target's probabilities; see ``gdn_draft_verify`` in include/gdn.h.
 
-    p [n,m+1,V] and q [n,m,V] (None: the drafts were certain) fp32 or bf16, parts of wider rows or not; ``u`` [n,m+1]
+    p [n,m+1,V] and q [n,m,V] (None: the drafts were certain) fp32 or bf16, parts of wider rows or not, but all rows of a
+    tensor equally far apart (a part of a sequence's rows is to be copied); ``u`` [n,m+1]
     fp32 in [0, 1); ``drafts`` [n,m] int32, ``draft_lens`` [n] int32 (None: m each).  m = 0 draws a token from each row: the
     drafts, their rows and lengths may then be given (empty, the lengths all count as 0) or not.  Returns (tokens
     [n,m+1], counts [n]) int32: the accepted drafts and the token behind them, then -1.

@@ -391,8 +391,9 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void k_
 // its product by u 19 + c, c = V / 65536 rounded up (a lane's slices), so (78 + 3 c) 2^-53 of W, 2^-46 of it for a million tokens.
 // w = p, too, where no w is positive.  Entries that are not positive and finite count as 0.
 // k_verify_sums: a wave for each slice of VS tokens of the row that is left, their sum of w; k_verify_pick: the slice that holds
-// u W, then the token in it.  Bound by the two rows' bytes: 64 sequences, rows of 131072 floats (67 MB), 12.0 and 4.0 us (5.6 TB/s);
-// small calls by latency (drafts, their probabilities, the rows, the sums wait for one another): 3.7 and 2.8 for one of 50000.
+// u W, then the token in it.  Bound by the two rows' bytes: 64 sequences, rows of 131072 floats (67 MB, of which 54 came from
+// memory and the rest from the last-level cache), 11.8 and 4.1 us; small calls by latency (drafts, their probabilities, the rows,
+// the sums wait for one another): 3.5 and 2.9 for one of 50000.
 // Waves that take several slices of a sequence, one after another, so that 24 (12) a CU are all there are, look the drafts up
 // less often but wait longer: 96 rows of 100003 floats 16.8 (17.5) us a call against 16.4 of one each, 64 of 131072 in bf16 15.3 (17.7)
 // against 13.2.  Slices of 512: 12.7 us for 96 rows of 100003 in bf16 (11.3 of 1024), 16.8 (16.3) of two in floats, but 5.8 (6.2) for
