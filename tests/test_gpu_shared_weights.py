@@ -61,3 +61,20 @@ def test_weights_keep_more_than_bf16(d, H, Hkv, groups, page, cache):
     average, and by several times that among these thousands.)"""
     print("case: shared weights", cache, page, d, H, Hkv, flush=True)
     check(cache, d, H, Hkv, groups, page)
+
+
+@pytest.mark.parametrize("n,new", [(4, 1), (24, 1), (3, 70)])
+def test_an_infinite_value_of_little_weight(n, new):
+    """An infinity in the prefix under a weight of 2^-92 of the others': its channel is that infinity in every row of either block
+    size, and no other channel is."""
+    table, lens, _, prefix, cg, n_pages = batch([(192, [(40, new)] * n)], 64, 3)
+    k, v = (torch.zeros(n_pages, 1, 64, 64, dtype=torch.bfloat16) for _ in "kv")
+    q = torch.zeros(n, new, 2, 64, dtype=torch.bfloat16)
+    q[..., 0] = 8
+    k[table[0, 1], 0, 9, 0] = -64                        # (8 * 64 / 64^1/2 = 64 = 92.3 log 2)
+    v[table[0, 1], 0, 9, 5] = float("inf")
+    v[table[0, 1], 0, 9, 6] = -float("inf")
+    o = call(q.cuda(), cuda(k, v, None, None), *cuda(i32(table), i32(lens), i32(prefix))).float().cpu()
+    assert (o[..., 5] == float("inf")).all() and (o[..., 6] == -float("inf")).all()
+    o[..., 5:7] = 0
+    assert (o == 0).all()
