@@ -680,7 +680,7 @@ def gdn_attention_shared(q, k_cache, v_cache, block_table, seq_lens, prefix_lens
     """``gdn_attention_paged`` where groups of sequences share a prefix; see ``gdn_attention_shared`` in include/gdn.h.
 
     ``prefix_lens`` [n_groups] int32: tokens at the front of each group's sequences that lie in the same pages;
-    ``cu_groups`` [n_groups+1] int32 offsets among the sequences, at most 2048 (None: one group of all).  Returns o.
+    ``cu_groups`` [n_groups+1] int32 offsets among the sequences (None: one group of all).  At most 2048 sequences.  Returns o.
     """
     _dev(q, "q", _BF16)
     if q.dim() != 4:

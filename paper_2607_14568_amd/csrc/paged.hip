@@ -756,8 +756,8 @@ __device__ __forceinline__ float sum_bf16(bf16x8 w, float c) {
 // Eight weights as two bf16 numbers each, hi + lo, off by 2^-15 of them at most: hi the upper half of the float's bits, lo
 // what is left, under 2^-7 of it, rounded.  2^-20 of the weight more keeps lo's sign that of hi where nothing is left, so that an
 // infinite value's products with both add up to that infinity (0 x infinity and a difference of infinities are NaN), down to
-// weights of 2^-106 at least, whose lo is a normal number in bf16.  (Kept from 0 further down by a maximum and a minimum: 79 us for 75 of 48 sequences behind
-// 65536 tokens, e4m3.)
+// weights of 2^-106 at least, whose lo is a normal number in bf16.  (Kept from 0 further down by a maximum and a minimum:
+// 48 sequences behind 65536 tokens, e4m3, 79 us a call against 75.)
 __device__ __forceinline__ void split_weights(floatx4 a, floatx4 b, bf16x8& hi, bf16x8& lo) {
     int4v h;
 #pragma unroll

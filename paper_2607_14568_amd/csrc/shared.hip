@@ -193,8 +193,9 @@ __device__ __forceinline__ void write_notes(const SharedParams& p, const SharedN
 // other took 21.5 and 35.4 us, this one 45, for 64 sequences behind 8192 tokens with 64 to 2000 of their own (179 MB, 4.0 TB/s;
 // 16 heads over 8, as below).  A prefix is bound by the tile's steps, not by memory: 65536 tokens in e4m3 under 48 sequences, 151 MB,
 // 74 us.  (With weights in one bf16 number 62; 2.85 us for two workgroups' blocks of 64 keys on a CU, of which products, exponentials,
-// loads and conversions were 1.3 to 8 of the 61 us each when left out.)  Tried there, with those weights, without gain: blocks of 32 keys with loads three and four ahead (70 against 64),
-// tiles shared out over the waves, all of a block's LDS reads ahead of its products (spills), an item's head tied to an XCD.
+// loads and conversions were 1.3 to 8 of the 61 us each when left out.)  Tried there, with those weights, without gain: blocks of 32
+// keys with loads three and four ahead (70 against 64), tiles shared out over the waves, all of a block's LDS reads ahead of its
+// products (spills), an item's head tied to an XCD.
 template <int DH, typename CT, int FORM>
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_attn_shared(SharedParams g, SharedParams t, int prefix_wgs, SharedNotes notes) {
     if (blockIdx.x == 0 && threadIdx.x < 64 && !g.part) write_notes(t, notes);
